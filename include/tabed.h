@@ -25,6 +25,8 @@
  *   tabed_draft_body_step, Sec. 5.1 "Ensemble learning via Batched Inference", Sec. 4.1 "Target and Draft
  *   tabed_draft_body_rollback   Models": one decode step of the shared LLaMA-style draft model for the n * B rows.
  *   tabed_draft_step_static     tabed_draft_step for callers that cannot allocate device memory.
+ *   tabed_norm_q8, tabed_linear_q8,                The draft model in 8 bits: norm, product, key / value cache and
+ *   tabed_cache_append_q8, tabed_attention_q8      the attention over it.
  *
  * Notation: n = number of drafting methods (the paper's m), B independent
  * sequences, V vocabulary size, d draft hidden size, gamma block length,
@@ -333,7 +335,95 @@ int tabed_draft_body_rollback(int32_t rows, int32_t rows_per_seq, int32_t gamma,
                               const int32_t* accept_len, int32_t* ctx_len, void* stream);
 
 /*
- * The uniforms the two calls above would draw: out[b,pos,word] for b < B,
+ * The draft model in 8 bits.  Weights, activations and the key / value cache as int8 (-127 .. 127) with fp32 scales: a value is
+ * step * scale.  A scale is 1/127 of the largest magnitude it covers; it is 0, with all steps 0, where no magnitude reaches 2^-100,
+ * and NaN, with all steps 0, where some value is not finite (what reads such a row or block gives NaN, not a number that looks
+ * right).  Storage types of other operands are given as in tabed_cfg.w_dtype: 0 = fp32, 1 = bf16.  Strides count elements; rows
+ * need no more than their type's own alignment unless said otherwise.  rows (M) = 0 and T = 0 are errors, as an empty batch is
+ * everywhere in this library.
+ *
+ * tabed_norm_q8: residual addition, RMSNorm and int8 rows with a scale each.
+ *   r = x + delta;  y = r / sqrt(mean r^2 + eps) * gain;  q = round(y / scale), ties to even
+ *   x     [rows,d] x_dtype in, row stride ldx            delta [rows,d] delta_dtype in, row stride ldd; NULL: r = x
+ *   sum   [rows,d] x_dtype out, row stride lds: r, rounded to that type (the norm is of r before that); may be x itself; NULL: not
+ *                  stored; without delta: NULL
+ *   gain  [d] fp32 in; NULL: no norm, y = r (quantises weights, or activations that are normalised already; eps is not read)
+ *   q     [rows,d] int8 out, row stride ldq              scale [rows] fp32 out
+ *   d 1 .. 32768, rows up to 2^20; strides at least d; a row whose squares exceed fp32 counts as not finite.
+ */
+int tabed_norm_q8(int32_t rows, int32_t d, int32_t x_dtype, const void* x, int64_t ldx, int32_t delta_dtype, const void* delta, int64_t ldd,
+                  void* sum, int64_t lds, const float* gain, float eps, void* q, int64_t ldq, float* scale, void* stream);
+
+/*
+ * tabed_linear_q8: Y[m][n] = (sum_k X[m][k] W[n][k]) * x_scale[m] * w_scale[n].  The sum is exact (int32); then one fp32 product for
+ * each scale, and the rounding to bf16 where y_dtype = 1.
+ *   X [M,K] int8 in, row stride ldx (a multiple of 16)    W [N,K] int8 in     x_scale [M], w_scale [N] fp32 in
+ *   Y [M,N] y_dtype out, row stride ldy >= N
+ *   K a multiple of 16 (pad with zeros), 16 .. 131056, for which the sum of any int8 values fits; N 1 .. 2^24; M 1 .. 2^20; X and W
+ *   16-byte aligned.
+ */
+int tabed_linear_q8(int32_t M, int32_t N, int32_t K, const void* X, int64_t ldx, const float* x_scale, const void* W, const float* w_scale,
+                    int32_t y_dtype, void* Y, int64_t ldy, void* stream);
+
+/*
+ * Key / value cache in 8 bits: a pool of blocks of TABED_CACHE_BLOCK tokens, and for every row a table of the blocks that hold its
+ * tokens, position p in entry p / TABED_CACHE_BLOCK.  Rows may share blocks that are full (a common beginning); a block that
+ * tokens are still appended to belongs to one row.  A table entry outside [0, blocks) is no block: its positions are not there.
+ *   k, v           [blocks, kv_heads, 64 * head_dim] int8; within a block of one head
+ *                  keys   [token / 4 % 4][dim / 16][token / 16][token % 4][dim % 16]
+ *                  values [dim / 16][token / 16][dim % 16][token % 16]
+ *                  (the order in which v_mfma_i32_16x16x64_i8 takes them)
+ *   kscale, vscale [blocks, kv_heads] fp32
+ *   table          [rows, max_blocks] int32
+ * A HOST struct of device pointers; k and v 16-byte aligned.
+ */
+#define TABED_CACHE_BLOCK 64
+typedef struct tabed_cache_q8 {
+    int32_t kv_heads;   /* 1..1024                                   */
+    int32_t head_dim;   /* 32, 64, 96, 128 or 256                    */
+    int32_t blocks;     /* of the pool, >= 1                         */
+    int32_t max_blocks; /* entries of a row of the table, 1..2^24    */
+    void* k;
+    void* v;
+    float* kscale;
+    float* vscale;
+    const int32_t* table;
+} tabed_cache_q8;
+
+/*
+ * tabed_cache_append_q8: quantises the keys and values of up to T new tokens a row into the cache.
+ *   k, v     [rows, T, kv_heads, head_dim] kv_dtype in; row_stride, tok_stride: of a row and of a token; a token's heads lie side by side
+ *   ctx_len  [rows] int32 in   tokens the row holds already; token t goes to position ctx_len[r] + t (not changed by the call; below 0: 0)
+ *   n_new    [rows] int32 in   new tokens of the row, clamped to 0 .. T; NULL: T
+ * A block's scale covers the tokens that it keeps (those before ctx_len) and the new ones: the larger of the old scale, if
+ * any token is kept, and 1/127 of the new tokens' largest magnitude.  Where it grows the kept tokens are rounded again:
+ * q = round(q * old / new).  A token taken back (a smaller ctx_len) leaves the scale it has raised until its block begins anew.
+ * Tokens past the table, or whose entry is no block, are dropped.  Calling again with the same arguments changes nothing.
+ */
+int tabed_cache_append_q8(const tabed_cache_q8* cache, int32_t rows, int32_t T, int32_t kv_dtype, const void* k, const void* v,
+                          int64_t row_stride, int64_t tok_stride, const int32_t* ctx_len, const int32_t* n_new, void* stream);
+
+/*
+ * tabed_attention_q8: causal attention of the T new tokens of every row over its cache, in which they are already
+ * (tabed_cache_append_q8 with the same ctx_len and n_new).  Token t sees positions 0 .. ctx_len[r] + t; query head i reads
+ * key / value head i / (q_heads / kv_heads).  Scores, softmax and sums are as accurate as in fp32: queries and probabilities enter
+ * as 32-bit integers relative to their largest.
+ *   q    [rows, T, q_heads, head_dim] q_dtype in     out  the same, out_dtype, out; both with strides of a row and of a token
+ *   lse  [rows, T, q_heads] fp32 out, optional: natural logarithm of the sum of exp(scale * score)
+ *   scale > 0, commonly 1 / sqrt(head_dim)
+ * A token that sees nothing (its blocks are not there) gets zeros and an lse of -inf.  Entries of tokens from n_new[r] on are left as
+ * they were.  q_heads is a multiple of kv_heads, T * q_heads at most 2^20.
+ * `ws`: tabed_attention_q8_workspace_bytes bytes, prepared once by ..._init, for calls with the same cache sizes, rows, T and q_heads.
+ * Calls that share a workspace must not overlap.
+ */
+size_t tabed_attention_q8_workspace_bytes(const tabed_cache_q8* cache, int32_t rows, int32_t T, int32_t q_heads);   /* 0: invalid */
+int tabed_attention_q8_workspace_init(const tabed_cache_q8* cache, int32_t rows, int32_t T, int32_t q_heads, void* ws, void* stream);
+int tabed_attention_q8(const tabed_cache_q8* cache, void* ws, int32_t rows, int32_t T, int32_t q_heads, int32_t q_dtype, const void* q,
+                       int64_t q_row_stride, int64_t q_tok_stride, const int32_t* ctx_len, const int32_t* n_new, float scale,
+                       int32_t out_dtype, void* out, int64_t out_row_stride, int64_t out_tok_stride, float* lse, void* stream);
+
+/*
+ * The uniforms tabed_draft_step and tabed_verify would draw: out[b,pos,word] for b < B,
  * pos <= gamma, word in {0,1}.  out is [B,gamma+1,2] fp32.
  */
 int tabed_philox_uniforms(const tabed_cfg* cfg, uint64_t round, float* out, void* stream);

@@ -16,6 +16,8 @@ EXPORTS = [
     "tabed_workspace_bytes", "tabed_workspace_init", "tabed_strerror", "tabed_last_hip_error", "tabed_dev_width",
     "tabed_draft_step", "tabed_draft_step_static", "tabed_verify", "tabed_draft_siblings", "tabed_verify_tree", "tabed_update_weights", "tabed_philox_uniforms",
     "tabed_body_workspace_bytes", "tabed_body_workspace_init", "tabed_draft_body_step", "tabed_draft_body_rollback",
+    "tabed_norm_q8", "tabed_linear_q8", "tabed_cache_append_q8",
+    "tabed_attention_q8", "tabed_attention_q8_workspace_bytes", "tabed_attention_q8_workspace_init",
     "tabed_prof_enable", "tabed_prof_read", "tabed_prof_reset", "tabed_kernel_name", "tabed_prof_null",
 ]
 
@@ -41,6 +43,12 @@ class TabedBodyWeights(C.Structure):
     """Mirror of `tabed_body_weights` (device pointers)."""
     _fields_ = [("embed", C.c_void_p), ("g_final", C.c_void_p)] + [
         (name, C.c_void_p * BODY_MAX_LAYERS) for name in ("g_attn", "wqkv", "wo", "g_mlp", "wgu", "wdown")]
+
+
+class TabedCacheQ8(C.Structure):
+    """Mirror of `tabed_cache_q8`."""
+    _fields_ = [("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("blocks", C.c_int32), ("max_blocks", C.c_int32),
+                ("k", C.c_void_p), ("v", C.c_void_p), ("kscale", C.c_void_p), ("vscale", C.c_void_p), ("table", C.c_void_p)]
 
 
 class TabedError(RuntimeError):
@@ -93,6 +101,19 @@ def load():
     lib.tabed_draft_body_step.argtypes = [bcfgp, C.POINTER(TabedBodyWeights), vp, i32, vp, i32, i32] + [vp] * 5
     lib.tabed_draft_body_rollback.restype = C.c_int
     lib.tabed_draft_body_rollback.argtypes = [i32, i32, i32, vp, vp, vp, vp]
+    i64, f32, cachep = C.c_int64, C.c_float, C.POINTER(TabedCacheQ8)
+    lib.tabed_norm_q8.restype = C.c_int
+    lib.tabed_norm_q8.argtypes = [i32, i32, i32, vp, i64, i32, vp, i64, vp, i64, vp, f32, vp, i64, vp, vp]
+    lib.tabed_linear_q8.restype = C.c_int
+    lib.tabed_linear_q8.argtypes = [i32, i32, i32, vp, i64, vp, vp, vp, i32, vp, i64, vp]
+    lib.tabed_cache_append_q8.restype = C.c_int
+    lib.tabed_cache_append_q8.argtypes = [cachep, i32, i32, i32, vp, vp, i64, i64, vp, vp, vp]
+    lib.tabed_attention_q8_workspace_bytes.restype = C.c_size_t
+    lib.tabed_attention_q8_workspace_bytes.argtypes = [cachep, i32, i32, i32]
+    lib.tabed_attention_q8_workspace_init.restype = C.c_int
+    lib.tabed_attention_q8_workspace_init.argtypes = [cachep, i32, i32, i32, vp, vp]
+    lib.tabed_attention_q8.restype = C.c_int
+    lib.tabed_attention_q8.argtypes = [cachep, vp, i32, i32, i32, i32, vp, i64, i64, vp, vp, f32, i32, vp, i64, i64, vp, vp]
     lib.tabed_prof_enable.restype = C.c_int
     lib.tabed_prof_enable.argtypes = [C.c_int]
     lib.tabed_prof_read.restype = C.c_int
@@ -428,6 +449,254 @@ class PreparedCall:
         rc = self.fn(*self.args)
         if rc != 0:
             _check(rc, self.what)
+
+
+# ------------------------------------------------------------------ the draft model in 8 bits
+CACHE_BLOCK = 64
+
+
+class DeviceCall(PreparedCall):
+    """A PreparedCall that makes its tensors' device current and keeps the tensors (and its HOST structs) alive."""
+
+    __slots__ = ("device", "keep")
+
+    def __init__(self, fn, args, what, device, keep):
+        super().__init__(fn, args, what)
+        self.device, self.keep = device, keep
+
+    def __call__(self):
+        import torch
+        if torch.cuda.current_device() == self.device:
+            rc = self.fn(*self.args)
+        else:
+            with torch.cuda.device(self.device):
+                rc = self.fn(*self.args)
+        if rc != 0:
+            _check(rc, self.what)
+
+
+def _device_of(named: dict):
+    """The one device of the tensors given (None entries are left out)."""
+    device = None
+    for name, t in named.items():
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise TabedError(f"{name} must live on the GPU")
+        if device is not None and t.device != device:
+            raise TabedError(f"{name} is on {t.device}, other operands on {device}")
+        device = t.device
+    return device.index
+
+
+def _stream_on(device, stream):
+    import torch
+    if stream is None:
+        return torch.cuda.current_stream(device).cuda_stream
+    if stream.device.index != device:
+        raise TabedError(f"the stream belongs to {stream.device}, the tensors to cuda:{device}")
+    return stream.cuda_stream
+
+
+def _storage_type(t, name):
+    import torch
+    if t.dtype == torch.float32:
+        return 0
+    if t.dtype == torch.bfloat16:
+        return 1
+    raise TabedError(f"{name} must be float32 or bfloat16, got {t.dtype}")
+
+
+def _matrix(t, rows, cols, name, dtype=None):
+    """(pointer, row stride) of a [rows, cols] view whose columns lie side by side (either size may be None: any)."""
+    if t is None:
+        return None, 0
+    if t.dim() != 2 or (rows is not None and t.shape[0] != rows) or (cols is not None and t.shape[1] != cols):
+        raise TabedError(f"{name} must be [{'rows' if rows is None else rows}, {'columns' if cols is None else cols}], got {tuple(t.shape)}")
+    if dtype is not None and t.dtype != dtype:
+        raise TabedError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise TabedError(f"{name}: the values of a row must lie side by side")
+    stride = t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
+    if stride < t.shape[1]:
+        raise TabedError(f"{name}: rows overlap")
+    return t.data_ptr(), stride
+
+
+def _prepare_norm_q8(x, q, scale, delta, sum_out, gain, eps, stream):
+    import torch
+    dev = _device_of(dict(x=x, q=q, scale=scale, delta=delta, sum_out=sum_out, gain=gain))
+    xp, ldx = _matrix(x, None, None, "x")
+    rows, d = x.shape
+    xt = _storage_type(x, "x")
+    dp, ldd = _matrix(delta, rows, d, "delta")
+    sp, lds = _matrix(sum_out, rows, d, "sum_out", x.dtype)
+    qp, ldq = _matrix(q, rows, d, "q", torch.int8)
+    args = [rows, d, xt, xp, ldx, 0 if delta is None else _storage_type(delta, "delta"), dp, ldd, sp, lds,
+            _ptr(gain, torch.float32, d, "gain"), eps, qp, ldq, _ptr(scale, torch.float32, rows, "scale"), _stream_on(dev, stream)]
+    return DeviceCall(load().tabed_norm_q8, args, "tabed_norm_q8", dev, (x, q, scale, delta, sum_out, gain))
+
+
+def tabed_norm_q8(x, q, scale, delta=None, sum_out=None, gain=None, eps=1e-5, stream=None):
+    """Residual addition, RMSNorm, int8 rows with a scale each: sum_out = x + delta, q * scale ~ rms_norm(x + delta) * gain; without
+    a gain the rows are quantised as they are.  x, delta, sum_out: [rows, d] views with their own row strides; sum_out may be x."""
+    _prepare_norm_q8(x, q, scale, delta, sum_out, gain, eps, stream)()
+
+
+def prepare_norm_q8(x, q, scale, delta=None, sum_out=None, gain=None, eps=1e-5, stream=None) -> PreparedCall:
+    return _prepare_norm_q8(x, q, scale, delta, sum_out, gain, eps, stream)
+
+
+def _prepare_linear_q8(x, x_scale, w, w_scale, y, stream):
+    import torch
+    dev = _device_of(dict(x=x, x_scale=x_scale, w=w, w_scale=w_scale, y=y))
+    xp, ldx = _matrix(x, None, None, "x", torch.int8)
+    M, K = x.shape
+    if w.dim() != 2 or w.shape[1] != K:
+        raise TabedError(f"w must be [N, {K}], got {tuple(w.shape)}")
+    N = w.shape[0]
+    yp, ldy = _matrix(y, M, N, "y")
+    args = [M, N, K, xp, ldx, _ptr(x_scale, torch.float32, M, "x_scale"), _ptr(w, torch.int8, N * K, "w"),
+            _ptr(w_scale, torch.float32, N, "w_scale"), _storage_type(y, "y"), yp, ldy, _stream_on(dev, stream)]
+    return DeviceCall(load().tabed_linear_q8, args, "tabed_linear_q8", dev, (x, x_scale, w, w_scale, y))
+
+
+def tabed_linear_q8(x, x_scale, w, w_scale, y, stream=None):
+    """y [M, N] = (x [M, K] @ w [N, K].T) * x_scale[:, None] * w_scale, x and w int8, the sum exact."""
+    _prepare_linear_q8(x, x_scale, w, w_scale, y, stream)()
+
+
+def prepare_linear_q8(x, x_scale, w, w_scale, y, stream=None) -> PreparedCall:
+    return _prepare_linear_q8(x, x_scale, w, w_scale, y, stream)
+
+
+class CacheQ8:
+    """8-bit key / value cache over tensors of the caller's: k, v [blocks, kv_heads, 64 * head_dim] int8, kscale, vscale
+    [blocks, kv_heads] fp32, table [rows, max_blocks] int32 (entries outside [0, blocks): no block).  The struct holds the tensors'
+    addresses: the object keeps them alive."""
+
+    def __init__(self, k, v, kscale, vscale, table, head_dim):
+        import torch
+        self.device = _device_of(dict(k=k, v=v, kscale=kscale, vscale=vscale, table=table))
+        if k.dim() != 3 or k.shape[2] != CACHE_BLOCK * head_dim:
+            raise TabedError(f"k must be [blocks, kv_heads, {CACHE_BLOCK * head_dim}], got {tuple(k.shape)}")
+        if table.dim() != 2:
+            raise TabedError("table must be [rows, max_blocks]")
+        blocks, kvh = k.shape[:2]
+        self.rows, self.head_dim, self.kv_heads = table.shape[0], head_dim, kvh
+        self.k, self.v, self.kscale, self.vscale, self.table = k, v, kscale, vscale, table
+        self.struct = TabedCacheQ8(kvh, head_dim, blocks, table.shape[1], _ptr(k, torch.int8, None, "k"), _ptr(v, torch.int8, k.numel(), "v"),
+                                   _ptr(kscale, torch.float32, blocks * kvh, "kscale"), _ptr(vscale, torch.float32, blocks * kvh, "vscale"),
+                                   _ptr(table, torch.int32, None, "table"))
+
+    @classmethod
+    def allocate(cls, rows, tokens, kv_heads, head_dim, device="cuda:0"):
+        """An empty cache with room for `tokens` tokens in every row, blocks dealt to the rows in order."""
+        import torch
+        width = (tokens + CACHE_BLOCK - 1) // CACHE_BLOCK
+        k = torch.zeros((rows * width, kv_heads, CACHE_BLOCK * head_dim), dtype=torch.int8, device=device)
+        ks = torch.zeros((rows * width, kv_heads), dtype=torch.float32, device=device)
+        table = torch.arange(rows * width, dtype=torch.int32, device=device).view(rows, width)
+        return cls(k, torch.zeros_like(k), ks, torch.zeros_like(ks), table, head_dim)
+
+
+def _heads_view(t, rows, T, heads, hd, name):
+    """(pointer, row stride, token stride) of [rows, T, heads, hd] (or [rows, heads * hd] where T is 1), a token's heads side by side."""
+    if t.dim() == 2 and T == 1:
+        t = t.unsqueeze(1)
+    if t.dim() == 4:
+        if t.shape[2:] != (heads, hd) or (heads > 1 and t.stride(2) != hd):
+            raise TabedError(f"{name}: a token's {heads} heads of {hd} must lie side by side, got {tuple(t.shape)}, strides {t.stride()}")
+    elif t.dim() != 3 or t.shape[2] != heads * hd:
+        raise TabedError(f"{name} must be [{rows}, {T}, {heads}, {hd}], got {tuple(t.shape)}")
+    if t.shape[:2] != (rows, T) or t.stride(-1) != 1:
+        raise TabedError(f"{name} must be [{rows}, {T}, {heads}, {hd}] with values side by side, got {tuple(t.shape)}, strides {t.stride()}")
+    row = t.stride(0) if rows > 1 else max(t.stride(0), T * heads * hd)
+    tok = t.stride(1) if T > 1 else max(t.stride(1), heads * hd)
+    if tok < heads * hd or row < heads * hd or (rows > 1 and T > 1 and min(row, tok) * (T if tok < row else rows) > max(row, tok)):
+        raise TabedError(f"{name}: tokens overlap")
+    return t.data_ptr(), row, tok
+
+
+def _new_tokens(t, heads, hd):
+    return 1 if t.dim() == 2 else t.shape[1]
+
+
+def _prepare_cache_append_q8(cache, k, v, ctx_len, n_new, stream):
+    import torch
+    dev = _device_of({"cache": cache.k, "k": k, "v": v, "ctx_len": ctx_len, "n_new": n_new})
+    T = _new_tokens(k, cache.kv_heads, cache.head_dim)
+    kp, row, tok = _heads_view(k, cache.rows, T, cache.kv_heads, cache.head_dim, "k")
+    vp_, vrow, vtok = _heads_view(v, cache.rows, T, cache.kv_heads, cache.head_dim, "v")
+    if (row, tok) != (vrow, vtok) or k.dtype != v.dtype:
+        raise TabedError("k and v must have the same type and strides")
+    args = [C.byref(cache.struct), cache.rows, T, _storage_type(k, "k"), kp, vp_, row, tok, _ptr(ctx_len, torch.int32, cache.rows, "ctx_len"),
+            _ptr(n_new, torch.int32, cache.rows, "n_new"), _stream_on(dev, stream)]
+    return DeviceCall(load().tabed_cache_append_q8, args, "tabed_cache_append_q8", dev, (cache, k, v, ctx_len, n_new))
+
+
+def tabed_cache_append_q8(cache: CacheQ8, k, v, ctx_len, n_new=None, stream=None):
+    """Quantises k, v [rows, T, kv_heads, head_dim] into the cache at positions ctx_len[r] + t, t < n_new[r] (None: T)."""
+    _prepare_cache_append_q8(cache, k, v, ctx_len, n_new, stream)()
+
+
+def prepare_cache_append_q8(cache: CacheQ8, k, v, ctx_len, n_new=None, stream=None) -> PreparedCall:
+    return _prepare_cache_append_q8(cache, k, v, ctx_len, n_new, stream)
+
+
+def tabed_attention_q8_workspace_bytes(cache: CacheQ8, rows, T, q_heads) -> int:
+    return int(load().tabed_attention_q8_workspace_bytes(C.byref(cache.struct), rows, T, q_heads))
+
+
+def tabed_attention_q8_workspace_init(cache: CacheQ8, rows, T, q_heads, ws, stream=None):
+    import torch
+    dev = _device_of(dict(cache=cache.k, ws=ws))
+    need = tabed_attention_q8_workspace_bytes(cache, rows, T, q_heads)
+    if need == 0 or ws.numel() * ws.element_size() < need:
+        raise TabedError(f"attention workspace holds {ws.numel() * ws.element_size()} bytes, {need} needed (0: invalid sizes)")
+    with torch.cuda.device(dev):
+        _check(load().tabed_attention_q8_workspace_init(C.byref(cache.struct), rows, T, q_heads, _ptr(ws, torch.uint8, None, "ws"),
+                                                        _stream_on(dev, stream)), "tabed_attention_q8_workspace_init")
+
+
+def new_attention_workspace(cache: CacheQ8, rows, T, q_heads, stream=None):
+    """Allocate (torch) and prepare the workspace of tabed_attention_q8 for these sizes."""
+    import torch
+    nbytes = tabed_attention_q8_workspace_bytes(cache, rows, T, q_heads)
+    if nbytes == 0:
+        raise TabedError("invalid or unsupported attention sizes")
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=cache.k.device)
+    tabed_attention_q8_workspace_init(cache, rows, T, q_heads, ws, stream)
+    return ws
+
+
+def _prepare_attention_q8(cache, ws, q, ctx_len, out, n_new, scale, lse, stream):
+    import torch
+    dev = _device_of(dict(cache=cache.k, ws=ws, q=q, ctx_len=ctx_len, out=out, n_new=n_new, lse=lse))
+    hd = cache.head_dim
+    T = _new_tokens(q, None, hd)
+    heads = q.shape[2] if q.dim() == 4 else q.shape[-1] // hd
+    qp, qrow, qtok = _heads_view(q, cache.rows, T, heads, hd, "q")
+    op, orow, otok = _heads_view(out, cache.rows, T, heads, hd, "out")
+    need = tabed_attention_q8_workspace_bytes(cache, cache.rows, T, heads)
+    if ws.numel() * ws.element_size() < need:
+        raise TabedError(f"attention workspace holds {ws.numel() * ws.element_size()} bytes, {need} needed")
+    args = [C.byref(cache.struct), _ptr(ws, torch.uint8, None, "ws"), cache.rows, T, heads, _storage_type(q, "q"), qp, qrow, qtok,
+            _ptr(ctx_len, torch.int32, cache.rows, "ctx_len"), _ptr(n_new, torch.int32, cache.rows, "n_new"),
+            hd ** -0.5 if scale is None else scale, _storage_type(out, "out"), op, orow, otok,
+            _ptr(lse, torch.float32, cache.rows * T * heads, "lse"), _stream_on(dev, stream)]
+    return DeviceCall(load().tabed_attention_q8, args, "tabed_attention_q8", dev, (cache, ws, q, ctx_len, out, n_new, lse))
+
+
+def tabed_attention_q8(cache: CacheQ8, ws, q, ctx_len, out, n_new=None, scale=None, lse=None, stream=None):
+    """out [rows, T, q_heads, head_dim]: causal attention of q over the cache; token t sees positions up to ctx_len[r] + t, which
+    tabed_cache_append_q8 has filled.  scale: 1 / sqrt(head_dim) unless given; lse [rows, T, q_heads]: optional."""
+    _prepare_attention_q8(cache, ws, q, ctx_len, out, n_new, scale, lse, stream)()
+
+
+def prepare_attention_q8(cache: CacheQ8, ws, q, ctx_len, out, n_new=None, scale=None, lse=None, stream=None) -> PreparedCall:
+    return _prepare_attention_q8(cache, ws, q, ctx_len, out, n_new, scale, lse, stream)
+
 
 
 class BodyBuffers:

@@ -2,6 +2,7 @@
 // layout, launch sequencing, optional per-kernel event timing.  No allocation, no synchronisation,
 // except inside the tabed_prof_* calls.
 #include <atomic>
+#include <cmath>
 #include <mutex>
 #include <vector>
 
@@ -105,6 +106,20 @@ static int fail_hip(hipError_t e) {
     return TABED_EHIP;
 }
 static bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
+static bool storage_type(int32_t t) { return t == 0 || t == 1; }
+static bool element_misaligned(const void* p, int32_t type) { return (reinterpret_cast<uintptr_t>(p) & (type == 1 ? 1u : 3u)) != 0; }
+constexpr int64_t kMaxWorkgroups = 1 << 23;      // of the 8-bit cache's launches, 256 threads each: a grid has fewer than 2^32
+
+static int validate_cache(const tabed_cache_q8* c, bool pointers) {
+    if (c == nullptr) return TABED_ENULL;
+    if (c->kv_heads < 1 || c->kv_heads > 1024 || c->blocks < 1 || c->max_blocks < 1 || c->max_blocks > (1 << 24)) return TABED_ERANGE;
+    if (c->head_dim != 32 && c->head_dim != 64 && c->head_dim != 96 && c->head_dim != 128 && c->head_dim != 256) return TABED_EINVAL;
+    if (!pointers) return TABED_OK;
+    if (!c->k || !c->v || !c->kscale || !c->vscale || !c->table) return TABED_ENULL;
+    if (misaligned(c->k) || misaligned(c->v) || element_misaligned(c->kscale, 0) || element_misaligned(c->vscale, 0) || element_misaligned(c->table, 0))
+        return TABED_EALIGN;
+    return TABED_OK;
+}
 
 // ---------------------------------------------------------------- built-in scratch of tabed_draft_step_static
 // One array per GPU, part of the loaded code object, so no call ever allocates it.  `scratch` is only a
@@ -377,6 +392,91 @@ int tabed_draft_body_rollback(int32_t rows, int32_t rows_per_seq, int32_t gamma,
     if (rows < 1 || rows_per_seq < 1 || gamma < 1) return TABED_ERANGE;
     const hipError_t e = launch_body_rollback(rows, rows_per_seq, gamma, ctx_base, accept_len, ctx_len,
                                               static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? TABED_OK : fail_hip(e);
+}
+
+// ---------------------------------------------------------------- 8-bit operators
+int tabed_norm_q8(int32_t rows, int32_t d, int32_t x_dtype, const void* x, int64_t ldx, int32_t delta_dtype, const void* delta, int64_t ldd,
+                  void* sum, int64_t lds, const float* gain, float eps, void* q, int64_t ldq, float* scale, void* stream) {
+    if (!x || !q || !scale) return TABED_ENULL;
+    if (rows < 1 || rows > (1 << 20) || d < 1 || d > 32768) return TABED_ERANGE;
+    if (!storage_type(x_dtype) || (delta != nullptr && !storage_type(delta_dtype))) return TABED_EINVAL;
+    if (sum != nullptr && delta == nullptr) return TABED_EINVAL;
+    if (ldx < d || ldq < d || (delta != nullptr && ldd < d) || (sum != nullptr && lds < d)) return TABED_EINVAL;
+    if (gain != nullptr && !(eps > 0.f)) return TABED_EINVAL;
+    if (element_misaligned(x, x_dtype) || element_misaligned(sum, x_dtype) || element_misaligned(delta, delta_dtype) ||
+        element_misaligned(gain, 0) || element_misaligned(scale, 0))
+        return TABED_EALIGN;
+    const hipError_t e = launch_norm_q8(rows, d, x_dtype, x, ldx, delta_dtype, delta, ldd, sum, lds, gain, eps, static_cast<int8_t*>(q), ldq, scale,
+                                        nullptr, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? TABED_OK : fail_hip(e);
+}
+
+int tabed_linear_q8(int32_t M, int32_t N, int32_t K, const void* X, int64_t ldx, const float* x_scale, const void* W, const float* w_scale,
+                    int32_t y_dtype, void* Y, int64_t ldy, void* stream) {
+    if (!X || !x_scale || !W || !w_scale || !Y) return TABED_ENULL;
+    if (M < 1 || M > (1 << 20) || N < 1 || N > (1 << 24) || K < 16 || K > 131056) return TABED_ERANGE;
+    if (K % 16 != 0 || ldx % 16 != 0 || ldx < K || ldy < N || !storage_type(y_dtype)) return TABED_EINVAL;
+    if (misaligned(X) || misaligned(W) || element_misaligned(Y, y_dtype) || element_misaligned(x_scale, 0) || element_misaligned(w_scale, 0))
+        return TABED_EALIGN;
+    const hipError_t e = launch_linear_q8(M, N, K, static_cast<const int8_t*>(X), ldx, x_scale, static_cast<const int8_t*>(W), w_scale, y_dtype, Y, ldy,
+                                          static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? TABED_OK : fail_hip(e);
+}
+
+int tabed_cache_append_q8(const tabed_cache_q8* cache, int32_t rows, int32_t T, int32_t kv_dtype, const void* k, const void* v,
+                          int64_t row_stride, int64_t tok_stride, const int32_t* ctx_len, const int32_t* n_new, void* stream) {
+    const int rc = validate_cache(cache, true);
+    if (rc != TABED_OK) return rc;
+    if (!k || !v || !ctx_len) return TABED_ENULL;
+    if (rows < 1 || rows > 65535 || T < 1 || T > (1 << 20)) return TABED_ERANGE;
+    if (append_workgroups(*cache, rows, T) > kMaxWorkgroups) return TABED_ERANGE;
+    const int64_t heads = (int64_t)cache->kv_heads * cache->head_dim;
+    if (!storage_type(kv_dtype) || tok_stride < heads || row_stride < heads) return TABED_EINVAL;
+    if (element_misaligned(k, kv_dtype) || element_misaligned(v, kv_dtype) || element_misaligned(ctx_len, 0) || element_misaligned(n_new, 0))
+        return TABED_EALIGN;
+    const hipError_t e = launch_cache_append(*cache, rows, T, kv_dtype, k, v, row_stride, tok_stride, ctx_len, n_new, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? TABED_OK : fail_hip(e);
+}
+
+static int validate_attention(const tabed_cache_q8* cache, int32_t rows, int32_t T, int32_t q_heads, bool pointers) {
+    const int rc = validate_cache(cache, pointers);
+    if (rc != TABED_OK) return rc;
+    if (rows < 1 || rows > 65535 || T < 1 || q_heads < 1) return TABED_ERANGE;
+    if ((int64_t)T * q_heads > (1 << 20)) return TABED_ERANGE;
+    if (q_heads % cache->kv_heads != 0) return TABED_EINVAL;
+    if (attn_workgroups(*cache, rows, T, q_heads) > kMaxWorkgroups) return TABED_ERANGE;
+    return TABED_OK;
+}
+
+size_t tabed_attention_q8_workspace_bytes(const tabed_cache_q8* cache, int32_t rows, int32_t T, int32_t q_heads) {
+    if (validate_attention(cache, rows, T, q_heads, false) != TABED_OK) return 0;
+    return attn_layout(*cache, rows, T, q_heads).total;
+}
+
+int tabed_attention_q8_workspace_init(const tabed_cache_q8* cache, int32_t rows, int32_t T, int32_t q_heads, void* ws, void* stream) {
+    const int rc = validate_attention(cache, rows, T, q_heads, false);
+    if (rc != TABED_OK) return rc;
+    if (ws == nullptr) return TABED_ENULL;
+    if (misaligned(ws)) return TABED_EALIGN;
+    const hipError_t e = launch_attn_init(*cache, rows, T, q_heads, static_cast<char*>(ws), static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? TABED_OK : fail_hip(e);
+}
+
+int tabed_attention_q8(const tabed_cache_q8* cache, void* ws, int32_t rows, int32_t T, int32_t q_heads, int32_t q_dtype, const void* q,
+                       int64_t q_row_stride, int64_t q_tok_stride, const int32_t* ctx_len, const int32_t* n_new, float scale,
+                       int32_t out_dtype, void* out, int64_t out_row_stride, int64_t out_tok_stride, float* lse, void* stream) {
+    const int rc = validate_attention(cache, rows, T, q_heads, true);
+    if (rc != TABED_OK) return rc;
+    if (!ws || !q || !ctx_len || !out) return TABED_ENULL;
+    const int64_t heads = (int64_t)q_heads * cache->head_dim;
+    if (!storage_type(q_dtype) || !storage_type(out_dtype) || !(scale > 0.f) || !(scale < INFINITY)) return TABED_EINVAL;
+    if (q_row_stride < heads || q_tok_stride < heads || out_row_stride < heads || out_tok_stride < heads) return TABED_EINVAL;
+    if (misaligned(ws) || element_misaligned(q, q_dtype) || element_misaligned(out, out_dtype) || element_misaligned(ctx_len, 0) ||
+        element_misaligned(n_new, 0) || element_misaligned(lse, 0))
+        return TABED_EALIGN;
+    const hipError_t e = launch_attention_q8(*cache, static_cast<char*>(ws), rows, T, q_heads, q_dtype, q, q_row_stride, q_tok_stride, ctx_len, n_new,
+                                             scale, out_dtype, out, out_row_stride, out_tok_stride, lse, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? TABED_OK : fail_hip(e);
 }
 

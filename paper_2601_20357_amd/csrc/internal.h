@@ -139,6 +139,28 @@ hipError_t launch_gang(const tabed_body_cfg& c, const tabed_body_weights& w, cha
 hipError_t launch_body_rollback(int rows, int rows_per_seq, int gamma, const int32_t* ctx_base, const int32_t* accept_len,
                                 int32_t* ctx_len, hipStream_t s);
 
+// ---------------------------------------------------------------- 8-bit operators (arguments checked by the caller)
+hipError_t launch_norm_q8(int rows, int d, int x_dtype, const void* x, int64_t ldx, int delta_dtype, const void* delta, int64_t ldd, void* sum,
+                          int64_t lds, const float* g, float eps, int8_t* q, int64_t ldq, float* scale, int32_t* advance, hipStream_t s);
+hipError_t launch_linear_q8(int M, int N, int K, const int8_t* X, int64_t ldx, const float* sx, const int8_t* W, const float* sw, int y_dtype,
+                            void* Y, int64_t ldy, hipStream_t s);
+int64_t append_workgroups(const tabed_cache_q8& c, int rows, int T);
+hipError_t launch_cache_append(const tabed_cache_q8& c, int rows, int T, int kv_dtype, const void* k, const void* v, int64_t row_stride,
+                               int64_t tok_stride, const int32_t* ctx_len, const int32_t* n_new, hipStream_t s);
+struct AttnLayout {
+    int tiles, S;        // workgroups of a row and key / value head, times ranges of blocks
+    size_t units;        // uint32 [rows, kv_heads, tiles] arrival counters, first in the workspace
+    size_t off_po;       // float [units][S][queries of a workgroup][head_dim]: more than one range only
+    size_t off_pml;      // float [units][S][2][queries of a workgroup]
+    size_t total;
+};
+AttnLayout attn_layout(const tabed_cache_q8& c, int rows, int T, int q_heads);
+int64_t attn_workgroups(const tabed_cache_q8& c, int rows, int T, int q_heads);
+hipError_t launch_attn_init(const tabed_cache_q8& c, int rows, int T, int q_heads, char* ws, hipStream_t s);
+hipError_t launch_attention_q8(const tabed_cache_q8& c, char* ws, int rows, int T, int q_heads, int q_dtype, const void* q, int64_t q_row,
+                               int64_t q_tok, const int32_t* ctx_len, const int32_t* n_new, float scale, int out_dtype, void* out,
+                               int64_t out_row, int64_t out_tok, float* lse, hipStream_t s);
+
 // ---------------------------------------------------------------- event timing
 // While timing is enabled a launch goes through hipExtLaunchKernelGGL, which attaches a start and a stop
 // event to the dispatch itself: the pair measures the kernel's own begin-to-end time (what a kernel trace

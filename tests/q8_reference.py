@@ -1,0 +1,127 @@
+"""Plain definitions of the 8-bit operators for the tests, on the CPU: numpy / torch in 64 bits, or, where the definition fixes every
+rounding (appending to the cache), in fp32 step by step."""
+import math
+
+import numpy as np
+import torch
+
+BLOCK = 64
+TINY = np.float32(2.0 ** -100)
+
+
+def half_step(dtype):
+    """Largest relative error of one rounding to the type."""
+    return torch.finfo(dtype).eps / 2
+
+
+# ------------------------------------------------------------------ norm
+def norm(x, delta, gain, eps):
+    """(r, y, scale) in 64 bits."""
+    r = x.double() + (0 if delta is None else delta.double())
+    y = r
+    if gain is not None:
+        y = r / torch.sqrt(r.pow(2).mean(1, keepdim=True) + eps) * gain.double()
+    most = y.abs().amax(1)
+    return r, y, torch.where(most >= float(TINY), most / 127, torch.zeros_like(most))
+
+
+# ------------------------------------------------------------------ the cache's layout, element by element
+def key_at(tok, dim, hd):
+    return (((tok // 4 % 4) * (hd // 16) + dim // 16) * 16 + tok // 16 * 4 + tok % 4) * 16 + dim % 16
+
+
+def value_at(tok, dim, hd):
+    return ((dim // 16 * 4 + tok // 16) * 16 + dim % 16) * 16 + tok % 16
+
+
+def layout(which, hd):
+    """Index [64, hd] into a block's bytes."""
+    tok, dim = np.arange(BLOCK)[:, None], np.arange(hd)[None, :]
+    return key_at(tok, dim, hd) if which == "k" else value_at(tok, dim, hd)
+
+
+def fp32_scale(most):
+    return np.float32(np.nan) if not np.isfinite(most) else (np.float32(most) / np.float32(127) if most >= TINY else np.float32(0))
+
+
+def steps(x, s):
+    if not s > 0:
+        return np.zeros(x.shape, np.int8)
+    return np.clip(np.rint(x.astype(np.float32) / np.float32(s)), -127, 127).astype(np.int8)
+
+
+def append(pool, scales, table, which, new, ctx, n_new, hd):
+    """pool [blocks, kv_heads, 64 hd] int8 and scales [blocks, kv_heads] fp32, changed in place; new [rows, T, kv_heads, hd] fp32."""
+    where = layout(which, hd)
+    blocks, kvh = scales.shape
+    rows, T = new.shape[:2]
+    for r in range(rows):
+        n = T if n_new is None else min(max(int(n_new[r]), 0), T)
+        at, end = max(int(ctx[r]), 0), max(int(ctx[r]), 0) + n
+        first = at
+        while at < end:
+            slot, off = divmod(at, BLOCK)
+            count = min(BLOCK - off, end - at)
+            if slot >= table.shape[1]:
+                break
+            page = int(table[r, slot])
+            if 0 <= page < blocks:
+                for h in range(kvh):
+                    x = new[r, at - first:at - first + count, h].astype(np.float32)
+                    with np.errstate(invalid="ignore"):
+                        most = np.float32(np.nan) if not np.isfinite(x).all() else np.abs(x).max()
+                    fresh, before = fp32_scale(most), scales[page, h] if off else np.float32(0)
+                    s = np.float32(np.nan) if np.isnan(fresh) or np.isnan(before) else max(fresh, before)
+                    block = pool[page, h][where]
+                    if off and s != before:
+                        kept = block[:off].astype(np.float32) * before if s > 0 else np.zeros((off, hd), np.float32)
+                        block[:off] = steps(kept, s)
+                    block[off:off + count] = steps(x, s)
+                    pool[page, h][where] = block
+                    scales[page, h] = s
+            at += count
+
+
+# ------------------------------------------------------------------ attention
+def attention(pools, scales, table, q, ctx, n_new, scale, hd):
+    """(out, lse, bound) in 64 bits; tokens from n_new on hold NaN.  pools, scales: {"k", "v"}; q [rows, T, q_heads, hd].
+
+    bound [rows, T, q_heads]: how far the kernel may be from `out`, by counting its roundings.  A score is four integers, exact, each
+    rounded to fp32, scaled by a product of four roundings, and added: at most 8 half steps of A = sum_d (|q_d| + max|q| 2^-7) |k_d| * scale
+    (a digit's share can exceed its value by the balanced digits' carry, 1/128 of the next one), and the fixed point itself half a
+    unit of 2^-30 max|q| a dimension, below that.  In base 2 its difference from the maximum is rounded once more, and exp2 is good to 2 half
+    steps: a probability is off by e = ln 2 * (10 A + |s - m|) half steps + 2, of which |s - m| matters only while exp2 of it does (|s - m| 2^-|s - m| < 1).
+    Sums of p and of p v run over at most the row's blocks, 16 terms and a chain each, plus joins (waves, ranges): (blocks + 16 + 64 + 140) half steps
+    of sum p |v|; p itself is kept to 2^-31 of the largest.  Scale of the value, division: 3 more."""
+    rows, T, qh, _ = q.shape
+    kvh = scales["k"].shape[1]
+    group, u = qh // kvh, 2.0 ** -24
+    out, lse = np.full((rows, T, qh, hd), np.nan), np.full((rows, T, qh), np.nan)
+    bound = np.zeros((rows, T, qh))
+    for r in range(rows):
+        n = T if n_new is None else min(max(int(n_new[r]), 0), T)
+        cap = table.shape[1] * BLOCK
+        c = min(max(int(ctx[r]), 0), cap)
+        held = [b for b in range(min(table.shape[1], (c + n + BLOCK - 1) // BLOCK)) if 0 <= table[r, b] < scales["k"].shape[0]]
+        pos = np.array([b * BLOCK + i for b in held for i in range(BLOCK)], np.int64)
+        for h in range(kvh):
+            k, v = (np.concatenate([pools[n_][table[r, b], h][layout(n_, hd)].astype(np.float64) * float(scales[n_][table[r, b], h]) for b in held])
+                    if held else np.zeros((0, hd)) for n_ in ("k", "v"))
+            for t in range(n):
+                seen = pos <= c + t
+                for j in range(group):
+                    i = h * group + j
+                    if not seen.any():
+                        out[r, t, i], lse[r, t, i] = 0, -math.inf
+                        continue
+                    qq = q[r, t, i].astype(np.float64)
+                    s = k[seen] @ qq * scale
+                    m = s.max()
+                    p = np.exp(s - m)
+                    out[r, t, i], lse[r, t, i] = p @ v[seen] / p.sum(), m + math.log(p.sum())
+                    A = ((np.abs(qq) + np.abs(qq).max() / 128) @ np.abs(k[seen]).T).max() * scale / math.log(2)
+                    e = math.log(2) * (10 * A + 1) + 2
+                    w = p @ np.abs(v[seen]) / p.sum()
+                    lost = seen.sum() * 2.0 ** -31 / p.sum() * np.abs(v[seen]).max(0)
+                    bound[r, t, i] = ((2 * e + 2 * (len(held) + 220) + 3) * u * w + lost).max()
+    return out, lse, bound
