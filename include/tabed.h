@@ -359,7 +359,7 @@ int tabed_norm_q8(int32_t rows, int32_t d, int32_t x_dtype, const void* x, int64
  * each scale, and the rounding to bf16 where y_dtype = 1.
  *   X [M,K] int8 in, row stride ldx (a multiple of 16)    W [N,K] int8 in     x_scale [M], w_scale [N] fp32 in
  *   Y [M,N] y_dtype out, row stride ldy >= N
- *   K a multiple of 16 (pad with zeros), 16 .. 131056, for which the sum of any int8 values fits; N 1 .. 2^24; M 1 .. 2^20; X and W
+ *   K a multiple of 16 (pad with zeros), 16 .. 131056, for which the sum of any int8 values fits; N 1 .. 2^24; M 1 .. 2^20; M N up to 2^36; ldx up to 2^22; X and W
  *   16-byte aligned.
  */
 int tabed_linear_q8(int32_t M, int32_t N, int32_t K, const void* X, int64_t ldx, const float* x_scale, const void* W, const float* w_scale,

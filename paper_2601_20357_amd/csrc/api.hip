@@ -126,7 +126,6 @@ static int validate_cache(const tabed_cache_q8* c, bool pointers) {
 // host-side handle: the array's device address on the current GPU comes from hipGetSymbolAddress, looked up once
 // per device, and that pointer is what kernels and launchers receive.
 static __device__ __attribute__((used)) __align__(256) unsigned char scratch[TABED_STATIC_SCRATCH_BYTES];
-constexpr int kMaxDevices = 64;
 static std::mutex g_scratch_mu;
 static void* g_scratch_ptr[kMaxDevices];
 
@@ -415,7 +414,8 @@ int tabed_norm_q8(int32_t rows, int32_t d, int32_t x_dtype, const void* x, int64
 int tabed_linear_q8(int32_t M, int32_t N, int32_t K, const void* X, int64_t ldx, const float* x_scale, const void* W, const float* w_scale,
                     int32_t y_dtype, void* Y, int64_t ldy, void* stream) {
     if (!X || !x_scale || !W || !w_scale || !Y) return TABED_ENULL;
-    if (M < 1 || M > (1 << 20) || N < 1 || N > (1 << 24) || K < 16 || K > 131056) return TABED_ERANGE;
+    if (M < 1 || M > (1 << 20) || N < 1 || N > (1 << 24) || K < 16 || K > 131056 || ldx > (1 << 22)) return TABED_ERANGE;
+    if ((int64_t)M * N > (1ll << 36)) return TABED_ERANGE;
     if (K % 16 != 0 || ldx % 16 != 0 || ldx < K || ldy < N || !storage_type(y_dtype)) return TABED_EINVAL;
     if (misaligned(X) || misaligned(W) || element_misaligned(Y, y_dtype) || element_misaligned(x_scale, 0) || element_misaligned(w_scale, 0))
         return TABED_EALIGN;

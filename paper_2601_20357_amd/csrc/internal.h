@@ -9,6 +9,7 @@
 
 namespace tabed {
 
+constexpr int kMaxDevices = 64; // GPUs that one process uses
 constexpr int kWave = 64;
 constexpr int kBlock = 256;     // every vocab-pass kernel runs 4 waves per workgroup
 constexpr int kWavesPerBlock = kBlock / kWave;
