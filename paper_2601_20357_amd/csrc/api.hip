@@ -108,7 +108,7 @@ static int fail_hip(hipError_t e) {
 static bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 static bool storage_type(int32_t t) { return t == 0 || t == 1; }
 static bool element_misaligned(const void* p, int32_t type) { return (reinterpret_cast<uintptr_t>(p) & (type == 1 ? 1u : 3u)) != 0; }
-constexpr int64_t kMaxWorkgroups = 1 << 23;      // of the 8-bit cache's launches, 256 threads each: a grid has fewer than 2^32
+constexpr int64_t kMaxWorkgroups = (1 << 23) - 1;      // of the 8-bit cache's launches, up to 2^9 threads each: a grid has fewer than 2^32
 
 static int validate_cache(const tabed_cache_q8* c, bool pointers) {
     if (c == nullptr) return TABED_ENULL;

@@ -162,21 +162,26 @@ hipError_t launch_cache_append(const tabed_cache_q8& c, int rows, int T, int kv_
 }
 
 // ---------------------------------------------------------------- attention
-// One wave walks over blocks of one row and key / value head for CT column tiles of four queries (a query: one new token and one of
-// the heads that share the key / value head).  Scores are S^T = K Q^T and outputs O^T = V^T P^T with v_mfma_i32_16x16x64_i8: the cache's
-// bytes are operands as they are, and a query's 32-bit values stand in four columns, one for each digit of base 256:
-//   q = max|q| 2^-30 (d3 256^3 + d2 256^2 + d1 256 + d0),  p 2^30 = the same,  digits -128 .. 127.
-// Products and their sums are exact integers, and what fixed point costs is below fp32's own rounding: 2^-31 of the row's largest |q|, and
-// of the largest probability.  (Converting the cache to bf16 instead is one and a half vector instructions a byte, at which a
-// compute unit takes in less than memory delivers, and rounds p to 8 bits.)
-// Lane (g = lane / 16, c = lane % 16) has column c = 4 query + digit.  Its 16 scores of a block are those of tokens 16 g .. 16 g + 15, which
-// are also the 16 bytes that it gives to the second product: probabilities never leave the lane.
-// The four waves of a workgroup take blocks in turn and meet in LDS; a row's blocks are cut into S ranges where the rows and heads do
+// A query is one new token and one of the `group` heads that share a key / value head.  One wave walks over blocks of a row and key / value
+// head: scores S^T = K Q^T, outputs O^T = V^T P^T, the cache as the row operand of both products, softmax with a running maximum and sum.  The
+// lane that holds the scores of tokens 16 g .. 16 g + 15 (g = lane / 16) for a column (lane % 16) is the one that has to hold their
+// probabilities for the second product: they never leave it.  K of the next block is requested when the scores are there, V when
+// the outputs are.
+// Cached bytes go into the products as they are or exactly converted; queries and probabilities with 22 bits and more:
+//   * scores: v_mfma_i32_16x16x64_i8.  A query is integers relative to its largest, in digits of base 256 (-128 .. 127) that are multiplied
+//     one by one; the products and their sums are exact.
+//   * up to four queries (a step's token, up to four heads a group): four digits stand in four columns, lane 4 query + digit adds them up,
+//     and the probabilities (2^30 for 1) go the same way into v_mfma_i32_16x16x64_i8.  Nothing is converted.
+//   * more queries: sixteen, a column each; three digits are three products.  Probabilities (2^14 for 1) are the sum of two halves, for
+//     v_mfma_f32_16x16x32_f16, and the values' bytes become halves on the way, five vector instructions for four of them.  Digits
+//     would take half as many instructions again for the sixteen, and four times as many with the layout above.  Vector instructions
+//     bound this form from about 1000 tokens a row on: 380 a block of 128 dims, of which converting the values is 160.
+// The waves of a workgroup take blocks in turn and meet in LDS; a row's blocks are cut into S ranges where the rows and heads do
 // not fill the chip, and the last of its workgroups to arrive joins them (in range order: results do not depend on who is last).
 struct AttnArgs {
     CacheView c;
     int rows, T, group;          // group: query heads of a key / value head
-    int tiles;                   // workgroups of one row and key / value head: queries / (4 CT), rounded up
+    int tiles;                   // workgroups of one row and key / value head (and range)
     int S;                       // ranges of blocks
     int q_bf16, out_bf16;
     const void* q;
@@ -188,11 +193,20 @@ struct AttnArgs {
     const int32_t* n_new;
     float scale2;                // scale * log2(e)
     uint32_t* arrivals;          // [rows, kv_heads, tiles]
-    float* po;                   // [rows, kv_heads, tiles, S][4 CT][hd]: sums of p v, at the range's own maximum
-    float* pml;                  // the same [2][4 CT]: maxima (base 2), sums of p
+    float* po;                   // [rows, kv_heads, tiles, S][queries][hd]: sums of p v, at the range's own maximum
+    float* pml;                  // the same [2][queries]: maxima (base 2), sums of p
 };
 
-constexpr int kMinRange = 4;     // blocks: one for each wave
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
+typedef float f32x4v __attribute__((ext_vector_type(4)));
+typedef float f32x2_any __attribute__((ext_vector_type(2), aligned(4)));
+typedef uint32_t u32_e2 __attribute__((aligned(2)));
+
+constexpr int kMaxRanges = 64;
+constexpr int kMinBlocks = 1;    // of a wave, where a row has several ranges
+constexpr int attn_queries(bool wide) { return wide ? 16 : 4; }        // of a workgroup
 
 // The four lanes of a query add the same four products, each in its own order, and have to come to the same sum: they give the digits of one
 // probability.  A product that is fused into the addition in one lane, and rounded in the others, gave digits of different numbers.
@@ -201,268 +215,472 @@ __device__ __forceinline__ float rounded_product(float a, float b) {
     return a * b;
 }
 
-template <int HD, int CT>
-__global__ __launch_bounds__(kBlock) void k_attn_q8(AttnArgs a) {
-    constexpr int KS = (HD + 63) / 64, H16 = HD / 16, OT = HD / 16, NQ = 4 * CT;
-    __shared__ float s_o[kWavesPerBlock][NQ][HD + 4];
-    __shared__ float s_m[kWavesPerBlock][NQ], s_l[kWavesPerBlock][NQ];
+// Eight steps (two words of four bytes) as halves: 0x6400 + u is 1024 + u, and u = step + 128.
+__device__ __forceinline__ f16x8 halves_of(int lo, int hi) {
+    u32x4v r;
+    const uint32_t w[2] = {(uint32_t)lo ^ 0x80808080u, (uint32_t)hi ^ 0x80808080u};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const f16x2 shift = {(_Float16)1152.f, (_Float16)1152.f};
+        r[2 * i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, w[i], 0x04010400u)) - shift);
+        r[2 * i + 1] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, w[i], 0x04030402u)) - shift);
+    }
+    return __builtin_bit_cast(f16x8, r);
+}
+// x as the sum of two halves.
+__device__ __forceinline__ void split_halves(const float* x, f16x8& hi, f16x8& lo) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        hi[e] = (_Float16)x[e];
+        lo[e] = (_Float16)(x[e] - (float)hi[e]);
+    }
+}
+__device__ __forceinline__ void publish_pair(float* p, float a, float b) {          // 8-byte aligned
+    publish_store(reinterpret_cast<double*>(p), __builtin_bit_cast(double, make_float2(a, b)));
+}
+__device__ __forceinline__ float2 published_pair(const float* p) {
+    return __builtin_bit_cast(float2, published_load(reinterpret_cast<const double*>(p)));
+}
+// A lane's value and that of the lane 16 (32) away, in either order: over the four lanes of a column without going through LDS.
+__device__ __forceinline__ uint2 with_16(uint32_t v) {
+    const auto p = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return make_uint2(p[0], p[1]);
+}
+__device__ __forceinline__ uint2 with_32(uint32_t v) {
+    const auto p = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return make_uint2(p[0], p[1]);
+}
+template <typename F>
+__device__ __forceinline__ uint32_t over_groups(uint32_t v, F&& f) {
+    const uint2 a = with_16(v);
+    const uint2 b = with_32(f(a.x, a.y));
+    return f(b.x, b.y);
+}
+__device__ __forceinline__ float max_groups(float v) {
+    return __builtin_bit_cast(float, over_groups(__builtin_bit_cast(uint32_t, v), [](uint32_t x, uint32_t y) {
+        return __builtin_bit_cast(uint32_t, fmaxf(__builtin_bit_cast(float, x), __builtin_bit_cast(float, y)));
+    }));
+}
+__device__ __forceinline__ float sum_groups(float v) {
+    return __builtin_bit_cast(float, over_groups(__builtin_bit_cast(uint32_t, v), [](uint32_t x, uint32_t y) {
+        return __builtin_bit_cast(uint32_t, __builtin_bit_cast(float, x) + __builtin_bit_cast(float, y));
+    }));
+}
+// Byte `b` of four words side by side (sel: attn_byte(b)).
+__device__ __forceinline__ uint32_t attn_byte(int b) { return (uint32_t)b | (uint32_t)(4 + b) << 8 | 0x0c0c0000u; }
+__device__ __forceinline__ uint32_t bytes_of(const uint32_t (&z)[4], uint32_t sel) {
+    return __builtin_amdgcn_perm(z[1], z[0], sel) | __builtin_amdgcn_perm(z[3], z[2], sel) << 16;
+}
+
+template <int HD, bool WIDE, int NW>
+__global__ __launch_bounds__(NW * 64) void k_attn_q8(AttnArgs a) {
+    constexpr int NQ = attn_queries(WIDE), KS = (HD + 63) / 64, H16 = HD / 16, OT = HD / 16, DG = WIDE ? 3 : 1;
+    constexpr int RD = !WIDE ? HD : (HD % 64 == 0 ? 64 : 32);          // dims that meet in LDS at a time
+    __shared__ __attribute__((aligned(16))) float s_o[NW][NQ][RD + 4];
+    __shared__ float s_m[NW][NQ], s_l[NW][NQ], s_M[NQ], s_L[NQ];
+    __shared__ int64_t s_out[NQ];                                     // where a query's output begins; -1: it has none
+    __shared__ float s_f[kMaxRanges][NQ];                             // shares of the waves, later of the ranges
     __shared__ int s_last;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int g = lane >> 4, c = lane & 15, dig = c & 3;
-    int w = blockIdx.x;
-    const int tile = w % a.tiles;
-    w /= a.tiles;
+    const int g = lane >> 4, c = lane & 15, dig = c & 3, my_q = WIDE ? c : c >> 2;
+    // Workgroup w goes to XCD w % 8: the tiles of a row and head, which read the same blocks, run back to back on one.  The first
+    // ranges come first: short rows have no others.
+    const int tile = (int)(blockIdx.x >> 3) % a.tiles;
+    int w = ((int)(blockIdx.x >> 3) / a.tiles) * 8 + (int)(blockIdx.x & 7);
     const int h = w % a.c.kv_heads;
     w /= a.c.kv_heads;
-    const int sp = w % a.S, row = w / a.S;
-    const int n = row_tokens(a.n_new, row, a.T);
-    const int queries = n * a.group, q0 = tile * NQ;
+    const int row = w % a.rows, sp = w / a.rows;
+    if (sp >= a.S) return;                                             // uniform: the grid is padded to whole rounds of XCDs
+    const int q0 = tile * NQ, most = a.T * a.group;
+    const int32_t* const table = a.c.table + (int64_t)row * a.c.max_blocks;
+
+    // What does not wait for anything else is requested first: this lane's query (past the last: the last, whose result is not stored
+    // twice), and the first blocks' pages where the range is not yet to be worked out.
+    const int qi = min(q0 + my_q, most - 1), tok = qi / a.group;
+    u32x4_e4 raw[KS][4];                                               // (bf16: two of the four)
+    {
+        const int64_t base = row * a.q_row + tok * a.q_tok + (int64_t)(h * a.group + qi % a.group) * HD;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+            const int64_t from = base + (HD % 64 == 0 ? (ks * 4 + g) * 16 : min((ks * 4 + g) * 16, HD - 16));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (!a.q_bf16) raw[ks][i] = *reinterpret_cast<const u32x4_e4*>(static_cast<const float*>(a.q) + from + 4 * i);
+                else if (i < 2) raw[ks][i] = u32x4_e4(*reinterpret_cast<const u32x4_e2*>(static_cast<const uint16_t*>(a.q) + from + 8 * i));
+            }
+        }
+    }
+    int page_l = -1;                                                   // of this wave's blocks, one a lane; -1: none
+    if (a.S == 1) page_l = table[min(wave + NW * lane, a.c.max_blocks - 1)];
+    __builtin_amdgcn_sched_barrier(0);
+
+    // ---- blocks of this workgroup's range
+    const int n = row_tokens(a.n_new, row, a.T), queries = n * a.group;
     if (q0 >= queries) return;                                         // uniform
     const int64_t cap = (int64_t)a.c.max_blocks * kCB;
     const int ctx = (int)min((int64_t)max(a.ctx_len[row], 0), cap);
     const int t_first = q0 / a.group, t_last = min(n - 1, (q0 + NQ - 1) / a.group);
-    const int NB = (int)((min((int64_t)ctx + t_last + 1, cap) + kCB - 1) / kCB);       // blocks that some query of the tile sees
-    const int ranges = min(a.S, max(1, NB / kMinRange));
+    const int NB = (int)((min((int64_t)ctx + t_last + 1, cap) + kCB - 1) / kCB);       // that some query of the tile sees
+    const int ranges = min(a.S, max(1, NB / (NW * kMinBlocks)));
     if (sp >= ranges) return;
     const int per = (NB + ranges - 1) / ranges, b_begin = min(sp * per, NB), b_end = min(b_begin + per, NB);
 
-    // ---- queries: digits of this lane's columns, and what a step of them is worth
-    i32x4 qd[CT][KS];
-    float worth[CT];
-    int limit[CT];                                                     // last position that the column's query sees
+    float m_run = -INFINITY, l_run = 0.f;
+    f32x4v o[OT];
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct) {
-        const int qi = min(q0 + ct * 4 + (c >> 2), queries - 1), t = qi / a.group, head = h * a.group + qi % a.group;
-        limit[ct] = ctx + t;
-        const int64_t base = row * a.q_row + t * a.q_tok + (int64_t)head * HD;
-        float x[KS][16];
-        uint32_t most = 0;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            const int dim = (ks * 4 + g) * 16;
-            if (HD % 64 == 0 || dim < HD) {
-                if (a.q_bf16) load_values<16, true>(a.q, base + dim, x[ks]);
-                else load_values<16, false>(a.q, base + dim, x[ks]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 16; ++e) x[ks][e] = 0.f;
-            }
-#pragma unroll
-            for (int e = 0; e < 16; ++e) most = max(most, magnitude(x[ks][e]));
-        }
-        most = max(most, (uint32_t)__shfl_xor((int)most, 16));
-        most = max(most, (uint32_t)__shfl_xor((int)most, 32));
-        const float m = __builtin_bit_cast(float, most);
-        const bool finite = most < kInfBits, some = finite && m >= kTiny;
-        const float inv = some ? 0x1p30f / m : 0.f;
-        worth[ct] = finite ? (some ? m * 0x1p-30f : 0.f) * a.scale2 * (float)(1 << (8 * dig)) : __builtin_nanf("");
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                int digits = 0;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int xi = some ? (int)rintf(x[ks][4 * i + e] * inv) : 0;
-                    const uint32_t z = ((uint32_t)xi + 0x00808080u) ^ 0x00808080u;
-                    digits |= (int)(((z >> (8 * dig)) & 255u) << (8 * e));
-                }
-                qd[ct][ks][i] = digits;
-            }
-        }
-    }
-
-    float m_run[CT], l_run[CT];
-    float o[CT][OT][4];
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct) {
-        m_run[ct] = -INFINITY;
-        l_run[ct] = 0.f;
-#pragma unroll
-        for (int ot = 0; ot < OT; ++ot)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[ct][ot][i] = 0.f;
-    }
-    const uint32_t sel = (uint32_t)dig | (uint32_t)(4 + dig) << 8 | 0x0c0c0000u;       // byte `dig` of two words side by side
+    for (int ot = 0; ot < OT; ++ot) o[ot] = f32x4v{0.f, 0.f, 0.f, 0.f};
+    const uint32_t sel = attn_byte(dig);
     const uint32_t flip = dig == 3 ? 0u : 0x80808080u;
-    const int32_t* const table = a.c.table + (int64_t)row * a.c.max_blocks;
 
-    for (int b = b_begin + wave; b < b_end; b += kWavesPerBlock) {
-        const int page = table[b];
-        if (page < 0 || page >= a.c.blocks) continue;                  // uniform
-        const int64_t ph = (int64_t)page * a.c.kv_heads + h;
-        const float ksc = a.c.kscale[ph], vsc = a.c.vscale[ph];
-        const int8_t* const kb = a.c.k + ph * kCB * HD;
-        const int8_t* const vb = a.c.v + ph * kCB * HD;
-        i32x4 kf[4][KS], vf[OT];
+    i32x4 kf[4][KS], vf[OT];                                           // the block that is on its way
+    // Requests are never predicated, so that their number in flight is known: where there is no further block (mask 0 instead of ~0) all lanes
+    // read the first 16 bytes of pieces of some block.
+    const uint32_t at_lane = (uint32_t)lane * 16u, at_ragged = (HD % 64 == 0 || (KS - 1) * 4 + g < H16) ? at_lane : (uint32_t)c * 16u;     // (past a ragged
+    auto request_k = [&](int page, uint32_t mask) {                                                          // end: for zeros of the query)
+        const int8_t* const kb = a.c.k + ((int64_t)page * a.c.kv_heads + h) * (kCB * HD);
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                const int piece = (ks * 4 + g < H16) ? ks * 4 + g : 0;
-                kf[t][ks] = *reinterpret_cast<const i32x4*>(kb + ((t * H16 + piece) * 16 + c) * 16);
+            for (int ks = 0; ks < KS; ++ks)
+                kf[t][ks] = *reinterpret_cast<const i32x4*>(kb + ((ks + 1 < KS ? at_lane : at_ragged) & mask) + t * H16 * 256 + ks * 1024);
+    };
+    auto request_v = [&](int page, uint32_t mask) {
+        const int8_t* const vb = a.c.v + ((int64_t)page * a.c.kv_heads + h) * (kCB * HD);
+#pragma unroll
+        for (int ot = 0; ot < OT; ++ot) vf[ot] = *reinterpret_cast<const i32x4*>(vb + (at_lane & mask) + ot * 1024);
+    };
+
+    // This wave's blocks are b_begin + wave + NW i; 64 of them are opened at a time, one a lane: pages, scales, and the request of the first.
+    float ks_l = 0.f, vs_l = 0.f;
+    unsigned long long there = 0;                                      // lanes whose blocks have not been requested
+    int left = 0, at = 0;                                              // blocks that have not been used; the lane of the requested one
+    auto open = [&](int i0) {
+        const int b_lane = b_begin + wave + NW * (i0 + lane);
+        if (a.S > 1 || i0 > 0) page_l = table[min(b_lane, a.c.max_blocks - 1)];
+        if (b_lane >= b_end || page_l >= a.c.blocks) page_l = -1;
+        ks_l = vs_l = 0.f;
+        if (page_l >= 0) {
+            ks_l = a.c.kscale[(int64_t)page_l * a.c.kv_heads + h];
+            vs_l = a.c.vscale[(int64_t)page_l * a.c.kv_heads + h];
+        }
+        there = __ballot(page_l >= 0);
+        left = __builtin_amdgcn_readfirstlane(__builtin_popcountll(there));
+        if (left == 0) return;
+        at = __builtin_ctzll(there);
+        there &= there - 1;
+        request_k(__builtin_amdgcn_readlane(page_l, at), ~0u);
+        request_v(__builtin_amdgcn_readlane(page_l, at), ~0u);
+    };
+    open(0);
+    __builtin_amdgcn_sched_barrier(0);
+
+    // ---- the query as it goes into the product
+    i32x4 qd[DG][KS];
+    float worth;                                                       // what a step of it, times one of the keys', adds to a score
+    {
+        float x[KS][16];
+        uint32_t top = 0;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const uint32_t half = raw[ks][e / 8][e / 2 % 4];
+                const uint32_t bits = !a.q_bf16 ? raw[ks][e / 4][e % 4] : (e & 1) ? half & 0xffff0000u : half << 16;
+                x[ks][e] = (HD % 64 == 0 || (ks * 4 + g) * 16 < HD) ? __builtin_bit_cast(float, bits) : 0.f;
+                top = max(top, magnitude(x[ks][e]));
             }
+        }
+        top = over_groups(top, [](uint32_t x, uint32_t y) { return max(x, y); });
+        // The largest becomes 2^30, or 0x7f7f78 (0x7f7f7f is the most that three digits hold); below 2^-100 all are zeros.
+        constexpr float kTop = WIDE ? 8355704.f : 0x1p30f;
+        const float m = __builtin_bit_cast(float, top);
+        const bool finite = top < kInfBits, some = finite && m >= kTiny;
+        const float by = some ? kTop / m : 0.f;
+        worth = finite ? (some ? m / kTop : 0.f) * a.scale2 : __builtin_nanf("");
+        if constexpr (!WIDE) worth *= (float)(1 << (8 * dig));
 #pragma unroll
-        for (int ot = 0; ot < OT; ++ot) vf[ot] = *reinterpret_cast<const i32x4*>(vb + ot * 1024 + lane * 16);
+        for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-            const float step = worth[ct] * ksc;
-            float s[16];
+            for (int i = 0; i < 4; ++i) {
+                uint32_t z[4];                                         // bytes: digits + 128, the lowest first; the fourth is one as it is
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                i32x4 acc = {0, 0, 0, 0};
+                for (int e = 0; e < 4; ++e) z[e] = (uint32_t)(int)rintf(x[ks][4 * i + e] * by) + 0x00808080u;
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(kf[t][ks], qd[ct][ks], acc, 0, 0, 0);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) s[4 * t + i] = rounded_product((float)acc[i], step);
+                for (int d = 0; d < DG; ++d) qd[d][ks][i] = (int)(bytes_of(z, WIDE ? attn_byte(d) : sel) ^ (WIDE ? 0x80808080u : flip));
             }
+    }
+
+    // One block, whose K and V are on their way; those of `next` are requested in between.
+    auto block = [&](int b, float ksc, float vsc, int next, uint32_t mask) {
+        float s[16], step = worth * ksc;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            i32x4 acc[DG];
+#pragma unroll
+            for (int d = 0; d < DG; ++d) acc[d] = i32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                for (int d = 0; d < DG; ++d) acc[d] = __builtin_amdgcn_mfma_i32_16x16x64_i8(kf[t][ks], qd[d][ks], acc[d], 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (WIDE) s[4 * t + i] = fmaf((float)acc[2][i], 65536.f, (float)(acc[1][i] * 256 + acc[0][i]));    // (a digit's sum: below 2^22)
+                else s[4 * t + i] = rounded_product((float)acc[0][i], step);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        request_k(next, mask);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (!WIDE) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] += dpp_f32<kDppXor1>(s[i]);
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] += dpp_f32<kDppXor2>(s[i]);
-            if (b * kCB + kCB - 1 > ctx + t_first) {                   // uniform: some query does not see all of the block
+            step = 1.f;
+        }
+        if (b * kCB + kCB - 1 > ctx + t_first) {                       // uniform: some query does not see all of the block
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (b * kCB + g * 16 + i > limit[ct]) s[i] = -INFINITY;
-            }
-            float mx = s[0];
+            for (int i = 0; i < 16; ++i) s[i] = b * kCB + g * 16 + i > ctx + tok ? -INFINITY : s[i] * step;
+            step = 1.f;
+        }
+        float mx = s[0];
 #pragma unroll
-            for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
-            mx = fmaxf(mx, __shfl_xor(mx, 16));
-            mx = fmaxf(mx, __shfl_xor(mx, 32));
-            const float m_new = fmaxf(m_run[ct], mx), base = (m_new > -INFINITY) ? m_new : 0.f;
-            const float alpha = __builtin_amdgcn_exp2f(m_run[ct] - base);
-            m_run[ct] = m_new;
-            uint32_t pz[16];
-            float sum = 0.f;
+        for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+        mx = max_groups(mx) * step;                                    // (no step is negative: the largest before is the largest after)
+        const float m_new = fmaxf(m_run, mx), base = (m_new > -INFINITY) ? m_new : 0.f;
+        if (__any(m_new > m_run)) {                                    // seldom after the first blocks
+            const float alpha = __builtin_amdgcn_exp2f(m_run - base);
+            m_run = m_new;
+            l_run *= alpha;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float p = __builtin_amdgcn_exp2f(s[i] - base);
-                sum += p;
-                pz[i] = (uint32_t)(int)fmaf(p, 0x1p30f, 0.5f) + 0x00808080u;
-            }
-            l_run[ct] = l_run[ct] * alpha + sum;
+            for (int ot = 0; ot < OT; ++ot) o[ot] *= alpha;
+        }
+        constexpr float kOneExp = WIDE ? 14.f : 0.f;
+        const float off = kOneExp - base;
+        float p[16], sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], step, off));
+            sum += p[i];
+        }
+        l_run += sum;
+        if constexpr (!WIDE) {
             i32x4 pd;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const uint32_t lo = __builtin_amdgcn_perm(pz[4 * i + 1], pz[4 * i], sel), hi = __builtin_amdgcn_perm(pz[4 * i + 3], pz[4 * i + 2], sel);
-                pd[i] = (int)((lo | hi << 16) ^ flip);
+                uint32_t z[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) z[e] = (uint32_t)(int)fmaf(p[4 * i + e], 0x1p30f, 0.5f) + 0x00808080u;
+                pd[i] = (int)(bytes_of(z, sel) ^ flip);
             }
 #pragma unroll
             for (int ot = 0; ot < OT; ++ot) {
                 const i32x4 acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(vf[ot], pd, i32x4{0, 0, 0, 0}, 0, 0, 0);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) o[ct][ot][i] = fmaf((float)acc[i], vsc, o[ct][ot][i] * alpha);
+                for (int i = 0; i < 4; ++i) o[ot][i] = fmaf((float)acc[i], vsc, o[ot][i]);
+            }
+        } else {
+            f16x8 ph[2], pl[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) split_halves(&p[8 * u], ph[u], pl[u]);
+            constexpr int kSide = OT < 4 ? OT : (OT % 4 == 0 ? 4 : 2);  // accumulators side by side: a chain of four products each
+#pragma unroll
+            for (int o0 = 0; o0 < OT; o0 += kSide) {
+                f32x4v acc[kSide];
+                f16x8 v[kSide];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+#pragma unroll
+                    for (int i = 0; i < kSide; ++i) v[i] = halves_of(vf[o0 + i][2 * u], vf[o0 + i][2 * u + 1]);
+#pragma unroll
+                    for (int i = 0; i < kSide; ++i) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[i], pl[u], u == 0 ? f32x4v{0.f, 0.f, 0.f, 0.f} : acc[i], 0, 0, 0);
+#pragma unroll
+                    for (int i = 0; i < kSide; ++i) acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v[i], ph[u], acc[i], 0, 0, 0);
+                }
+#pragma unroll
+                for (int i = 0; i < kSide; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[o0 + i][e] = fmaf(acc[i][e], vsc, o[o0 + i][e]);
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
+        request_v(next, mask);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+
+    for (int i0 = 0;;) {
+        for (; left > 0; --left) {
+            const int i = at;
+            const uint32_t mask = there != 0 ? ~0u : 0u;
+            if (there != 0) at = __builtin_ctzll(there);
+            there &= there - 1;                                        // (0 stays 0)
+            block(b_begin + wave + NW * (i0 + i), lane_f32(ks_l, i), lane_f32(vs_l, i), __builtin_amdgcn_readlane(page_l, at), mask);
+        }
+        i0 += 64;
+        if (b_begin + wave + NW * i0 >= b_end) break;
+        open(i0);
     }
 
-    // ---- digits, then waves, then ranges meet
-    const float place = (float)(1 << (8 * dig)) * 0x1p-30f;
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct) {
-        float l = l_run[ct];
-        l += __shfl_xor(l, 16);
-        l += __shfl_xor(l, 32);
-        const int q = ct * 4 + (c >> 2);
-        if (g == 0 && dig == 0) { s_m[wave][q] = m_run[ct]; s_l[wave][q] = l; }
-#pragma unroll
-        for (int ot = 0; ot < OT; ++ot)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float v = o[ct][ot][i] * place;
-                v += dpp_f32<kDppXor1>(v);
-                v += dpp_f32<kDppXor2>(v);
-                if (dig == i) s_o[wave][q][ot * 16 + g * 4 + i] = v;
-            }
+    // ---- waves meet
+    constexpr float kOne = WIDE ? 0x1p-14f : 0x1p-30f;                 // of the outputs; the sums of p are 2^14 times too large, or right
+    const float l_all = sum_groups(l_run) * (WIDE ? kOne : 1.f);
+    if (g == 0 && (WIDE || dig == 0)) {
+        s_m[wave][my_q] = m_run;
+        s_l[wave][my_q] = l_all;
     }
-    __syncthreads();
-    auto finish = [&](int q, int dim, float m, float l, float v) {      // of query q0 + q
-        const int qi = q0 + q;
-        if (qi >= queries) return;
-        const int t = qi / a.group, head = h * a.group + qi % a.group;
-        const float r = (l > 0.f || l != l) ? v / l : 0.f;             // (nothing seen: zeros)
-        const int64_t at = row * a.out_row + t * a.out_tok + (int64_t)head * HD + dim;
-        if (a.out_bf16) static_cast<uint16_t*>(a.out)[at] = f32_to_bf16_bits(r);
-        else static_cast<float*>(a.out)[at] = r;
-        if (dim == 0 && a.lse != nullptr)
-            a.lse[((int64_t)row * a.T + t) * (a.c.kv_heads * a.group) + head] =
+    lds_barrier();
+    auto share_of = [](float l) { return (l > 0.f || l != l) ? 1.f / l : 0.f; };      // (nothing seen: zeros)
+    auto store_lse = [&](int q, float m, float l) {
+        if (a.lse != nullptr && q < queries)
+            a.lse[((int64_t)row * a.T + q / a.group) * (a.c.kv_heads * a.group) + h * a.group + q % a.group] =
                 (l > 0.f || l != l) ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
     };
-    const int64_t unit = ((int64_t)row * a.c.kv_heads + h) * a.tiles + tile;
-    for (int e = tid; e < NQ * HD; e += kBlock) {
-        const int q = e / HD, dim = e % HD;
-        float m = -INFINITY, l = 0.f, v = 0.f;
+    if (tid < NQ) {
+        float m = s_m[0][tid], l = 0.f;
 #pragma unroll
-        for (int u = 0; u < kWavesPerBlock; ++u) m = fmaxf(m, s_m[u][q]);
+        for (int u = 1; u < NW; ++u) m = fmaxf(m, s_m[u][tid]);
         const float base = (m > -INFINITY) ? m : 0.f;
 #pragma unroll
-        for (int u = 0; u < kWavesPerBlock; ++u) {
-            const float f = __builtin_amdgcn_exp2f(s_m[u][q] - base);
-            l += s_l[u][q] * f;
-            v += s_o[u][q][dim] * f;
+        for (int u = 0; u < NW; ++u) {
+            const float f = __builtin_amdgcn_exp2f(s_m[u][tid] - base);
+            s_f[u][tid] = f;
+            l += s_l[u][tid] * f;
         }
-        if (ranges == 1) {
-            finish(q, dim, m, l, v);
-        } else {
-            publish_store(a.po + ((unit * a.S + sp) * NQ + q) * HD + dim, v);
-            if (dim == 0) {
-                publish_store(a.pml + ((unit * a.S + sp) * 2 + 0) * NQ + q, m);
-                publish_store(a.pml + ((unit * a.S + sp) * 2 + 1) * NQ + q, l);
+        s_M[tid] = m;
+        s_L[tid] = ranges == 1 ? share_of(l) : l;
+        const int q = q0 + tid, t = q / a.group, head = h * a.group + q % a.group;
+        s_out[tid] = q < queries ? row * a.out_row + t * a.out_tok + (int64_t)head * HD : -1;
+        if (ranges == 1) store_lse(q, m, l);
+    }
+    const int64_t unit = ((int64_t)row * a.c.kv_heads + h) * a.tiles + tile;
+    float* const my_po = a.po + (unit * a.S + sp) * (NQ * HD);
+    // Two dims of query q0 + q from their sums.
+    auto finish = [&](int q, int dim, float v0, float v1) {
+        const int64_t at = s_out[q];
+        if (at < 0) return;
+        const float f = s_L[q], r0 = f != 0.f ? v0 * f : 0.f, r1 = f != 0.f ? v1 * f : 0.f;
+        if (a.out_bf16) *reinterpret_cast<u32_e2*>(static_cast<uint16_t*>(a.out) + at + dim) = pack_bf16x4(r0, r1, 0.f, 0.f).x;
+        else *reinterpret_cast<f32x2_any*>(static_cast<float*>(a.out) + at + dim) = f32x2_any{r0, r1};
+    };
+#pragma unroll
+    for (int d0 = 0; d0 < HD; d0 += RD) {
+        if (d0 > 0) lds_barrier();                                   // the last ones have been read
+#pragma unroll
+        for (int ot = 0; ot < RD / 16; ++ot) {
+            f32x4v v = o[d0 / 16 + ot];
+            if constexpr (!WIDE) {
+                const float place = (float)(1 << (8 * dig)) * kOne;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    v[i] *= place;
+                    v[i] += dpp_f32<kDppXor1>(v[i]);
+                    v[i] += dpp_f32<kDppXor2>(v[i]);
+                }
+                if (dig == 0) *reinterpret_cast<f32x4v*>(&s_o[wave][my_q][ot * 16 + g * 4]) = v;
+            } else {
+                *reinterpret_cast<f32x4v*>(&s_o[wave][my_q][ot * 16 + g * 4]) = v * kOne;
             }
+        }
+        lds_barrier();
+        for (int e = tid; e < NQ * RD / 2; e += NW * 64) {
+            const int q = e / (RD / 2), dim = e % (RD / 2) * 2;
+            float v0 = 0.f, v1 = 0.f;
+#pragma unroll
+            for (int u = 0; u < NW; ++u) {
+                const float2 x = *reinterpret_cast<const float2*>(&s_o[u][q][dim]);
+                v0 += x.x * s_f[u][q];
+                v1 += x.y * s_f[u][q];
+            }
+            if (ranges == 1) finish(q, d0 + dim, v0, v1);
+            else publish_pair(my_po + q * HD + d0 + dim, v0, v1);
         }
     }
     if (ranges == 1) return;
+
+    // ---- ranges meet
+    float* const unit_ml = a.pml + unit * a.S * (2 * NQ);
+    if (tid < NQ) {
+        publish_store(unit_ml + sp * (2 * NQ) + tid, s_M[tid]);
+        publish_store(unit_ml + sp * (2 * NQ) + NQ + tid, s_L[tid]);
+    }
     publish_barrier();
     if (tid == 0) s_last = arrive(a.arrivals + unit, (uint32_t)ranges);
     __syncthreads();
     if (!s_last) return;
-    for (int e = tid; e < NQ * HD; e += kBlock) {
-        const int q = e / HD, dim = e % HD;
-        float m = -INFINITY, l = 0.f, v = 0.f;
-        for (int u = 0; u < ranges; ++u) {
-            const float mu = published_load(a.pml + ((unit * a.S + u) * 2 + 0) * NQ + q), lu = published_load(a.pml + ((unit * a.S + u) * 2 + 1) * NQ + q);
-            const float vu = published_load(a.po + ((unit * a.S + u) * NQ + q) * HD + dim);
-            const float mn = fmaxf(m, mu), base = (mn > -INFINITY) ? mn : 0.f;
-            const float fo = __builtin_amdgcn_exp2f(m - base), fn = __builtin_amdgcn_exp2f(mu - base);
-            l = l * fo + lu * fn;
-            v = v * fo + vu * fn;
-            m = mn;
+    // Everything that is read is requested at once: a wave has the maxima and sums of its queries, a lane for every range, a thread the
+    // sums of two dims, kFly ranges at a time.
+    constexpr int kFly = 16, kPairs = NQ * HD / 2;
+    const float* const unit_po = a.po + unit * a.S * (NQ * HD);
+    float2 x[kFly];
+    auto fetch = [&](int e, int u0) {
+#pragma unroll
+        for (int u = 0; u < kFly; ++u) x[u] = published_pair(unit_po + min(u0 + u, ranges - 1) * (NQ * HD) + 2 * e);
+    };
+    if (tid < kPairs) fetch(tid, 0);
+    static_assert(kMaxRanges == 64, "a lane each");
+    for (int q = wave; q < NQ; q += NW) {
+        const float* const ml = unit_ml + min(lane, ranges - 1) * (2 * NQ) + q;
+        const float mu = published_load(ml), lu = published_load(ml + NQ), m = wave_max(mu), base = (m > -INFINITY) ? m : 0.f;
+        const float f = lane < ranges ? __builtin_amdgcn_exp2f(mu - base) : 0.f, l = wave_sum(lane < ranges ? lu * f : 0.f);
+        s_f[lane][q] = f;
+        if (lane == 0) {
+            s_L[q] = share_of(l);
+            store_lse(q0 + q, m, l);
         }
-        finish(q, dim, m, l, v);
+    }
+    __syncthreads();
+    for (int e = tid; e < kPairs; e += NW * 64) {
+        const int q = e / (HD / 2), dim = e % (HD / 2) * 2;
+        float v0 = 0.f, v1 = 0.f;
+        for (int u0 = 0; u0 < ranges; u0 += kFly) {
+            if (e != tid || u0 > 0) fetch(e, u0);
+#pragma unroll
+            for (int u = 0; u < kFly; ++u) {                
+                const float f = s_f[min(u0 + u, ranges - 1)][q];
+                v0 += u0 + u < ranges ? x[u].x * f : 0.f;
+                v1 += u0 + u < ranges ? x[u].y * f : 0.f;
+            }
+        }
+        finish(q, dim, v0, v1);
     }
 }
 
-// Column tiles of a workgroup: as many as the queries fill, at most four (two where a head's 256 dims leave no registers).
-static int attn_ct(int hd, int queries) { return queries <= 4 ? 1 : (queries <= 8 || hd > 128) ? 2 : 4; }
-static int attn_tiles(int hd, int queries) { return (queries + 4 * attn_ct(hd, queries) - 1) / (4 * attn_ct(hd, queries)); }
-
-// Ranges: enough workgroups for four on every compute unit, none shorter than kMinRange blocks of a full table.
-static int attn_ranges(const tabed_cache_q8& c, int rows, int T, int q_heads) {
-    const long units = (long)rows * c.kv_heads * attn_tiles(c.head_dim, T * (q_heads / c.kv_heads));
-    const long want = (1024 + units - 1) / units, most = std::max(1, c.max_blocks / kMinRange);
-    return (int)std::min<long>({want, most, 128});
+// How a call is cut up.  Eight waves a workgroup and ranges where units (row, head, tile of queries) are few, so that ranges are
+// joined in LDS as far as possible.
+struct AttnPlan {
+    bool wide;
+    int nw, tiles, S;
+};
+static AttnPlan attn_plan(const tabed_cache_q8& c, int rows, int T, int q_heads) {
+    AttnPlan p;
+    const int queries = T * (q_heads / c.kv_heads);
+    p.wide = queries > 4;
+    p.tiles = (queries + attn_queries(p.wide) - 1) / attn_queries(p.wide);
+    const long units = (long)rows * c.kv_heads * p.tiles;
+    p.nw = units <= 256 && c.head_dim <= 128 ? 8 : 4;
+    const long want = (256 + units - 1) / units, most = std::max(1, c.max_blocks / (p.nw * kMinBlocks));
+    p.S = (int)std::min<long>({want, most, kMaxRanges});
+    return p;
 }
 
 AttnLayout attn_layout(const tabed_cache_q8& c, int rows, int T, int q_heads) {
     AttnLayout L;
-    const int queries = T * (q_heads / c.kv_heads), nq = 4 * attn_ct(c.head_dim, queries);
-    L.tiles = attn_tiles(c.head_dim, queries);
-    L.S = attn_ranges(c, rows, T, q_heads);
-    const size_t units = (size_t)rows * c.kv_heads * L.tiles;
+    const AttnPlan p = attn_plan(c, rows, T, q_heads);
+    const size_t nq = attn_queries(p.wide);
+    L.tiles = p.tiles;
+    L.S = p.S;
+    L.units = (size_t)rows * c.kv_heads * p.tiles;
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
-    size_t off = 0;
-    L.units = units;
-    off = up(off + sizeof(uint32_t) * units);
-    L.off_po = off;  off = up(off + (L.S > 1 ? sizeof(float) * units * L.S * nq * c.head_dim : 0));
-    L.off_pml = off; off = up(off + (L.S > 1 ? sizeof(float) * units * L.S * nq * 2 : 0));
+    size_t off = up(sizeof(uint32_t) * L.units);
+    L.off_po = off;  off = up(off + (L.S > 1 ? sizeof(float) * L.units * L.S * nq * c.head_dim : 0));
+    L.off_pml = off; off = up(off + (L.S > 1 ? sizeof(float) * L.units * L.S * nq * 2 : 0));
     L.total = off;
     return L;
 }
 
 int64_t attn_workgroups(const tabed_cache_q8& c, int rows, int T, int q_heads) {
-    const int64_t tiles = attn_tiles(c.head_dim, T * (q_heads / c.kv_heads));
-    return (int64_t)rows * c.kv_heads * tiles * attn_ranges(c, rows, T, q_heads);
+    const AttnPlan p = attn_plan(c, rows, T, q_heads);
+    return ((int64_t)rows * c.kv_heads * p.S + 7) / 8 * 8 * p.tiles;
 }
 
 __global__ void k_attn_init(uint32_t* arrivals, size_t n) {
@@ -476,31 +694,37 @@ hipError_t launch_attn_init(const tabed_cache_q8& c, int rows, int T, int q_head
     return hipGetLastError();
 }
 
+template <int HD>
+static void launch_attn(const ProfScope* prof, const AttnPlan& p, unsigned grid, const AttnArgs& a, hipStream_t s) {
+    if constexpr (HD <= 128) {
+        if (p.nw == 8) {
+            if (p.wide) launch(prof, k_attn_q8<HD, true, 8>, dim3(grid), dim3(512), 0, s, a);
+            else launch(prof, k_attn_q8<HD, false, 8>, dim3(grid), dim3(512), 0, s, a);
+            return;
+        }
+    }
+    if (p.wide) launch(prof, k_attn_q8<HD, true, 4>, dim3(grid), dim3(256), 0, s, a);
+    else launch(prof, k_attn_q8<HD, false, 4>, dim3(grid), dim3(256), 0, s, a);
+}
+
 hipError_t launch_attention_q8(const tabed_cache_q8& c, char* ws, int rows, int T, int q_heads, int q_dtype, const void* q, int64_t q_row,
                                int64_t q_tok, const int32_t* ctx_len, const int32_t* n_new, float scale, int out_dtype, void* out,
                                int64_t out_row, int64_t out_tok, float* lse, hipStream_t s) {
+    const AttnPlan p = attn_plan(c, rows, T, q_heads);
     const AttnLayout L = attn_layout(c, rows, T, q_heads);
-    const int group = q_heads / c.kv_heads, ct = attn_ct(c.head_dim, T * group);
-    const AttnArgs a{view_of(c), rows, T, group, L.tiles, L.S, q_dtype == 1, out_dtype == 1, q, q_row, q_tok, out, out_row, out_tok, lse, ctx_len,
-                     n_new, scale * 1.4426950408889634f, reinterpret_cast<uint32_t*>(ws), reinterpret_cast<float*>(ws + L.off_po),
+    const AttnArgs a{view_of(c), rows, T, q_heads / c.kv_heads, p.tiles, p.S, q_dtype == 1, out_dtype == 1, q, q_row, q_tok, out, out_row, out_tok,
+                     lse, ctx_len, n_new, scale * 1.4426950408889634f, reinterpret_cast<uint32_t*>(ws), reinterpret_cast<float*>(ws + L.off_po),
                      reinterpret_cast<float*>(ws + L.off_pml)};
-    const dim3 grid((unsigned)(L.units * L.S)), block(kBlock);
+    const unsigned grid = (unsigned)attn_workgroups(c, rows, T, q_heads);
     ProfScope prof(TABED_K_BODY, s);
-#define TABED_ATTN(HD_)                                                              \
-    case HD_:                                                                        \
-        if (ct == 1) launch(&prof, k_attn_q8<HD_, 1>, grid, block, 0, s, a);         \
-        else if (ct == 2) launch(&prof, k_attn_q8<HD_, 2>, grid, block, 0, s, a);    \
-        else if constexpr (HD_ <= 128) launch(&prof, k_attn_q8<HD_, 4>, grid, block, 0, s, a); \
-        break;
     switch (c.head_dim) {
-        TABED_ATTN(32)
-        TABED_ATTN(64)
-        TABED_ATTN(96)
-        TABED_ATTN(128)
-        TABED_ATTN(256)
+        case 32: launch_attn<32>(&prof, p, grid, a, s); break;
+        case 64: launch_attn<64>(&prof, p, grid, a, s); break;
+        case 96: launch_attn<96>(&prof, p, grid, a, s); break;
+        case 128: launch_attn<128>(&prof, p, grid, a, s); break;
+        case 256: launch_attn<256>(&prof, p, grid, a, s); break;
         default: return hipErrorInvalidValue;
     }
-#undef TABED_ATTN
     return hipGetLastError();
 }
 

@@ -86,13 +86,15 @@ def append(pool, scales, table, which, new, ctx, n_new, hd):
 def attention(pools, scales, table, q, ctx, n_new, scale, hd):
     """(out, lse, bound) in 64 bits; tokens from n_new on hold NaN.  pools, scales: {"k", "v"}; q [rows, T, q_heads, hd].
 
-    bound [rows, T, q_heads]: how far the kernel may be from `out`, by counting its roundings.  A score is four integers, exact, each
-    rounded to fp32, scaled by a product of four roundings, and added: at most 8 half steps of A = sum_d (|q_d| + max|q| 2^-7) |k_d| * scale
-    (a digit's share can exceed its value by the balanced digits' carry, 1/128 of the next one), and the fixed point itself half a
-    unit of 2^-30 max|q| a dimension, below that.  In base 2 its difference from the maximum is rounded once more, and exp2 is good to 2 half
-    steps: a probability is off by e = ln 2 * (10 A + |s - m|) half steps + 2, of which |s - m| matters only while exp2 of it does (|s - m| 2^-|s - m| < 1).
-    Sums of p and of p v run over at most the row's blocks, 16 terms and a chain each, plus joins (waves, ranges): (blocks + 16 + 64 + 140) half steps
-    of sum p |v|; p itself is kept to 2^-31 of the largest.  Scale of the value, division: 3 more."""
+    bound [rows, T, q_heads]: how far the kernel may be from `out`, by counting its roundings in half steps of fp32 (2^-24).  A score is at most
+    four integers, exact, that are rounded to fp32, scaled by a product of four roundings, and added: at most 10 half steps of A = sum_d (|q_d| +
+    max|q| 2^-7) |k_d| * scale (a digit's share can exceed its value by the balanced digits' carry, 1/128 of the next one).  The integers
+    themselves stand for q to half a unit of max|q| / 0x7f7f78: one half step of B = max|q| sum_d |k_d| * scale.  The exponent is
+    rounded once for the maximum (|m| + 14) and once for the result (|s - m| + 14, which matters only while exp2 of it does: |s - m| 2^-|s - m| < 1);
+    exp2 is good to 2.  A probability is kept to 2^-22 (two halves of 11 bits; 4) and to 2^-31 of the largest one, so
+    it is off by e = ln 2 * (10 A + B + |m| + 29) + 6, A, B, m in base 2.
+    Sums of p and of p v run over at most the row's blocks, 64 terms and a chain each, plus joins (waves, ranges): blocks + 220 half steps
+    of sum p |v|.  Scale of the value, division: 3 more."""
     rows, T, qh, _ = q.shape
     kvh = scales["k"].shape[1]
     group, u = qh // kvh, 2.0 ** -24
@@ -120,7 +122,8 @@ def attention(pools, scales, table, q, ctx, n_new, scale, hd):
                     p = np.exp(s - m)
                     out[r, t, i], lse[r, t, i] = p @ v[seen] / p.sum(), m + math.log(p.sum())
                     A = ((np.abs(qq) + np.abs(qq).max() / 128) @ np.abs(k[seen]).T).max() * scale / math.log(2)
-                    e = math.log(2) * (10 * A + 1) + 2
+                    B = np.abs(qq).max() * np.abs(k[seen]).sum(1).max() * scale / math.log(2)
+                    e = math.log(2) * (10 * A + B + abs(m) / math.log(2) + 29) + 6
                     w = p @ np.abs(v[seen]) / p.sum()
                     lost = seen.sum() * 2.0 ** -31 / p.sum() * np.abs(v[seen]).max(0)
                     bound[r, t, i] = ((2 * e + 2 * (len(held) + 220) + 3) * u * w + lost).max()
