@@ -31,9 +31,8 @@ __device__ __forceinline__ int row_tokens(const int32_t* n_new, int row, int T) 
 }
 
 // ---------------------------------------------------------------- append
-// One workgroup: the keys, or the values, of one head in one block of one row's new tokens.  Reads the new tokens once;
-// tokens that a begun block keeps are read only where its scale grows (they are rounded again then), values also where a group
-// of 16 tokens is stored whole.  Latency bounds a decode step (positions -> page -> scale), memory a prompt.
+// The keys, or the values, of one head in one block of a row's new tokens are one task: largest magnitude, scale, steps.  Tokens that a
+// begun block keeps are read only where its scale grows; they are rounded again then.
 struct AppendArgs {
     CacheView c;
     int rows, T, nb;
@@ -44,41 +43,151 @@ struct AppendArgs {
     const int32_t* n_new;
 };
 
-template <bool BF16>
-__global__ __launch_bounds__(kBlock) void k_cache_append(AppendArgs a) {
-    __shared__ uint32_t s_most[kWavesPerBlock];
-    extern __shared__ __attribute__((aligned(16))) unsigned char s_t[];       // values: [hd][64 + 4] new tokens' steps
-    constexpr int kRow = kCB + 4;
-    int w = blockIdx.x;
-    const bool values = w & 1;
+struct AppendTask {
+    bool values;
+    int off, count;          // the first `off` tokens of the block are kept, `count` new ones go behind them
+    int64_t from;            // the first new token's, in k or v (elements)
+    int64_t ph;              // block and head: scale
+};
+// Task number w; false: there is nothing to do.
+__device__ __forceinline__ bool append_task(const AppendArgs& a, int w, AppendTask& t) {
+    t.values = w & 1;
     w >>= 1;
     const int h = w % a.c.kv_heads;
     w /= a.c.kv_heads;
     const int j = w % a.nb, row = w / a.nb;
-    const int tid = threadIdx.x, hd = a.c.hd, chunks = hd / 16;
+    if (row >= a.rows) return false;
     const int n = row_tokens(a.n_new, row, a.T), ctx = max(a.ctx_len[row], 0);
-    const int64_t slot = (int64_t)(ctx / kCB) + j;
-    if (slot >= a.c.max_blocks) return;
-    const int b0 = (int)slot * kCB, off = max(ctx - b0, 0);                  // the first `off` tokens are kept
-    const int t0 = b0 + off - ctx, count = min(kCB - off, n - t0);            // new tokens t0 .. t0 + count - 1 go behind them
-    if (count <= 0) return;
+    const int64_t slot = (int64_t)(ctx / kCB) + j, first = slot * kCB;         // (64 bits: a position may be near 2^31)
+    if (slot >= a.c.max_blocks) return false;
+    t.off = (int)max(ctx - first, (int64_t)0);
+    const int64_t t0 = first + t.off - ctx;
+    if (t0 >= n) return false;
+    t.count = (int)min((int64_t)(kCB - t.off), n - t0);
     const int page = a.c.table[(int64_t)row * a.c.max_blocks + slot];
-    if (page < 0 || page >= a.c.blocks) return;
-    const int64_t ph = (int64_t)page * a.c.kv_heads + h;
-    int8_t* const block = (values ? a.c.v : a.c.k) + ph * kCB * hd;
-    float* const scales = values ? a.c.vscale : a.c.kscale;
-    const float before = off > 0 ? scales[ph] : 0.f;
-    const void* const src = values ? a.v : a.k;
-    const int64_t base = row * a.row_stride + (int64_t)t0 * a.tok_stride + (int64_t)h * hd;
+    if (page < 0 || page >= a.c.blocks) return false;
+    t.ph = (int64_t)page * a.c.kv_heads + h;
+    t.from = row * a.row_stride + t0 * a.tok_stride + (int64_t)h * a.c.hd;
+    return true;
+}
+__device__ __forceinline__ float grown_scale(float before, uint32_t most) {
+    const float fresh = scale_of(most);
+    return (before != before || fresh != fresh) ? __builtin_nanf("") : fmaxf(before, fresh);
+}
+// A kept token's step, in steps of the new scale.
+__device__ __forceinline__ int step_again(int q, float before, float scale) { return scale > 0.f ? to_step((float)q * before / scale) : 0; }
+__device__ __forceinline__ uint32_t word_again(uint32_t w, int keep /* of its four steps, the first ones */, float before, float scale) {
+    int s[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int q = (int8_t)(w >> (8 * e));
+        s[e] = e < keep ? step_again(q, before, scale) : q;
+    }
+    return pack_i8(s[0], s[1], s[2], s[3]);
+}
+// round(x / scale), the division as fp32 rounds it.  A product with the reciprocal is off by less than 1.6e-5 steps: only where
+// one comes that near to the middle between two steps is the division made (a dozen instructions each: half of a prompt's time).
+__device__ __forceinline__ void steps_of(const float (&x)[16], float scale, float inv, int (&s)[16]) {
+    float far = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        const float t = x[e] * inv, r = rintf(t);
+        far = fmaxf(far, fabsf(t - r));
+        s[e] = (int)r;
+    }
+    if (__any(far > 0.5f - 2e-5f)) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = (int)rintf(x[e] / scale);
+    }
+}
+__device__ __forceinline__ u32x4_e4 pack_steps(const int (&s)[16]) {
+    return u32x4_e4{pack_i8(s[0], s[1], s[2], s[3]), pack_i8(s[4], s[5], s[6], s[7]), pack_i8(s[8], s[9], s[10], s[11]), pack_i8(s[12], s[13], s[14], s[15])};
+}
+__device__ __forceinline__ int key_piece(int at, int c, int chunks) { return ((at / 4 % 4) * chunks + c) * 16 + at / 16 * 4 + at % 4; }      // 16 dims of a token
+__device__ __forceinline__ int value_piece(int g, int dim) { return (dim / 16 * 4 + g) * 16 + dim % 16; }                                     // 16 tokens of a dim
 
-    constexpr int kPer = 4;                                                   // pieces of 16 dims a thread holds: 4 * 256 >= 64 * 256 / 16
+// Up to kFew new tokens a row: a wave a task, a lane for every 64th dim, a byte stored for each value.  Latency bounds it: positions
+// -> page -> scale.
+constexpr int kFew = 4;
+template <bool BF16, int hd>
+__global__ __launch_bounds__(kBlock) void k_cache_append_few(AppendArgs a) {
+    constexpr int chunks = hd / 16, kDims = (hd + 63) / 64;           // kDims: of a lane
+    AppendTask t;
+    if (!append_task(a, blockIdx.x * kWavesPerBlock + (threadIdx.x >> 6), t)) return;      // uniform for the wave; no barriers
+    const int lane = threadIdx.x & 63;
+    int8_t* const block = (t.values ? a.c.v : a.c.k) + t.ph * kCB * hd;
+    float* const scale_at = (t.values ? a.c.vscale : a.c.kscale) + t.ph;
+    const float before = t.off > 0 ? *scale_at : 0.f;
+    const void* const src = t.values ? a.v : a.k;
+    float x[kFew][kDims];
+    uint32_t most = 0;
+#pragma unroll
+    for (int n = 0; n < kFew; ++n)
+#pragma unroll
+        for (int i = 0; i < kDims; ++i) {
+            const int dim = i * 64 + lane;
+            if (n < t.count && dim < hd) {
+                x[n][i] = load_value<BF16>(src, t.from + n * a.tok_stride + dim);
+                most = max(most, magnitude(x[n][i]));
+            }
+        }
+    const float scale = grown_scale(before, wave_max_u32(most));
+    const bool live = scale > 0.f;
+    if (t.off > 0 && !(scale == before)) {                             // pieces with kept tokens, a lane each
+        for (int p = lane; p < (t.values ? (t.off + 15) / 16 * hd : t.off * chunks); p += 64) {
+            const int piece = t.values ? value_piece(p / hd, p % hd) : key_piece(p / chunks, p % chunks, chunks);
+            const int keep = t.values ? t.off - p / hd * 16 : 16;      // of its 16 steps
+            u32x4_e4* const at = reinterpret_cast<u32x4_e4*>(block) + piece;
+            u32x4_e4 w = *at;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = word_again(w[i], keep - 4 * i, before, scale);
+            *at = w;
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");              // the new tokens' bytes, which share pieces with them, come after
+    }
+#pragma unroll
+    for (int n = 0; n < kFew; ++n)
+#pragma unroll
+        for (int i = 0; i < kDims; ++i) {
+            const int dim = i * 64 + lane, at = t.off + n;
+            if (n < t.count && dim < hd)
+                block[t.values ? value_piece(at / 16, dim) * 16 + at % 16 : key_piece(at, dim / 16, chunks) * 16 + dim % 16] =
+                    (int8_t)(live ? (int)rintf(x[n][i] / scale) : 0);
+        }
+    if (lane == 0) *scale_at = scale;
+}
+
+// Four words of four bytes, transposed.
+__device__ __forceinline__ void transpose_bytes(const uint32_t (&r)[4], uint32_t (&out)[4]) {
+    const uint32_t a = __builtin_amdgcn_perm(r[1], r[0], 0x05010400u), b = __builtin_amdgcn_perm(r[1], r[0], 0x07030602u);
+    const uint32_t c = __builtin_amdgcn_perm(r[3], r[2], 0x05010400u), d = __builtin_amdgcn_perm(r[3], r[2], 0x07030602u);
+    out[0] = __builtin_amdgcn_perm(c, a, 0x05040100u);
+    out[1] = __builtin_amdgcn_perm(c, a, 0x07060302u);
+    out[2] = __builtin_amdgcn_perm(d, b, 0x05040100u);
+    out[3] = __builtin_amdgcn_perm(d, b, 0x07060302u);
+}
+
+// More: a workgroup a task, a thread for pieces of 16 dims of a token.  Keys are stored as such a piece, values go through LDS, from
+// where a thread takes 16 tokens of four dims and transposes them.  Memory bounds a prompt.
+template <bool BF16, int hd>
+__global__ __launch_bounds__(kBlock) void k_cache_append(AppendArgs a) {
+    constexpr int chunks = hd / 16, row_bytes = hd + 16, kPer = (kCB * chunks + kBlock - 1) / kBlock;      // kPer: pieces of a thread
+    __shared__ uint32_t s_most[kWavesPerBlock];
+    __shared__ __attribute__((aligned(16))) unsigned char s_t[kCB * row_bytes];       // values: [token][hd] steps
+    AppendTask t;
+    if (!append_task(a, blockIdx.x, t)) return;                        // uniform
+    const int tid = threadIdx.x;
+    int8_t* const block = (t.values ? a.c.v : a.c.k) + t.ph * kCB * hd;
+    float* const scale_at = (t.values ? a.c.vscale : a.c.kscale) + t.ph;
+    const float before = t.off > 0 ? *scale_at : 0.f;
+    const void* const src = t.values ? a.v : a.k;
     float x[kPer][16];
     uint32_t most = 0;
 #pragma unroll
     for (int p = 0; p < kPer; ++p) {
-        const int idx = p * kBlock + tid, tok = idx / chunks, c = idx % chunks;
-        if (tok < count) {
-            load_values<16, BF16>(src, base + (int64_t)tok * a.tok_stride + c * 16, x[p]);
+        const int idx = p * kBlock + tid;
+        if (idx < t.count * chunks) {
+            load_values<16, BF16>(src, t.from + (int64_t)(idx / chunks) * a.tok_stride + idx % chunks * 16, x[p]);
 #pragma unroll
             for (int e = 0; e < 16; ++e) most = max(most, magnitude(x[p][e]));
         }
@@ -87,62 +196,67 @@ __global__ __launch_bounds__(kBlock) void k_cache_append(AppendArgs a) {
     if ((tid & 63) == 0) s_most[tid >> 6] = most;
     __syncthreads();
     most = max(max(s_most[0], s_most[1]), max(s_most[2], s_most[3]));
-    const float fresh = scale_of(most);
-    const float scale = (before != before || fresh != fresh) ? __builtin_nanf("") : fmaxf(before, fresh);
-    const bool live = scale > 0.f, grown = off > 0 && !(scale == before);      // uniform
-    if (tid == 0) scales[ph] = scale;
-    auto again = [&](int q) { return live ? to_step((float)q * before / scale) : 0; };       // a kept token's step, in steps of the new scale
-
+    const float scale = grown_scale(before, most), inv = scale > 0.f ? 1.f / scale : 0.f;
+    const bool grown = t.off > 0 && !(scale == before);                // uniform
+    if (tid == 0) *scale_at = scale;
 #pragma unroll
     for (int p = 0; p < kPer; ++p) {
-        const int idx = p * kBlock + tid, tok = idx / chunks, c = idx % chunks;
-        if (tok < count) {
+        const int idx = p * kBlock + tid, at = t.off + idx / chunks, c = idx % chunks;
+        if (idx < t.count * chunks) {
             int s[16];
-#pragma unroll
-            for (int e = 0; e < 16; ++e) s[e] = live ? to_step(x[p][e] / scale) : 0;
-            const int at = off + tok;
-            if (!values) {
-                const u32x4_e4 out = {pack_i8(s[0], s[1], s[2], s[3]), pack_i8(s[4], s[5], s[6], s[7]), pack_i8(s[8], s[9], s[10], s[11]),
-                                      pack_i8(s[12], s[13], s[14], s[15])};
-                *reinterpret_cast<u32x4_e4*>(block + (((at / 4 % 4) * chunks + c) * 16 + at / 16 * 4 + at % 4) * 16) = out;
+            if (scale > 0.f) {
+                steps_of(x[p], scale, inv, s);
             } else {
 #pragma unroll
-                for (int e = 0; e < 16; ++e) s_t[(c * 16 + e) * kRow + at] = (unsigned char)s[e];
+                for (int e = 0; e < 16; ++e) s[e] = 0;
             }
+            if (t.values) *reinterpret_cast<u32x4_e4*>(s_t + at * row_bytes + c * 16) = pack_steps(s);
+            else reinterpret_cast<u32x4_e4*>(block)[key_piece(at, c, chunks)] = pack_steps(s);
         }
     }
-    if (!values) {
+    if (!t.values) {
         if (grown)
-            for (int idx = tid; idx < off * chunks; idx += kBlock) {
-                const int at = idx / chunks, c = idx % chunks;
-                u32x4_e4* const p = reinterpret_cast<u32x4_e4*>(block + (((at / 4 % 4) * chunks + c) * 16 + at / 16 * 4 + at % 4) * 16);
-                u32x4_e4 old = *p;
+            for (int idx = tid; idx < t.off * chunks; idx += kBlock) {
+                u32x4_e4* const at = reinterpret_cast<u32x4_e4*>(block) + key_piece(idx / chunks, idx % chunks, chunks);
+                u32x4_e4 w = *at;
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    old[i] = pack_i8(again((int8_t)old[i]), again((int8_t)(old[i] >> 8)), again((int8_t)(old[i] >> 16)), again((int8_t)(old[i] >> 24)));
-                *p = old;
+                for (int i = 0; i < 4; ++i) w[i] = word_again(w[i], 4, before, scale);
+                *at = w;
             }
         return;
     }
     __syncthreads();
-    const int g0 = grown ? 0 : off / 16, g1 = (off + count - 1) / 16;          // groups of 16 tokens that change
-    for (int idx = tid; idx < (g1 - g0 + 1) * hd; idx += kBlock) {
-        const int g = g0 + idx / hd, dim = idx % hd;
-        u32x4_e4* const p = reinterpret_cast<u32x4_e4*>(block + ((dim / 16 * 4 + g) * 16 + dim % 16) * 16);
-        u32x4_e4 old = {0u, 0u, 0u, 0u};
-        if (g * 16 < off || (g + 1) * 16 > off + count) old = *p;               // some of its tokens stay
-        const unsigned char* const now = s_t + dim * kRow;
+    const int end = t.off + t.count, g0 = grown ? 0 : t.off / 16, g1 = (end + 15) / 16;       // groups of 16 tokens that change
+    for (int idx = tid; idx < (g1 - g0) * (hd / 4); idx += kBlock) {
+        const int g = g0 + idx / (hd / 4), dim0 = idx % (hd / 4) * 4, keep = t.off - g * 16;   // of its tokens, the first `keep` are kept
+        u32x4_e4 w[4];                                                 // [dim]: words of four tokens
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            int s[4];
+            uint32_t r[4], c[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int at = g * 16 + 4 * i + e, q = (int8_t)(old[i] >> (8 * e));
-                s[e] = at < off ? (grown ? again(q) : q) : at < off + count ? (int8_t)now[at] : q;
-            }
-            old[i] = pack_i8(s[0], s[1], s[2], s[3]);
+            for (int e = 0; e < 4; ++e) r[e] = *reinterpret_cast<const uint32_t*>(s_t + (g * 16 + 4 * i + e) * row_bytes + dim0);      // (not new: replaced below)
+            transpose_bytes(r, c);
+#pragma unroll
+            for (int d = 0; d < 4; ++d) w[d][i] = c[d];
         }
-        *p = old;
+        const bool some_stay = keep > 0 || (g + 1) * 16 > end;
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+            u32x4_e4* const at = reinterpret_cast<u32x4_e4*>(block) + value_piece(g, dim0 + d);
+            if (some_stay) {
+                const u32x4_e4 old = *at;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t kept = grown ? word_again(old[i], keep - 4 * i, before, scale) : old[i];
+                    uint32_t mask = 0;                                 // bytes of tokens that are not new
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (4 * i + e < keep || g * 16 + 4 * i + e >= end) mask |= 255u << (8 * e);
+                    w[d][i] = (w[d][i] & ~mask) | (kept & mask);
+                }
+            }
+            *at = w[d];
+        }
     }
 }
 
@@ -150,14 +264,29 @@ static int append_blocks(int T) { return (T + kCB - 2) / kCB + 1; }
 
 int64_t append_workgroups(const tabed_cache_q8& c, int rows, int T) { return 2ll * c.kv_heads * rows * append_blocks(T); }
 
+template <int hd>
+static void launch_append(const ProfScope* prof, int kv_dtype, unsigned tasks, const AppendArgs& a, hipStream_t s) {
+    const bool few = a.T <= kFew;
+    const dim3 grid(few ? (tasks + kWavesPerBlock - 1) / kWavesPerBlock : tasks);
+    if (few && kv_dtype == 1) launch(prof, k_cache_append_few<true, hd>, grid, dim3(kBlock), 0, s, a);
+    else if (few) launch(prof, k_cache_append_few<false, hd>, grid, dim3(kBlock), 0, s, a);
+    else if (kv_dtype == 1) launch(prof, k_cache_append<true, hd>, grid, dim3(kBlock), 0, s, a);
+    else launch(prof, k_cache_append<false, hd>, grid, dim3(kBlock), 0, s, a);
+}
+
 hipError_t launch_cache_append(const tabed_cache_q8& c, int rows, int T, int kv_dtype, const void* k, const void* v, int64_t row_stride,
                                int64_t tok_stride, const int32_t* ctx_len, const int32_t* n_new, hipStream_t s) {
     const AppendArgs a{view_of(c), rows, T, append_blocks(T), k, v, row_stride, tok_stride, ctx_len, n_new};
-    const dim3 grid((unsigned)append_workgroups(c, rows, T));
-    const size_t lds = (size_t)c.head_dim * (kCB + 4);
     ProfScope prof(TABED_K_BODY, s);
-    if (kv_dtype == 1) launch(&prof, k_cache_append<true>, grid, dim3(kBlock), lds, s, a);
-    else launch(&prof, k_cache_append<false>, grid, dim3(kBlock), lds, s, a);
+    const unsigned tasks = (unsigned)append_workgroups(c, rows, T);
+    switch (c.head_dim) {
+        case 32: launch_append<32>(&prof, kv_dtype, tasks, a, s); break;
+        case 64: launch_append<64>(&prof, kv_dtype, tasks, a, s); break;
+        case 96: launch_append<96>(&prof, kv_dtype, tasks, a, s); break;
+        case 128: launch_append<128>(&prof, kv_dtype, tasks, a, s); break;
+        case 256: launch_append<256>(&prof, kv_dtype, tasks, a, s); break;
+        default: return hipErrorInvalidValue;
+    }
     return hipGetLastError();
 }
 
