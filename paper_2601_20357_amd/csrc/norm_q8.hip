@@ -28,21 +28,32 @@ typedef uint32_t u32x2_e1 __attribute__((ext_vector_type(2), aligned(1)));
 
 enum { kF32 = 0, kB16 = 1, kNone = 2 };
 
-constexpr int kNormPieces = 4;     // pieces of 8 values a thread keeps
-
-template <int TPR /* threads of a row */, int X, int D>
+// TPR threads of a row, P pieces of 8 values each, as few as hold the row: 8192 rows of 4096 in bf16 with their deltas, 235 MB, took 58 us
+// with room for four pieces, 46 with the two that there are, which is what a copy of as many bytes takes.
+template <int TPR, int P, int X, int D>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_q8(NormArgs a) {
     constexpr int kWaves = TPR / 64;
     __shared__ float s_sum[kWaves];
     __shared__ uint32_t s_most[kWaves];
-    const int t = threadIdx.x % TPR;
-    const int row = (TPR == 64) ? blockIdx.x * (int)(blockDim.x / 64) + (int)(threadIdx.x / 64) : (int)blockIdx.x;
-    if (row >= a.rows) return;                               // uniform for a wave, and for a workgroup that meets at a barrier
-    const int d = a.d;
-    float v[kNormPieces][8];
-    float ss = 0.f;
+    const int t = threadIdx.x % TPR, d = a.d;
+    const int64_t row = (TPR == 64) ? (int64_t)blockIdx.x * (blockDim.x / 64) + threadIdx.x / 64 : (int64_t)blockIdx.x;
+    if (row >= a.rows) return;                                        // uniform for a wave, and for a workgroup that meets at a barrier
+    float g[P][8];
+    if (a.g != nullptr) {
 #pragma unroll
-    for (int p = 0; p < kNormPieces; ++p) {
+        for (int p = 0; p < P; ++p) {
+            const int at = (p * TPR + t) * 8;
+            if (at + 8 <= d) {
+                load_values<8, false>(a.g, at, g[p]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) g[p][e] = (at + e < d) ? a.g[at + e] : 0.f;
+            }
+        }
+    }
+    float v[P][8], ss = 0.f;
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
         const int at = (p * TPR + t) * 8;
         if (at + 8 <= d) {
             load_values<8, X == kB16>(a.x, row * a.ldx + at, v[p]);
@@ -66,7 +77,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_q8(NormArgs a) {
     if constexpr (D != kNone) {
         if (a.sum != nullptr) {
 #pragma unroll
-            for (int p = 0; p < kNormPieces; ++p) {
+            for (int p = 0; p < P; ++p) {
                 const int at = (p * TPR + t) * 8;
                 if (at + 8 <= d) {
                     if constexpr (X == kB16) {
@@ -90,7 +101,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_q8(NormArgs a) {
     }
     if (a.g != nullptr) {
 #pragma unroll
-        for (int p = 0; p < kNormPieces; ++p)
+        for (int p = 0; p < P; ++p)
 #pragma unroll
             for (int e = 0; e < 8; ++e) ss = fmaf(v[p][e], v[p][e], ss);
         ss = wave_sum(ss);
@@ -103,23 +114,13 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_q8(NormArgs a) {
         }
         const float rms = 1.f / sqrtf(ss / (float)d + a.eps);
 #pragma unroll
-        for (int p = 0; p < kNormPieces; ++p) {
-            const int at = (p * TPR + t) * 8;
-            if (at + 8 <= d) {
-                float g[8];
-                load_values<8, false>(a.g, at, g);
+        for (int p = 0; p < P; ++p)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[p][e] = v[p][e] * rms * g[e];
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (at + e < d) v[p][e] = v[p][e] * rms * a.g[at + e];
-            }
-        }
+            for (int e = 0; e < 8; ++e) v[p][e] = v[p][e] * rms * g[p][e];
     }
-    uint32_t most = (ss < INFINITY) ? 0u : kInfBits;          // (squares past fp32: the row is not finite either)
+    uint32_t most = (ss < INFINITY) ? 0u : kInfBits;               // (squares past fp32: the row is not finite either)
 #pragma unroll
-    for (int p = 0; p < kNormPieces; ++p)
+    for (int p = 0; p < P; ++p)
 #pragma unroll
         for (int e = 0; e < 8; ++e) most = max(most, magnitude(v[p][e]));
     most = wave_max_u32(most);
@@ -132,7 +133,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_q8(NormArgs a) {
     const float scale = scale_of(most);
     const float inv = (scale > 0.f) ? 127.f / __builtin_bit_cast(float, most) : 0.f;
 #pragma unroll
-    for (int p = 0; p < kNormPieces; ++p) {
+    for (int p = 0; p < P; ++p) {
         const int at = (p * TPR + t) * 8;
         int s[8];
 #pragma unroll
@@ -152,16 +153,19 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_q8(NormArgs a) {
     }
 }
 
-template <int TPR>
-static void launch_norm_t(const ProfScope* prof, int xt, int dt, dim3 grid, dim3 block, const NormArgs& a, hipStream_t s) {
+template <int TPR, int P>
+static void launch_norm_t(const ProfScope* prof, int xt, int dt, const NormArgs& a, hipStream_t s) {
+    const int per = (TPR == 64 && a.rows >= 1024) ? 4 : 1;             // rows of a workgroup, a wave each
+    const dim3 grid((a.rows + per - 1) / per), block(TPR * per);
+    auto go = [&](auto kernel) { launch(prof, kernel, grid, block, 0, s, a); };
     if (xt == kF32) {
-        if (dt == kF32) launch(prof, k_norm_q8<TPR, kF32, kF32>, grid, block, 0, s, a);
-        else if (dt == kB16) launch(prof, k_norm_q8<TPR, kF32, kB16>, grid, block, 0, s, a);
-        else launch(prof, k_norm_q8<TPR, kF32, kNone>, grid, block, 0, s, a);
+        if (dt == kF32) go(k_norm_q8<TPR, P, kF32, kF32>);
+        else if (dt == kB16) go(k_norm_q8<TPR, P, kF32, kB16>);
+        else go(k_norm_q8<TPR, P, kF32, kNone>);
     } else {
-        if (dt == kF32) launch(prof, k_norm_q8<TPR, kB16, kF32>, grid, block, 0, s, a);
-        else if (dt == kB16) launch(prof, k_norm_q8<TPR, kB16, kB16>, grid, block, 0, s, a);
-        else launch(prof, k_norm_q8<TPR, kB16, kNone>, grid, block, 0, s, a);
+        if (dt == kF32) go(k_norm_q8<TPR, P, kB16, kF32>);
+        else if (dt == kB16) go(k_norm_q8<TPR, P, kB16, kB16>);
+        else go(k_norm_q8<TPR, P, kB16, kNone>);
     }
 }
 
@@ -170,14 +174,13 @@ hipError_t launch_norm_q8(int rows, int d, int x_dtype, const void* x, int64_t l
     const NormArgs a{rows, d, x, ldx, delta, ldd, sum, lds, g, eps, q, ldq, scale, advance};
     const int dt = delta == nullptr ? kNone : delta_dtype;
     ProfScope prof(TABED_K_BODY, s);
-    if (d <= 64 * 8 * kNormPieces) {
-        const int per = rows >= 1024 ? 4 : 1;                  // rows of a workgroup, a wave each
-        launch_norm_t<64>(&prof, x_dtype, dt, dim3((rows + per - 1) / per), dim3(64 * per), a, s);
-    } else if (d <= 256 * 8 * kNormPieces) {
-        launch_norm_t<256>(&prof, x_dtype, dt, dim3(rows), dim3(256), a, s);
-    } else {
-        launch_norm_t<1024>(&prof, x_dtype, dt, dim3(rows), dim3(1024), a, s);
-    }
+    if (d <= 64 * 8) launch_norm_t<64, 1>(&prof, x_dtype, dt, a, s);
+    else if (d <= 64 * 16) launch_norm_t<64, 2>(&prof, x_dtype, dt, a, s);
+    else if (d <= 64 * 32) launch_norm_t<64, 4>(&prof, x_dtype, dt, a, s);
+    else if (d <= 256 * 16) launch_norm_t<256, 2>(&prof, x_dtype, dt, a, s);
+    else if (d <= 256 * 32) launch_norm_t<256, 4>(&prof, x_dtype, dt, a, s);
+    else if (d <= 1024 * 16) launch_norm_t<1024, 2>(&prof, x_dtype, dt, a, s);
+    else launch_norm_t<1024, 4>(&prof, x_dtype, dt, a, s);
     return hipGetLastError();
 }
 
