@@ -80,6 +80,9 @@ def parse():
     ap.add_argument("--tree-width", type=int, default=1,
                     help="token tree of this width (2 or 3) instead of the chain: every draft step also draws the "
                          "siblings, tabed_verify_tree verifies; the window update is then a call of its own")
+    ap.add_argument("--bits", type=int, default=16, choices=[16, 8],
+                    help="8: the drafts' LM head in int8 (rows quantised once, hidden states per row) and, with --draft-body, an 8-bit "
+                         "key / value cache; bf16 workloads")
     ap.add_argument("--draft-body", default="none", choices=["none", "68m", "160m"],
                     help="run the draft model's body (random weights) in front of every LM-head call instead of "
                          "feeding pre-generated hidden states; reports rounds/s of body + head + verify")
@@ -232,6 +235,12 @@ def main():
         args.separate_update = True
         buf.enable_tree(args.tree_width)
         Ls = gen_leaf_logits(wl, Ws, Hs, args.tree_width, device)
+    q8 = args.bits == 8
+    if q8:
+        if wl.w_dtype != 1:
+            sys.exit("bench.py: --bits 8 needs a bf16 workload")
+        Ws8 = [binding.quantize_rows(W) for W in Ws]
+        Hs8 = [[binding.quantize_rows(H.view(-1, wl.d)) for H in row] for row in Hs]
     upd_first = buf.prepare_update_weights(True)
     upd = buf.prepare_update_weights(False)
     body = None
@@ -245,14 +254,20 @@ def main():
         tensors = {k: ([as_dev(a) for a in v] if isinstance(v, list) else as_dev(v)) for k, v in bw.items()}
         bcfg = binding.make_body_cfg(layers=bc.layers, d=bc.d, heads=bc.heads, d_ff=bc.d_ff, V=bc.V, max_ctx=bc.max_ctx,
                                      rope_theta=bc.rope_theta, rms_eps=bc.rms_eps)
-        body = binding.BodyBuffers(bcfg, wl.n * wl.B, tensors, device)
+        body = (binding.BodyBuffersQ8 if q8 else binding.BodyBuffers)(bcfg, wl.n * wl.B, tensors, device)
         g = torch.Generator(device="cpu").manual_seed(11)
         # contexts of a few hundred tokens (prompt, image or caption tokens, what was generated so far), different
         # for every drafting method of a sequence; the caches hold unit-variance keys and values up to there
         body.ctx_base.copy_(torch.randint(256, 768, (wl.n * wl.B,), generator=g, dtype=torch.int32))
         body.ctx_len.copy_(body.ctx_base)
-        body.kcache.normal_()
-        body.vcache.normal_()
+        if q8:
+            for t in (body.cache.k, body.cache.v):
+                t.random_(-127, 128)
+            for t in (body.cache.kscale, body.cache.vscale):
+                t.fill_(3.0 / 127)            # unit variance, roughly
+        else:
+            body.kcache.normal_()
+            body.vcache.normal_()
         first_tokens = torch.randint(0, wl.V, (args.pool, wl.B), generator=g, dtype=torch.int32).to(device)
     def make_slots(per_step_rotation):
         out = []
@@ -266,7 +281,11 @@ def main():
                     # position 0 is fed the round's first token, position i > 0 the token drafted at i - 1
                     drafts.append(body.prepare_step(first_tokens[r], 0, 1, wl.n) if pos == 0 else
                                   body.prepare_step(buf.draft_tokens, pos - 1, wl.gamma, wl.n))
-                drafts.append(buf.prepare_draft_step(0, pos, W, body.H if body is not None else Hs[r][pos], temp))
+                if q8:
+                    W8 = Ws8[(r * wl.gamma + pos) % len(Ws)] if per_step_rotation else Ws8[r % len(Ws)]
+                    drafts.append(buf.prepare_draft_step_q8(0, pos, *W8, *((body.H8, body.h_scale) if body is not None else Hs8[r][pos]), temp))
+                else:
+                    drafts.append(buf.prepare_draft_step(0, pos, W, body.H if body is not None else Hs[r][pos], temp))
                 if tree:
                     drafts.append(buf.prepare_draft_siblings(0, pos, temp))
             ver = (buf.prepare_verify_tree(0, Ts[r], Ls[r], temp) if tree else
@@ -376,12 +395,12 @@ def main():
     kernels = {}
     roofline = None
     M = wl.n * wl.B
-    esz = 4 if wl.w_dtype == 0 else 2
+    esz = 1 if q8 else 4 if wl.w_dtype == 0 else 2
     NT = (wl.V + 31) // 32
     n_sampling = int((temp > 0).sum().item())
     # algorithmic bytes per launch: what the method must move, each logit written once and read once
     alg_bytes = {
-        "lmhead": wl.V * wl.d * esz + M * wl.V * 4 + M * wl.d * esz,            # W once + logits once + H
+        "lmhead": wl.V * wl.d * esz + M * wl.V * 4 + M * wl.d * esz + (4 * (wl.V + M) if q8 else 0),     # W once + logits once + H (+ scales)
         "sample": M * NT * 8 + n_sampling * wl.n * 32 * 4                         # softmax partials + one tile per row
                   + (wl.B - n_sampling) * wl.n * wl.V * 4,                        # greedy rows: the whole row
         "stats": wl.B * (wl.gamma + 1) * wl.V * 4 + wl.gamma * M * wl.V * 4,     # target rows + draft rows
@@ -438,12 +457,12 @@ def main():
         kernels["lmhead"].update(flops=lm_flops, achieved_tflops=tflops, frac_of_bf16_mfma_peak=tflops / MFMA_BF16_PEAK_TFLOPS)
         # the LM head is the dominant kernel; it is bound by the matrix cores only when its intensity
         # (flop per algorithmic byte) exceeds the ridge of the chip, i.e. at several hundred rows
-        mfma_bound = wl.w_dtype == 1 and lm_flops / lm_bytes > MFMA_BF16_PEAK_TFLOPS * 1e12 / (HBM_PEAK_GBS * 1e9)
-        traffic, traffic_note = measured_traffic(wl.name, "lmhead")
+        mfma_peak = 2 * MFMA_BF16_PEAK_TFLOPS if q8 else MFMA_BF16_PEAK_TFLOPS
+        mfma_bound = wl.w_dtype == 1 and lm_flops / lm_bytes > mfma_peak * 1e12 / (HBM_PEAK_GBS * 1e9)
+        traffic, traffic_note = (None, "not measured in 8 bits") if q8 else measured_traffic(wl.name, "lmhead")
         roofline = {"kernel": "lmhead"}
         if mfma_bound:
-            roofline.update(bound="mfma", achieved=tflops, peak=MFMA_BF16_PEAK_TFLOPS, unit="TFLOP/s",
-                            frac=tflops / MFMA_BF16_PEAK_TFLOPS)
+            roofline.update(bound="mfma", achieved=tflops, peak=mfma_peak, unit="TFLOP/s", frac=tflops / mfma_peak)
         else:
             roofline.update(bound="hbm", achieved=gbs, peak=HBM_PEAK_GBS, unit="GB/s", frac=gbs / HBM_PEAK_GBS)
         roofline.update(traffic=traffic, traffic_source=traffic_note,
@@ -458,18 +477,18 @@ def main():
     round_bytes = wl.gamma * (lm_bytes + alg_bytes["sample"]) + alg_bytes["stats"] + alg_bytes["resid"]
     out = {
         "metric": ("ensemble-draft+verify steps/sec at V=32k,n=4,B=16; HBM GB/s & MFMA % of peak"
-                   if wl.name == "serving" and not tree and body is None else "ensemble-draft+verify steps/sec"),
+                   if wl.name == "serving" and not tree and body is None and not q8 else "ensemble-draft+verify steps/sec"),
         "value": args.steps / dt, "unit": "steps/s",
         "n_gpus": 1, "steps": args.steps, "warmup": args.warmup, "ms_per_step": ms_per_step,
         "higher_is_better": True, "scaling": "weak", "vs_baseline": None,
-        "dtype": "bf16" if wl.w_dtype == 1 else "f32", "data": "synthetic",
+        "dtype": "int8" if q8 else "bf16" if wl.w_dtype == 1 else "f32", "data": "synthetic",
         "config": {"workload": f"{wl.name}: V={wl.V} d={wl.d} n={wl.n} B={wl.B} gamma={wl.gamma} h={wl.h} "
                                f"temperature={wl.temperature} policy={args.policy} distance={args.distance}",
                    "pool_rounds": args.pool, "w_copies": args.w_copies,
                    "calls_per_step": (2 if args.separate_update else 1) + wl.gamma * (2 if tree or body is not None else 1)
                                      + (1 if body is not None else 0), "launch": launch,
                    "window_update": "separate call" if args.separate_update else "fused into tabed_verify",
-                   "tree_width": args.tree_width, "draft_body": args.draft_body},
+                   "tree_width": args.tree_width, "draft_body": args.draft_body, **({"bits": 8} if q8 else {})},
         "roofline": roofline,
         "cpu_baseline": None,
         "detail": {"kernels": kernels, "mean_tokens_per_round": emitted,

@@ -26,7 +26,8 @@
  *   tabed_draft_body_rollback   Models": one decode step of the shared LLaMA-style draft model for the n * B rows.
  *   tabed_draft_step_static     tabed_draft_step for callers that cannot allocate device memory.
  *   tabed_norm_q8, tabed_linear_q8,                The draft model in 8 bits: norm, product, key / value cache and
- *   tabed_cache_append_q8, tabed_attention_q8      the attention over it.
+ *   tabed_cache_append_q8, tabed_attention_q8      the attention over it; a draft step and a body step of them:
+ *   tabed_draft_step_q8, tabed_draft_body_step_q8
  *
  * Notation: n = number of drafting methods (the paper's m), B independent
  * sequences, V vocabulary size, d draft hidden size, gamma block length,
@@ -421,6 +422,35 @@ int tabed_attention_q8_workspace_init(const tabed_cache_q8* cache, int32_t rows,
 int tabed_attention_q8(const tabed_cache_q8* cache, void* ws, int32_t rows, int32_t T, int32_t q_heads, int32_t q_dtype, const void* q,
                        int64_t q_row_stride, int64_t q_tok_stride, const int32_t* ctx_len, const int32_t* n_new, float scale,
                        int32_t out_dtype, void* out, int64_t out_row_stride, int64_t out_tok_stride, float* lse, void* stream);
+
+/*
+ * tabed_draft_step with the LM head in 8 bits: L = (H8 W8^T) * h_scale * w_scale, everything after the logits as there.
+ *   W [V,d] int8, w_scale [V] fp32: tabed_norm_q8 without a gain over the rows of a bf16 or fp32 matrix
+ *   H [B,n,d] int8, h_scale [B,n] fp32: as tabed_draft_body_step_q8 or tabed_norm_q8 leave them
+ * cfg->w_dtype is not read beyond its check; d is a multiple of 16, at most 131056, n B V at most 2^36.  `ws` as for tabed_draft_step, which may
+ * use the same one in between; siblings, verification and trees follow as after that call.
+ */
+int tabed_draft_step_q8(const tabed_cfg* cfg, void* ws, uint64_t round, int32_t pos, const void* W, const float* w_scale, const void* H,
+                        const float* h_scale, const float* weights, const float* temperature, const float* u_draft,
+                        float* draft_logits, double* draft_lse, int32_t* draft_tokens, float* draft_q, uint8_t* flags, void* stream);
+
+/*
+ * tabed_draft_body_step over an 8-bit cache (half the bytes of keys and values, and blocks that rows may share), with the hidden
+ * states in bf16, in int8 for tabed_draft_step_q8, or both.
+ *   cache    k, v [layers, blocks, heads, 64 * head_dim], kscale, vscale [layers, blocks, heads], one table for all layers;
+ *            kv_heads = heads, head_dim = d / heads (32, 64 or 128), max_blocks * 64 >= cfg->max_ctx.  The block that a row's next token goes to
+ *            belongs to that row.
+ *   H        [rows,d] bf16 out, or NULL      H8, h_scale  [rows,d] int8 and [rows] fp32 out, or both NULL (not with H NULL)
+ * Other arguments and the positions as for tabed_draft_body_step, tabed_draft_body_rollback included; a ctx_len entry outside [0, max_ctx) is
+ * an error of the caller: nothing is written outside the table's blocks, the results are not defined.
+ * `ws`: tabed_body_q8_workspace_bytes bytes, prepared once by ..._init for these sizes and rows (not shared with other calls that
+ * run at the same time).
+ */
+size_t tabed_body_q8_workspace_bytes(const tabed_body_cfg* cfg, const tabed_cache_q8* cache, int32_t rows);   /* 0: invalid */
+int tabed_body_q8_workspace_init(const tabed_body_cfg* cfg, const tabed_cache_q8* cache, int32_t rows, void* ws, void* stream);
+int tabed_draft_body_step_q8(const tabed_body_cfg* cfg, const tabed_body_weights* weights, void* ws, int32_t rows, const int32_t* token_src,
+                             int32_t token_stride, int32_t rows_per_token, int32_t* ctx_len, const tabed_cache_q8* cache, void* H, void* H8,
+                             float* h_scale, void* stream);
 
 /*
  * The uniforms tabed_draft_step and tabed_verify would draw: out[b,pos,word] for b < B,

@@ -18,6 +18,7 @@ EXPORTS = [
     "tabed_body_workspace_bytes", "tabed_body_workspace_init", "tabed_draft_body_step", "tabed_draft_body_rollback",
     "tabed_norm_q8", "tabed_linear_q8", "tabed_cache_append_q8",
     "tabed_attention_q8", "tabed_attention_q8_workspace_bytes", "tabed_attention_q8_workspace_init",
+    "tabed_draft_step_q8", "tabed_body_q8_workspace_bytes", "tabed_body_q8_workspace_init", "tabed_draft_body_step_q8",
     "tabed_prof_enable", "tabed_prof_read", "tabed_prof_reset", "tabed_kernel_name", "tabed_prof_null",
 ]
 
@@ -114,6 +115,14 @@ def load():
     lib.tabed_attention_q8_workspace_init.argtypes = [cachep, i32, i32, i32, vp, vp]
     lib.tabed_attention_q8.restype = C.c_int
     lib.tabed_attention_q8.argtypes = [cachep, vp, i32, i32, i32, i32, vp, i64, i64, vp, vp, f32, i32, vp, i64, i64, vp, vp]
+    lib.tabed_draft_step_q8.restype = C.c_int
+    lib.tabed_draft_step_q8.argtypes = [cfgp, vp, u64, i32] + [vp] * 13
+    lib.tabed_body_q8_workspace_bytes.restype = C.c_size_t
+    lib.tabed_body_q8_workspace_bytes.argtypes = [bcfgp, cachep, i32]
+    lib.tabed_body_q8_workspace_init.restype = C.c_int
+    lib.tabed_body_q8_workspace_init.argtypes = [bcfgp, cachep, i32, vp, vp]
+    lib.tabed_draft_body_step_q8.restype = C.c_int
+    lib.tabed_draft_body_step_q8.argtypes = [bcfgp, C.POINTER(TabedBodyWeights), vp, i32, vp, i32, i32, vp, cachep] + [vp] * 4
     lib.tabed_prof_enable.restype = C.c_int
     lib.tabed_prof_enable.argtypes = [C.c_int]
     lib.tabed_prof_read.restype = C.c_int
@@ -572,30 +581,33 @@ def prepare_linear_q8(x, x_scale, w, w_scale, y, stream=None) -> PreparedCall:
 
 class CacheQ8:
     """8-bit key / value cache over tensors of the caller's: k, v [blocks, kv_heads, 64 * head_dim] int8, kscale, vscale
-    [blocks, kv_heads] fp32, table [rows, max_blocks] int32 (entries outside [0, blocks): no block).  The struct holds the tensors'
-    addresses: the object keeps them alive."""
+    [blocks, kv_heads] fp32, table [rows, max_blocks] int32 (entries outside [0, blocks): no block); for a body of several layers with
+    a leading dimension `layers`, one table for all.  The struct holds the tensors' addresses: the object keeps them alive."""
 
     def __init__(self, k, v, kscale, vscale, table, head_dim):
         import torch
         self.device = _device_of(dict(k=k, v=v, kscale=kscale, vscale=vscale, table=table))
-        if k.dim() != 3 or k.shape[2] != CACHE_BLOCK * head_dim:
-            raise TabedError(f"k must be [blocks, kv_heads, {CACHE_BLOCK * head_dim}], got {tuple(k.shape)}")
+        if k.dim() not in (3, 4) or k.shape[-1] != CACHE_BLOCK * head_dim:
+            raise TabedError(f"k must be [(layers,) blocks, kv_heads, {CACHE_BLOCK * head_dim}], got {tuple(k.shape)}")
         if table.dim() != 2:
             raise TabedError("table must be [rows, max_blocks]")
-        blocks, kvh = k.shape[:2]
+        blocks, kvh = k.shape[-3:-1]
+        self.layers = k.shape[0] if k.dim() == 4 else 1
         self.rows, self.head_dim, self.kv_heads = table.shape[0], head_dim, kvh
         self.k, self.v, self.kscale, self.vscale, self.table = k, v, kscale, vscale, table
         self.struct = TabedCacheQ8(kvh, head_dim, blocks, table.shape[1], _ptr(k, torch.int8, None, "k"), _ptr(v, torch.int8, k.numel(), "v"),
-                                   _ptr(kscale, torch.float32, blocks * kvh, "kscale"), _ptr(vscale, torch.float32, blocks * kvh, "vscale"),
+                                   _ptr(kscale, torch.float32, self.layers * blocks * kvh, "kscale"),
+                                   _ptr(vscale, torch.float32, self.layers * blocks * kvh, "vscale"),
                                    _ptr(table, torch.int32, None, "table"))
 
     @classmethod
-    def allocate(cls, rows, tokens, kv_heads, head_dim, device="cuda:0"):
+    def allocate(cls, rows, tokens, kv_heads, head_dim, layers=None, device="cuda:0"):
         """An empty cache with room for `tokens` tokens in every row, blocks dealt to the rows in order."""
         import torch
         width = (tokens + CACHE_BLOCK - 1) // CACHE_BLOCK
-        k = torch.zeros((rows * width, kv_heads, CACHE_BLOCK * head_dim), dtype=torch.int8, device=device)
-        ks = torch.zeros((rows * width, kv_heads), dtype=torch.float32, device=device)
+        lead = () if layers is None else (layers,)
+        k = torch.zeros((*lead, rows * width, kv_heads, CACHE_BLOCK * head_dim), dtype=torch.int8, device=device)
+        ks = torch.zeros((*lead, rows * width, kv_heads), dtype=torch.float32, device=device)
         table = torch.arange(rows * width, dtype=torch.int32, device=device).view(rows, width)
         return cls(k, torch.zeros_like(k), ks, torch.zeros_like(ks), table, head_dim)
 
@@ -624,6 +636,7 @@ def _new_tokens(t, heads, hd):
 
 def _prepare_cache_append_q8(cache, k, v, ctx_len, n_new, stream):
     import torch
+    _one_layer(cache, "tabed_cache_append_q8")
     dev = _device_of({"cache": cache.k, "k": k, "v": v, "ctx_len": ctx_len, "n_new": n_new})
     T = _new_tokens(k, cache.kv_heads, cache.head_dim)
     kp, row, tok = _heads_view(k, cache.rows, T, cache.kv_heads, cache.head_dim, "k")
@@ -672,6 +685,7 @@ def new_attention_workspace(cache: CacheQ8, rows, T, q_heads, stream=None):
 
 def _prepare_attention_q8(cache, ws, q, ctx_len, out, n_new, scale, lse, stream):
     import torch
+    _one_layer(cache, "tabed_attention_q8")
     dev = _device_of(dict(cache=cache.k, ws=ws, q=q, ctx_len=ctx_len, out=out, n_new=n_new, lse=lse))
     hd = cache.head_dim
     T = _new_tokens(q, None, hd)
@@ -697,6 +711,89 @@ def tabed_attention_q8(cache: CacheQ8, ws, q, ctx_len, out, n_new=None, scale=No
 def prepare_attention_q8(cache: CacheQ8, ws, q, ctx_len, out, n_new=None, scale=None, lse=None, stream=None) -> PreparedCall:
     return _prepare_attention_q8(cache, ws, q, ctx_len, out, n_new, scale, lse, stream)
 
+
+
+def _one_layer(cache, what):
+    if cache.layers != 1:
+        raise TabedError(f"{what} takes the cache of one layer, this one has {cache.layers}")
+
+
+def _prepare_draft_step_q8(cfg, ws, rnd, pos, W, w_scale, H, h_scale, weights, temperature, draft_logits, draft_lse, draft_tokens,
+                           draft_q, flags, u_draft, stream):
+    import torch
+    V, d, n, B, g = cfg.V, cfg.d, cfg.n, cfg.B, cfg.gamma
+    dev = _device_of(dict(ws=ws, W=W, w_scale=w_scale, H=H, h_scale=h_scale, weights=weights, temperature=temperature, draft_logits=draft_logits,
+                          draft_lse=draft_lse, draft_tokens=draft_tokens, draft_q=draft_q, flags=flags, u_draft=u_draft))
+    vp = C.c_void_p
+    args = [C.byref(cfg), vp(_ptr(ws, torch.uint8, name="ws")), C.c_uint64(rnd), C.c_int32(pos), vp(_ptr(W, torch.int8, V * d, "W")),
+            vp(_ptr(w_scale, torch.float32, V, "w_scale")), vp(_ptr(H, torch.int8, B * n * d, "H")),
+            vp(_ptr(h_scale, torch.float32, B * n, "h_scale")), vp(_ptr(weights, torch.float32, B * n, "weights")),
+            vp(_ptr(temperature, torch.float32, B, "temperature")), vp(_ptr(u_draft, torch.float32, B * g, "u_draft")),
+            vp(_ptr(draft_logits, torch.float32, g * B * n * V, "draft_logits")), vp(_ptr(draft_lse, torch.float64, g * B * n, "draft_lse")),
+            vp(_ptr(draft_tokens, torch.int32, B * g, "draft_tokens")), vp(_ptr(draft_q, torch.float32, B * g, "draft_q")),
+            vp(_ptr(flags, torch.uint8, B * g, "flags")), vp(_stream_on(dev, stream))]
+    call = DeviceCall(load().tabed_draft_step_q8, args, "tabed_draft_step_q8", dev,
+                      (cfg, ws, W, w_scale, H, h_scale, weights, temperature, u_draft, draft_logits, draft_lse, draft_tokens, draft_q, flags))
+    call.round_arg = args[2]
+    return call
+
+
+def tabed_draft_step_q8(cfg, ws, rnd, pos, W, w_scale, H, h_scale, weights, temperature, draft_logits, draft_lse, draft_tokens,
+                        draft_q, flags, u_draft=None, stream=None):
+    """tabed_draft_step with int8 W and H and their scales (see tabed_norm_q8)."""
+    _prepare_draft_step_q8(cfg, ws, rnd, pos, W, w_scale, H, h_scale, weights, temperature, draft_logits, draft_lse, draft_tokens, draft_q,
+                           flags, u_draft, stream)()
+
+
+def quantize_rows(x, stream=None):
+    """(int8 rows, scales) of a [rows, d] bf16 or fp32 matrix: how an LM head or other weights are laid out, once, for the 8-bit products."""
+    import torch
+    q = torch.empty(x.shape, dtype=torch.int8, device=x.device)
+    scale = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
+    tabed_norm_q8(x, q, scale, stream=stream)
+    return q, scale
+
+
+def tabed_body_q8_workspace_bytes(bcfg, cache, rows) -> int:
+    return int(load().tabed_body_q8_workspace_bytes(C.byref(bcfg), C.byref(cache.struct), rows))
+
+
+def tabed_body_q8_workspace_init(bcfg, cache, rows, ws, stream=None):
+    import torch
+    dev = _device_of(dict(cache=cache.k, ws=ws))
+    need = tabed_body_q8_workspace_bytes(bcfg, cache, rows)
+    if need == 0 or ws.numel() * ws.element_size() < need:
+        raise TabedError(f"body workspace holds {ws.numel() * ws.element_size()} bytes, {need} needed (0: invalid sizes)")
+    with torch.cuda.device(dev):
+        _check(load().tabed_body_q8_workspace_init(C.byref(bcfg), C.byref(cache.struct), rows, _ptr(ws, torch.uint8, None, "ws"), _stream_on(dev, stream)),
+               "tabed_body_q8_workspace_init")
+
+
+def _prepare_draft_body_step_q8(bcfg, weights, ws, rows, token_src, token_stride, rows_per_token, ctx_len, cache, H, H8, h_scale, stream):
+    import torch
+    base, off = token_src if isinstance(token_src, tuple) else (token_src, 0)
+    need = off + ((rows - 1) // rows_per_token) * token_stride + 1
+    if base.dtype != torch.int32 or not base.is_cuda or not base.is_contiguous() or base.numel() < need or off < 0:
+        raise TabedError("token_src must be a contiguous int32 GPU tensor covering every token read")
+    dev = _device_of(dict(cache=cache.k, ws=ws, token_src=base, ctx_len=ctx_len, H=H, H8=H8, h_scale=h_scale))
+    if cache.rows != rows or cache.layers != bcfg.layers:
+        raise TabedError(f"the cache is of {cache.rows} rows and {cache.layers} layers, the step of {rows} and {bcfg.layers}")
+    if ws.numel() * ws.element_size() < tabed_body_q8_workspace_bytes(bcfg, cache, rows):
+        raise TabedError("body workspace too small")
+    if H is not None and H.dtype not in (torch.bfloat16, torch.int16, torch.uint16):
+        raise TabedError(f"H must hold bf16 values, got {H.dtype}")
+    vp = C.c_void_p
+    args = [C.byref(bcfg), C.byref(weights), vp(_ptr(ws, torch.uint8, name="ws")), C.c_int32(rows), vp(base.data_ptr() + 4 * off),
+            C.c_int32(token_stride), C.c_int32(rows_per_token), vp(_ptr(ctx_len, torch.int32, rows, "ctx_len")), C.byref(cache.struct),
+            vp(_ptr(H, None, rows * bcfg.d, "H")), vp(_ptr(H8, torch.int8, rows * bcfg.d, "H8")), vp(_ptr(h_scale, torch.float32, rows, "h_scale")),
+            vp(_stream_on(dev, stream))]
+    return DeviceCall(load().tabed_draft_body_step_q8, args, "tabed_draft_body_step_q8", dev, (bcfg, weights, ws, base, ctx_len, cache, H, H8, h_scale))
+
+
+def tabed_draft_body_step_q8(bcfg, weights, ws, rows, token_src, token_stride, rows_per_token, ctx_len, cache, H=None, H8=None, h_scale=None,
+                             stream=None):
+    """tabed_draft_body_step over an 8-bit cache (CacheQ8 with `layers`), writing H (bf16), H8 and h_scale (int8), or all three."""
+    _prepare_draft_body_step_q8(bcfg, weights, ws, rows, token_src, token_stride, rows_per_token, ctx_len, cache, H, H8, h_scale, stream)()
 
 
 class BodyBuffers:
@@ -737,6 +834,31 @@ class BodyBuffers:
         args = [C.c_int32(self.rows), C.c_int32(rows_per_seq), C.c_int32(gamma), vp(self.ctx_base.data_ptr()),
                 vp(_ptr(accept_len, torch.int32, nseq, "accept_len")), vp(self.ctx_len.data_ptr()), vp(_stream(stream))]
         return PreparedCall(load().tabed_draft_body_rollback, args, "tabed_draft_body_rollback")
+
+
+class BodyBuffersQ8:
+    """BodyBuffers over an 8-bit cache: weight table, scratch, cache of max_ctx tokens a row, positions, hidden states in int8."""
+
+    def __init__(self, bcfg: TabedBodyCfg, rows: int, tensors: dict, device="cuda:0"):
+        import torch
+        self.cfg, self.rows, self.tensors = bcfg, rows, tensors
+        self.table = make_body_weights(bcfg, tensors)
+        self.cache = CacheQ8.allocate(rows, bcfg.max_ctx, bcfg.heads, bcfg.d // bcfg.heads, bcfg.layers, device)
+        need = tabed_body_q8_workspace_bytes(bcfg, self.cache, rows)
+        if need == 0:
+            raise TabedError("invalid body configuration")
+        self.ws = torch.empty(need, dtype=torch.uint8, device=device)
+        tabed_body_q8_workspace_init(bcfg, self.cache, rows, self.ws)
+        self.ctx_len = torch.zeros(rows, dtype=torch.int32, device=device)
+        self.ctx_base = torch.zeros(rows, dtype=torch.int32, device=device)
+        self.H8 = torch.zeros((rows, bcfg.d), dtype=torch.int8, device=device)
+        self.h_scale = torch.zeros(rows, dtype=torch.float32, device=device)
+
+    def prepare_step(self, token_src, token_offset, token_stride, rows_per_token, stream=None) -> PreparedCall:
+        return _prepare_draft_body_step_q8(self.cfg, self.table, self.ws, self.rows, (token_src, token_offset), token_stride, rows_per_token,
+                                           self.ctx_len, self.cache, None, self.H8, self.h_scale, stream)
+
+    prepare_rollback = BodyBuffers.prepare_rollback
 
 
 class RoundBuffers:
@@ -829,6 +951,10 @@ class RoundBuffers:
                 vp(self.draft_logits.data_ptr()), vp(self.draft_lse.data_ptr()), vp(self.draft_tokens.data_ptr()),
                 vp(self.draft_q.data_ptr()), vp(self.draft_flags.data_ptr()), vp(_stream(stream))]
         return PreparedCall(load().tabed_draft_step, args, "tabed_draft_step", args[2])
+
+    def prepare_draft_step_q8(self, rnd, pos, W, w_scale, H, h_scale, temperature, u_draft=None, stream=None) -> PreparedCall:
+        return _prepare_draft_step_q8(self.cfg, self.ws, rnd, pos, W, w_scale, H, h_scale, self.weights, temperature, self.draft_logits,
+                                      self.draft_lse, self.draft_tokens, self.draft_q, self.draft_flags, u_draft, stream)
 
     def prepare_verify(self, rnd, target_logits, temperature, u_acc=None, u_res=None, stream=None,
                        fused_update=False) -> PreparedCall:

@@ -351,6 +351,17 @@ int tabed_body_workspace_init(const tabed_body_cfg* cfg, int32_t rows, void* ws,
     return e == hipSuccess ? TABED_OK : fail_hip(e);
 }
 
+static int check_body_weights(const tabed_body_cfg& cfg, const tabed_body_weights& w) {
+    if (!w.embed || !w.g_final) return TABED_ENULL;
+    for (int l = 0; l < cfg.layers; ++l) {
+        if (!w.g_attn[l] || !w.wqkv[l] || !w.wo[l] || !w.g_mlp[l] || !w.wgu[l] || !w.wdown[l]) return TABED_ENULL;
+        if (misaligned(w.wqkv[l]) || misaligned(w.wo[l]) || misaligned(w.wgu[l]) || misaligned(w.wdown[l]) || misaligned(w.g_attn[l]) ||
+            misaligned(w.g_mlp[l]))
+            return TABED_EALIGN;
+    }
+    return misaligned(w.embed) || misaligned(w.g_final) ? TABED_EALIGN : TABED_OK;
+}
+
 // tabed_draft_body_step, for the tests with workgroups of the one-launch step from number late_from on that come after the others
 // have stopped waiting for them, and with one that takes part and does nothing, so that waits for it end unanswered, after
 // milliseconds (0: as in earnest).
@@ -361,18 +372,9 @@ int tabed_testing_body_step(const tabed_body_cfg* cfg, const tabed_body_weights*
     if (rc != TABED_OK) return rc;
     if (!weights || !ws || !token_src || !ctx_len || !kcache || !vcache || !H) return TABED_ENULL;
     if (rows_per_token < 1 || token_stride < 0) return TABED_ERANGE;
-    if (!weights->embed || !weights->g_final) return TABED_ENULL;
-    for (int l = 0; l < cfg->layers; ++l) {
-        if (!weights->g_attn[l] || !weights->wqkv[l] || !weights->wo[l] || !weights->g_mlp[l] || !weights->wgu[l] ||
-            !weights->wdown[l])
-            return TABED_ENULL;
-        if (misaligned(weights->wqkv[l]) || misaligned(weights->wo[l]) || misaligned(weights->wgu[l]) ||
-            misaligned(weights->wdown[l]) || misaligned(weights->g_attn[l]) || misaligned(weights->g_mlp[l]))
-            return TABED_EALIGN;
-    }
-    if (misaligned(ws) || misaligned(kcache) || misaligned(vcache) || misaligned(H) || misaligned(weights->embed) ||
-        misaligned(weights->g_final))
-        return TABED_EALIGN;
+    const int rw = check_body_weights(*cfg, *weights);
+    if (rw != TABED_OK) return rw;
+    if (misaligned(ws) || misaligned(kcache) || misaligned(vcache) || misaligned(H)) return TABED_EALIGN;
     const hipError_t e = launch_body_step(*cfg, *weights, static_cast<char*>(ws), rows, token_src, token_stride, rows_per_token,
                                           ctx_len, static_cast<uint16_t*>(kcache), static_cast<uint16_t*>(vcache),
                                           static_cast<uint16_t*>(H), static_cast<hipStream_t>(stream), late_from, absent);
@@ -477,6 +479,67 @@ int tabed_attention_q8(const tabed_cache_q8* cache, void* ws, int32_t rows, int3
         return TABED_EALIGN;
     const hipError_t e = launch_attention_q8(*cache, static_cast<char*>(ws), rows, T, q_heads, q_dtype, q, q_row_stride, q_tok_stride, ctx_len, n_new,
                                              scale, out_dtype, out, out_row_stride, out_tok_stride, lse, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? TABED_OK : fail_hip(e);
+}
+
+int tabed_draft_step_q8(const tabed_cfg* cfg, void* ws, uint64_t round, int32_t pos, const void* W, const float* w_scale, const void* H,
+                        const float* h_scale, const float* weights, const float* temperature, const float* u_draft,
+                        float* draft_logits, double* draft_lse, int32_t* draft_tokens, float* draft_q, uint8_t* flags, void* stream) {
+    const int rc = validate_cfg(cfg);
+    if (rc != TABED_OK) return rc;
+    if (!ws || !W || !w_scale || !H || !h_scale || !weights || !temperature || !draft_logits || !draft_lse || !draft_tokens || !draft_q || !flags)
+        return TABED_ENULL;
+    if (pos < 0 || pos >= cfg->gamma) return TABED_ERANGE;
+    if (cfg->d % 16 != 0) return TABED_EINVAL;
+    if (cfg->d > 131056 || (int64_t)cfg->B * cfg->n * cfg->V > (1ll << 36)) return TABED_ERANGE;
+    if (misaligned(ws) || misaligned(W) || misaligned(H) || misaligned(draft_logits) || misaligned(draft_lse) || element_misaligned(w_scale, 0) ||
+        element_misaligned(h_scale, 0))
+        return TABED_EALIGN;
+    const WsLayout L = ws_layout(*cfg);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    float* slot = draft_logits + (size_t)pos * L.M * cfg->V;
+    hipError_t e = launch_lmhead_q8(*cfg, L, static_cast<char*>(ws), static_cast<const int8_t*>(W), w_scale, static_cast<const int8_t*>(H), h_scale,
+                                    temperature, slot, s);
+    if (e != hipSuccess) return fail_hip(e);
+    e = launch_sample(*cfg, L, static_cast<char*>(ws), round, pos, slot, weights, temperature, u_draft, draft_lse, draft_tokens, draft_q, flags, s);
+    return e == hipSuccess ? TABED_OK : fail_hip(e);
+}
+
+static int validate_body_q8(const tabed_body_cfg* cfg, const tabed_cache_q8* cache, int32_t rows, bool pointers) {
+    int rc = validate_body_cfg(cfg, rows);
+    if (rc == TABED_OK) rc = validate_cache(cache, pointers);
+    if (rc != TABED_OK) return rc;
+    if (cache->kv_heads != cfg->heads || cache->head_dim != cfg->d / cfg->heads) return TABED_EINVAL;
+    if ((int64_t)cache->max_blocks * TABED_CACHE_BLOCK < cfg->max_ctx) return TABED_EINVAL;
+    return validate_attention(cache, rows, 1, cfg->heads, false);
+}
+
+size_t tabed_body_q8_workspace_bytes(const tabed_body_cfg* cfg, const tabed_cache_q8* cache, int32_t rows) {
+    if (validate_body_q8(cfg, cache, rows, false) != TABED_OK) return 0;
+    return body_q8_layout(*cfg, *cache, rows).total;
+}
+
+int tabed_body_q8_workspace_init(const tabed_body_cfg* cfg, const tabed_cache_q8* cache, int32_t rows, void* ws, void* stream) {
+    const int rc = validate_body_q8(cfg, cache, rows, false);
+    if (rc != TABED_OK) return rc;
+    if (ws == nullptr) return TABED_ENULL;
+    if (misaligned(ws)) return TABED_EALIGN;
+    const hipError_t e = launch_body_q8_init(*cfg, *cache, rows, static_cast<char*>(ws), static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? TABED_OK : fail_hip(e);
+}
+
+int tabed_draft_body_step_q8(const tabed_body_cfg* cfg, const tabed_body_weights* weights, void* ws, int32_t rows, const int32_t* token_src,
+                             int32_t token_stride, int32_t rows_per_token, int32_t* ctx_len, const tabed_cache_q8* cache, void* H, void* H8,
+                             float* h_scale, void* stream) {
+    int rc = validate_body_q8(cfg, cache, rows, true);
+    if (rc != TABED_OK) return rc;
+    if (!weights || !ws || !token_src || !ctx_len || (!H && !H8) || (H8 == nullptr) != (h_scale == nullptr)) return TABED_ENULL;
+    if (rows_per_token < 1 || token_stride < 0) return TABED_ERANGE;
+    rc = check_body_weights(*cfg, *weights);
+    if (rc != TABED_OK) return rc;
+    if (misaligned(ws) || misaligned(H) || misaligned(H8) || element_misaligned(h_scale, 0)) return TABED_EALIGN;
+    const hipError_t e = launch_body_step_q8(*cfg, *weights, static_cast<char*>(ws), rows, token_src, token_stride, rows_per_token, ctx_len, *cache,
+                                             static_cast<uint16_t*>(H), static_cast<int8_t*>(H8), h_scale, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? TABED_OK : fail_hip(e);
 }
 

@@ -627,14 +627,14 @@ static int attn_splits(const tabed_body_cfg& c, int rows) {
 
 int body_route(const tabed_body_cfg& c, int rows) { return gang_applies(c, rows) ? 0 : attn_splits(c, rows); }
 
-BodyLayout body_layout(const tabed_body_cfg& c, int rows) {
+BodyLayout body_layout(const tabed_body_cfg& c, int rows, bool q8) {
     BodyLayout L;
     const int act = (c.d > c.d_ff) ? c.d : c.d_ff;
-    const size_t S = (size_t)attn_splits(c, rows);
+    const size_t S = q8 ? 1 : (size_t)attn_splits(c, rows);            // (the 8-bit cache's attention joins its ranges itself)
     size_t off = 0;
     L.off_ctl = off;  off += kGangControlBytes;
     // (here, so that where its buffers are follows from the sizes that the control block remembers them by, which leave max_ctx out)
-    L.off_gang = off; off = al256(off + (gang_applies(c, rows) ? gang_bytes(c, rows) : 0));
+    L.off_gang = off; off = al256(off + (!q8 && gang_applies(c, rows) ? gang_bytes(c, rows) : 0));
     L.off_x = off;    off = al256(off + sizeof(float) * (size_t)rows * c.d);
     L.off_q = off;    off = al256(off + sizeof(float) * (size_t)rows * c.d);
     L.off_trig = off; off = al256(off + sizeof(double2) * (size_t)rows * ((c.d / c.heads) / 2));
@@ -771,22 +771,21 @@ static void launch_attn(const ProfScope* prof, const tabed_body_cfg& c, int rows
     launch(prof, k_body_attn<LPK>, dim3(c.heads, rows, splits), dim3(kBlock), 0, s, c.d, c.max_ctx, q, ctx_len, kc, vc, att, po, pml);
 }
 
-hipError_t launch_body_step(const tabed_body_cfg& c, const tabed_body_weights& w, char* ws, int rows,
-                            const int32_t* token_src, int token_stride, int rows_per_token, int32_t* ctx_len,
-                            uint16_t* kcache, uint16_t* vcache, uint16_t* H, hipStream_t s, int late_from, int absent) {
-    const BodyLayout L = body_layout(c, rows);
-    if (gang_applies(c, rows))
-        return launch_gang(c, w, ws + L.off_ctl, ws + L.off_gang, rows, token_src, token_stride, rows_per_token, ctx_len, kcache, vcache, H, s,
-                           late_from, absent);
+// The launches of a step up to the final norm, whose arguments come back in `last`.  caches(l, a) says where layer l's projection puts
+// the new keys and values, attend(l, a) leaves the layer's attention in hb (splits = 1) or its ranges' sums.
+template <typename Caches, typename Attend>
+static hipError_t body_layers(const tabed_body_cfg& c, const tabed_body_weights& w, char* ws, const BodyLayout& L, int rows, int splits,
+                              const int32_t* token_src, int token_stride, int rows_per_token, int32_t* ctx_len, Caches&& caches,
+                              Attend&& attend, ProjArgs& last, hipStream_t s) {
     uint16_t* hb = reinterpret_cast<uint16_t*>(ws + L.off_hb);
-    float* po = reinterpret_cast<float*>(ws + L.off_po);
-    float* pml = reinterpret_cast<float*>(ws + L.off_pml);
-    const int d = c.d, hd = c.d / c.heads, splits = attn_splits(c, rows);
+    const int d = c.d, hd = c.d / c.heads;
     const bool many = !fused_rows(c.d, rows);
     uint16_t* hn = reinterpret_cast<uint16_t*>(ws + L.off_hn);
     ProjArgs base{};
     base.M = rows; base.eps = c.rms_eps; base.hd = hd; base.max_ctx = c.max_ctx;
-    base.ctx_len = ctx_len; base.splits = splits; base.po = po; base.pml = pml;
+    base.ctx_len = ctx_len; base.splits = splits;
+    base.po = reinterpret_cast<float*>(ws + L.off_po);
+    base.pml = reinterpret_cast<float*>(ws + L.off_pml);
     base.x = reinterpret_cast<float*>(ws + L.off_x);
     base.q = reinterpret_cast<float*>(ws + L.off_q);
     base.X = hb; base.act = hb;
@@ -801,23 +800,11 @@ hipError_t launch_body_step(const tabed_body_cfg& c, const tabed_body_weights& w
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     for (int l = 0; l < c.layers; ++l) {
-        const size_t layer_off = (size_t)l * rows * c.max_ctx * d;
         ProjArgs a = base;
-        a.kc = kcache + layer_off; a.vc = vcache + layer_off;
+        caches(l, a);
         a.W = static_cast<const uint16_t*>(w.wqkv[l]); a.N = 3 * d; a.K = d; a.g = w.g_attn[l];
         if ((e = norm_projection<kEpiRope>(a, hn, 3 * ((d + 31) / 32), ws, L, s)) != hipSuccess) return e;
-        {
-            ProfScope prof(TABED_K_BODY, s);
-            switch (hd) {
-                case 8: launch_attn<1>(&prof, c, rows, splits, a.q, ctx_len, a.kc, a.vc, hb, po, pml, s); break;
-                case 16: launch_attn<2>(&prof, c, rows, splits, a.q, ctx_len, a.kc, a.vc, hb, po, pml, s); break;
-                case 32: launch_attn<4>(&prof, c, rows, splits, a.q, ctx_len, a.kc, a.vc, hb, po, pml, s); break;
-                case 64: launch_attn<8>(&prof, c, rows, splits, a.q, ctx_len, a.kc, a.vc, hb, po, pml, s); break;
-                case 128: launch_attn<16>(&prof, c, rows, splits, a.q, ctx_len, a.kc, a.vc, hb, po, pml, s); break;
-                default: return hipErrorInvalidValue;
-            }
-            if ((e = hipGetLastError()) != hipSuccess) return e;
-        }
+        if ((e = attend(l, a)) != hipSuccess) return e;
         a = base;
         a.W = static_cast<const uint16_t*>(w.wo[l]); a.N = d; a.K = d;
         if (many) e = gemm_projection<kEpiAdd>(a, hb, ws, L, s);
@@ -832,9 +819,89 @@ hipError_t launch_body_step(const tabed_body_cfg& c, const tabed_body_weights& w
         e = many ? gemm_projection<kEpiAdd>(a, hb, ws, L, s) : projection<kInBf16, kEpiAdd>(a, (d + 15) / 16, s);
         if (e != hipSuccess) return e;
     }
-    ProjArgs a = base;
-    a.K = d; a.g = w.g_final;
-    return launch_norm(a, H, ctx_len, s);
+    last = base;
+    last.K = d; last.g = w.g_final;
+    return hipSuccess;
+}
+
+hipError_t launch_body_step(const tabed_body_cfg& c, const tabed_body_weights& w, char* ws, int rows,
+                            const int32_t* token_src, int token_stride, int rows_per_token, int32_t* ctx_len,
+                            uint16_t* kcache, uint16_t* vcache, uint16_t* H, hipStream_t s, int late_from, int absent) {
+    const BodyLayout L = body_layout(c, rows);
+    if (gang_applies(c, rows))
+        return launch_gang(c, w, ws + L.off_ctl, ws + L.off_gang, rows, token_src, token_stride, rows_per_token, ctx_len, kcache, vcache, H, s,
+                           late_from, absent);
+    uint16_t* hb = reinterpret_cast<uint16_t*>(ws + L.off_hb);
+    const int hd = c.d / c.heads, splits = attn_splits(c, rows);
+    ProjArgs last;
+    auto caches = [&](int l, ProjArgs& a) {
+        const size_t layer_off = (size_t)l * rows * c.max_ctx * c.d;
+        a.kc = kcache + layer_off; a.vc = vcache + layer_off;
+    };
+    auto attend = [&](int, const ProjArgs& a) {
+        ProfScope prof(TABED_K_BODY, s);
+        float* const po = const_cast<float*>(a.po);
+        float* const pml = const_cast<float*>(a.pml);
+        switch (hd) {
+            case 8: launch_attn<1>(&prof, c, rows, splits, a.q, ctx_len, a.kc, a.vc, hb, po, pml, s); break;
+            case 16: launch_attn<2>(&prof, c, rows, splits, a.q, ctx_len, a.kc, a.vc, hb, po, pml, s); break;
+            case 32: launch_attn<4>(&prof, c, rows, splits, a.q, ctx_len, a.kc, a.vc, hb, po, pml, s); break;
+            case 64: launch_attn<8>(&prof, c, rows, splits, a.q, ctx_len, a.kc, a.vc, hb, po, pml, s); break;
+            case 128: launch_attn<16>(&prof, c, rows, splits, a.q, ctx_len, a.kc, a.vc, hb, po, pml, s); break;
+            default: return hipErrorInvalidValue;
+        }
+        return hipGetLastError();
+    };
+    const hipError_t e = body_layers(c, w, ws, L, rows, splits, token_src, token_stride, rows_per_token, ctx_len, caches, attend, last, s);
+    return e != hipSuccess ? e : launch_norm(last, H, ctx_len, s);
+}
+
+// ---------------------------------------------------------------- the same with an 8-bit cache
+// The projection leaves the new keys and values, rounded to bf16 as everything that a projection hands on, in a cache of one position a row;
+// from there they are appended to the blocks.  Six launches a layer.
+BodyQ8Layout body_q8_layout(const tabed_body_cfg& c, const tabed_cache_q8& cache, int rows) {
+    BodyQ8Layout L;
+    L.body = body_layout(c, rows, true);
+    size_t off = L.body.total;
+    L.off_k = off;    off = al256(off + sizeof(uint16_t) * (size_t)rows * c.d);
+    L.off_v = off;    off = al256(off + sizeof(uint16_t) * (size_t)rows * c.d);
+    L.off_attn = off; off = al256(off + attn_layout(cache, rows, 1, c.heads).total);
+    L.total = off;
+    return L;
+}
+
+hipError_t launch_body_q8_init(const tabed_body_cfg& c, const tabed_cache_q8& cache, int rows, char* ws, hipStream_t s) {
+    return launch_attn_init(cache, rows, 1, c.heads, ws + body_q8_layout(c, cache, rows).off_attn, s);
+}
+
+hipError_t launch_body_step_q8(const tabed_body_cfg& c, const tabed_body_weights& w, char* ws, int rows, const int32_t* token_src,
+                               int token_stride, int rows_per_token, int32_t* ctx_len, const tabed_cache_q8& cache, uint16_t* H,
+                               int8_t* H8, float* h_scale, hipStream_t s) {
+    const BodyQ8Layout L = body_q8_layout(c, cache, rows);
+    const int d = c.d, hd = c.d / c.heads;
+    uint16_t* kn = reinterpret_cast<uint16_t*>(ws + L.off_k);
+    uint16_t* vn = reinterpret_cast<uint16_t*>(ws + L.off_v);
+    ProjArgs last;
+    auto caches = [&](int, ProjArgs& a) {
+        a.kc = kn; a.vc = vn; a.max_ctx = 1;
+    };
+    auto attend = [&](int l, const ProjArgs& a) {
+        tabed_cache_q8 layer = cache;
+        const size_t heads = (size_t)l * cache.blocks * cache.kv_heads;
+        layer.k = static_cast<int8_t*>(cache.k) + heads * TABED_CACHE_BLOCK * hd;
+        layer.v = static_cast<int8_t*>(cache.v) + heads * TABED_CACHE_BLOCK * hd;
+        layer.kscale = cache.kscale + heads;
+        layer.vscale = cache.vscale + heads;
+        const hipError_t e = launch_cache_append(layer, rows, 1, 1, kn, vn, d, d, ctx_len, nullptr, s);
+        if (e != hipSuccess) return e;
+        return launch_attention_q8(layer, ws + L.off_attn, rows, 1, c.heads, 0, a.q, d, d, ctx_len, nullptr, 1.f / std::sqrt((float)hd), 1,
+                                   ws + L.body.off_hb, d, d, nullptr, s);
+    };
+    hipError_t e = body_layers(c, w, ws, L.body, rows, 1, token_src, token_stride, rows_per_token, ctx_len, caches, attend, last, s);
+    if (e != hipSuccess) return e;
+    if (H != nullptr && (e = launch_norm(last, H, H8 == nullptr ? ctx_len : nullptr, s)) != hipSuccess) return e;
+    if (H8 == nullptr) return hipSuccess;
+    return launch_norm_q8(rows, d, 0, last.x, d, 0, nullptr, 0, nullptr, 0, last.g, c.rms_eps, H8, d, h_scale, ctx_len, s);
 }
 
 hipError_t launch_body_rollback(int rows, int rows_per_seq, int gamma, const int32_t* ctx_base, const int32_t* accept_len,

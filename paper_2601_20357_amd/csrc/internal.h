@@ -122,7 +122,7 @@ struct BodyLayout {
     size_t off_ones;   //   float [rows]: the "temperature" they divide by
     size_t total;
 };
-BodyLayout body_layout(const tabed_body_cfg& c, int rows);
+BodyLayout body_layout(const tabed_body_cfg& c, int rows, bool q8 = false);
 size_t body_workspace_bytes(const tabed_body_cfg& c, int rows);
 int validate_body_cfg(const tabed_body_cfg* c, int rows);
 hipError_t launch_body_init(const tabed_body_cfg& c, int rows, char* ws, hipStream_t s);
@@ -161,6 +161,21 @@ hipError_t launch_attn_init(const tabed_cache_q8& c, int rows, int T, int q_head
 hipError_t launch_attention_q8(const tabed_cache_q8& c, char* ws, int rows, int T, int q_heads, int q_dtype, const void* q, int64_t q_row,
                                int64_t q_tok, const int32_t* ctx_len, const int32_t* n_new, float scale, int out_dtype, void* out,
                                int64_t out_row, int64_t out_tok, float* lse, hipStream_t s);
+
+struct BodyQ8Layout {
+    BodyLayout body;
+    size_t off_k, off_v; // bf16 [rows,d] the layer's new keys and values
+    size_t off_attn;     // workspace of the attention
+    size_t total;
+};
+BodyQ8Layout body_q8_layout(const tabed_body_cfg& c, const tabed_cache_q8& cache, int rows);
+hipError_t launch_body_q8_init(const tabed_body_cfg& c, const tabed_cache_q8& cache, int rows, char* ws, hipStream_t s);
+hipError_t launch_body_step_q8(const tabed_body_cfg& c, const tabed_body_weights& w, char* ws, int rows, const int32_t* token_src,
+                               int token_stride, int rows_per_token, int32_t* ctx_len, const tabed_cache_q8& cache, uint16_t* H,
+                               int8_t* H8, float* h_scale, hipStream_t s);
+// The LM head in 8 bits: logits and softmax partials as launch_lmhead leaves them.
+hipError_t launch_lmhead_q8(const tabed_cfg& c, const WsLayout& L, char* ws, const int8_t* W, const float* w_scale, const int8_t* H,
+                            const float* h_scale, const float* temperature, float* logits, hipStream_t s);
 
 // ---------------------------------------------------------------- event timing
 // While timing is enabled a launch goes through hipExtLaunchKernelGGL, which attaches a start and a stop

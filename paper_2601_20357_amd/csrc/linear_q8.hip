@@ -589,4 +589,12 @@ hipError_t launch_linear_q8(int M, int N, int K, const int8_t* X, int64_t ldx, c
     return y_dtype == 1 ? launch_product<kOutB16>(&prof, a, s) : launch_product<kOutF32>(&prof, a, s);
 }
 
+hipError_t launch_lmhead_q8(const tabed_cfg& c, const WsLayout& L, char* ws, const int8_t* W, const float* w_scale, const int8_t* H,
+                            const float* h_scale, const float* temperature, float* logits, hipStream_t s) {
+    const LinearArgs a{L.M, c.V, c.d, H, (uint32_t)c.d, h_scale, W, w_scale, logits, c.V, c.n, temperature,
+                       reinterpret_cast<float*>(ws + L.off_pm), reinterpret_cast<float*>(ws + L.off_ps)};
+    ProfScope prof(TABED_K_LMHEAD, s);
+    return launch_product<kOutHead>(&prof, a, s);
+}
+
 }  // namespace tabed

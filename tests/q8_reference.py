@@ -128,3 +128,36 @@ def attention(pools, scales, table, q, ctx, n_new, scale, hd):
                     lost = seen.sum() * 2.0 ** -31 / p.sum() * np.abs(v[seen]).max(0)
                     bound[r, t, i] = ((2 * e + 2 * (len(held) + 220) + 3) * u * w + lost).max()
     return out, lse, bound
+
+
+# ------------------------------------------------------------------ the draft body over the 8-bit cache
+def bf16(x):
+    return torch.from_numpy(np.ascontiguousarray(x, dtype=np.float32)).to(torch.bfloat16).double().numpy()
+
+
+def body_step(bc, w, caches, table, ctx, tokens):
+    """One step for all rows in 64 bits with the kernels' storage points: bf16 for weights and whatever feeds a projection or the cache, int8
+    for the cache (caches[l] = ({"k", "v"} bytes, {"k", "v"} scales), changed in place).  Returns the final norm's rows, not rounded."""
+    rows, d, hd = len(ctx), bc.d, bc.d // bc.heads
+    f = lambda bits: (bits.astype(np.uint32) << 16).view(np.float32).astype(np.float64)
+    norm = lambda x, g: x / np.sqrt((x * x).mean(1, keepdims=True) + bc.rms_eps) * g
+    x = f(w["embed"])[np.asarray(tokens)]
+    freq = bc.rope_theta ** (-2.0 * np.arange(hd // 2) / hd)
+    cos, sin = (fn(np.asarray(ctx)[:, None] * freq)[:, None, :] for fn in (np.cos, np.sin))
+
+    def rotate(y):
+        a, b = y[..., :hd // 2], y[..., hd // 2:]
+        return np.concatenate([a * cos - b * sin, b * cos + a * sin], -1)
+
+    for l in range(bc.layers):
+        qkv = (bf16(norm(x, w["g_attn"][l])) @ f(w["wqkv"][l]).T).reshape(rows, 3, bc.heads, hd)
+        q, k, v = rotate(qkv[:, 0]), bf16(rotate(qkv[:, 1])), bf16(qkv[:, 2])
+        pools, scales = caches[l]
+        for n, new in (("k", k), ("v", v)):
+            append(pools[n], scales[n], table, n, new[:, None].astype(np.float32), ctx, None, hd)
+        att, _, _ = attention(pools, scales, table, q[:, None], ctx, None, hd ** -0.5, hd)
+        x = x + bf16(att[:, 0].reshape(rows, d)) @ f(w["wo"][l]).T
+        gu = bf16(norm(x, w["g_mlp"][l])) @ f(w["wgu"][l]).T
+        gate, up = gu[:, :bc.d_ff], gu[:, bc.d_ff:]
+        x = x + bf16(gate / (1 + np.exp(-gate)) * up) @ f(w["wdown"][l]).T
+    return norm(x, w["g_final"])

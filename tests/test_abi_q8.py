@@ -122,3 +122,67 @@ def test_binding_refuses_what_does_not_fit():
                 torch.zeros(2, 2, 256)):
         with pytest.raises(binding.TabedError):
             view(bad, 3, 2, 4, 64, "q")
+
+
+STEP = "cfg ws round pos W wsc H hsc weights temp u logits lse tokens q flags stream".split()
+
+
+def step_ok(**kw):
+    cfg = dict(V=32000, d=768, n=4, B=16, gamma=5, h=8, w_dtype=1)
+    cfg.update(kw)
+    return dict({n: P for n in STEP}, cfg=C.byref(binding.make_cfg(**cfg)), round=0, pos=0, u=None, stream=None)
+
+
+def test_draft_step_q8_refuses(lib):
+    fn = lib.tabed_draft_step_q8
+    for name in STEP:
+        if name not in ("cfg", "round", "pos", "u", "stream"):
+            assert call(fn, STEP, step_ok(), **{name: None}) == ENULL, name
+    assert call(fn, STEP, step_ok(), cfg=None) == ENULL
+    assert call(fn, STEP, step_ok(), pos=5) == ERANGE and call(fn, STEP, step_ok(), pos=-1) == ERANGE
+    assert call(fn, STEP, step_ok(d=776)) == EINVAL
+    assert call(fn, STEP, step_ok(d=131072)) == ERANGE
+    assert call(fn, STEP, step_ok(V=262144, B=65535, n=16)) == ERANGE
+    assert call(fn, STEP, step_ok(n=17)) == ERANGE
+    for name in ("ws", "W", "H", "logits", "lse"):
+        assert call(fn, STEP, step_ok(), **{name: C.c_void_p(0x1008)}) == EALIGN, name
+    for name in ("wsc", "hsc"):
+        assert call(fn, STEP, step_ok(), **{name: ODD}) == EALIGN, name
+
+
+BODY = "cfg weights ws rows src stride per ctx cache H H8 hs stream".split()
+
+
+def body_ok(cache_kw=None, **kw):
+    cfg = dict(layers=2, d=128, heads=2, d_ff=256, V=1000, max_ctx=320)
+    cfg.update(kw)
+    w = binding.TabedBodyWeights()
+    w.embed = w.g_final = 0x1000
+    for l in range(2):
+        for key in ("g_attn", "wqkv", "wo", "g_mlp", "wgu", "wdown"):
+            getattr(w, key)[l] = 0x1000
+    return dict(cfg=C.byref(binding.make_body_cfg(**cfg)), weights=C.byref(w), ws=P, rows=3, src=P, stride=1, per=1, ctx=P, cache=cache(**(cache_kw or {})),
+                H=P, H8=P, hs=P, stream=None)
+
+
+def test_body_step_q8_refuses(lib):
+    fn = lib.tabed_draft_body_step_q8
+    for name in ("cfg", "weights", "ws", "src", "ctx", "cache"):
+        assert call(fn, BODY, body_ok(), **{name: None}) == ENULL, name
+    assert call(fn, BODY, body_ok(), H=None, H8=None, hs=None) == ENULL
+    assert call(fn, BODY, body_ok(), hs=None) == ENULL and call(fn, BODY, body_ok(), H8=None) == ENULL
+    assert call(fn, BODY, body_ok(), rows=0) == ERANGE and call(fn, BODY, body_ok(), per=0) == ERANGE and call(fn, BODY, body_ok(), stride=-1) == ERANGE
+    assert call(fn, BODY, body_ok(layers=17)) == ERANGE
+    assert call(fn, BODY, body_ok(max_ctx=321)) == EINVAL                     # five blocks hold 320 tokens
+    for bad in (dict(kv_heads=1), dict(head_dim=128)):
+        assert call(fn, BODY, body_ok(bad)) == EINVAL
+        assert lib.tabed_body_q8_workspace_bytes(body_ok()["cfg"], cache(**bad), 3) == 0
+    assert call(fn, BODY, body_ok(dict(head_dim=16), heads=8)) == EINVAL       # heads of 16: no such cache
+    assert call(fn, BODY, body_ok(dict(kscale=None))) == ENULL
+    for name in ("ws", "H", "H8"):
+        assert call(fn, BODY, body_ok(), **{name: C.c_void_p(0x1008)}) == EALIGN, name
+    assert call(fn, BODY, body_ok(), hs=ODD) == EALIGN
+    assert lib.tabed_body_q8_workspace_bytes(body_ok()["cfg"], cache(k=None), 3) > 0
+    assert lib.tabed_body_q8_workspace_init(body_ok()["cfg"], cache(), 3, None, None) == ENULL
+    assert lib.tabed_body_q8_workspace_init(body_ok()["cfg"], cache(), 3, C.c_void_p(0x1008), None) == EALIGN
+    assert lib.tabed_body_q8_workspace_init(body_ok()["cfg"], cache(kv_heads=1), 3, P, None) == EINVAL
