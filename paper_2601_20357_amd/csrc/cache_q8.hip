@@ -356,13 +356,13 @@ __device__ __forceinline__ f16x8 halves_of(int lo, int hi) {
     }
     return __builtin_bit_cast(f16x8, r);
 }
-// x as the sum of two halves.
-__device__ __forceinline__ void split_halves(const float* x, f16x8& hi, f16x8& lo) {
+// x as the sum of two halves.  (`one` is 1 in a way that the compiler does not see: a product and a sum with a half among their operands
+// are one instruction that rounds to a half, v_fma_mixlo_f16; the sum alone takes three.)
+__device__ __forceinline__ void split_halves(const float* x, float one, f16x8& hi, f16x8& lo) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        hi[e] = (_Float16)x[e];
-        lo[e] = (_Float16)(x[e] - (float)hi[e]);
-    }
+    for (int e = 0; e < 8; ++e) hi[e] = (_Float16)x[e];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) lo[e] = (_Float16)fmaf(x[e], one, -(float)hi[e]);
 }
 __device__ __forceinline__ void publish_pair(float* p, float a, float b) {          // 8-byte aligned
     publish_store(reinterpret_cast<double*>(p), __builtin_bit_cast(double, make_float2(a, b)));
@@ -401,8 +401,10 @@ __device__ __forceinline__ uint32_t bytes_of(const uint32_t (&z)[4], uint32_t se
     return __builtin_amdgcn_perm(z[1], z[0], sel) | __builtin_amdgcn_perm(z[3], z[2], sel) << 16;
 }
 
+// (Two waves a SIMD: up to 256 registers, all of them vector registers.  With more at hand the products' results go through accumulation
+// registers, an instruction each to get them back.)
 template <int HD, bool WIDE, int NW>
-__global__ __launch_bounds__(NW * 64) void k_attn_q8(AttnArgs a) {
+__global__ __launch_bounds__(NW * 64, HD <= 128 ? 2 : 1) void k_attn_q8(AttnArgs a) {
     constexpr int NQ = attn_queries(WIDE), KS = (HD + 63) / 64, H16 = HD / 16, OT = HD / 16, DG = WIDE ? 3 : 1;
     constexpr int RD = !WIDE ? HD : (HD % 64 == 0 ? 64 : 32);          // dims that meet in LDS at a time
     __shared__ __attribute__((aligned(16))) float s_o[NW][NQ][RD + 4];
@@ -460,6 +462,8 @@ __global__ __launch_bounds__(NW * 64) void k_attn_q8(AttnArgs a) {
     for (int ot = 0; ot < OT; ++ot) o[ot] = f32x4v{0.f, 0.f, 0.f, 0.f};
     const uint32_t sel = attn_byte(dig);
     const uint32_t flip = dig == 3 ? 0u : 0x80808080u;
+    float one = 1.f;
+    asm("" : "+s"(one));
 
     i32x4 kf[4][KS], vf[OT];                                           // the block that is on its way
     // Requests are never predicated, so that their number in flight is known: where there is no further block (mask 0 instead of ~0) all lanes
@@ -611,7 +615,7 @@ __global__ __launch_bounds__(NW * 64) void k_attn_q8(AttnArgs a) {
         } else {
             f16x8 ph[2], pl[2];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) split_halves(&p[8 * u], ph[u], pl[u]);
+            for (int u = 0; u < 2; ++u) split_halves(&p[8 * u], one, ph[u], pl[u]);
             constexpr int kSide = OT < 4 ? OT : (OT % 4 == 0 ? 4 : 2);  // accumulators side by side: a chain of four products each
 #pragma unroll
             for (int o0 = 0; o0 < OT; o0 += kSide) {
@@ -736,16 +740,18 @@ __global__ __launch_bounds__(NW * 64) void k_attn_q8(AttnArgs a) {
     if (tid == 0) s_last = arrive(a.arrivals + unit, (uint32_t)ranges);
     __syncthreads();
     if (!s_last) return;
-    // Everything that is read is requested at once: a wave has the maxima and sums of its queries, a lane for every range, a thread the
-    // sums of two dims, kFly ranges at a time.
-    constexpr int kFly = 16, kPairs = NQ * HD / 2;
+    // Everything that is read is requested at once: a wave has the maxima and sums of its queries, a lane for every range, a thread kE
+    // pairs of dims, kFly ranges at a time.
+    constexpr int kPairs = NQ * HD / 2, kE = (kPairs + NW * 64 - 1) / (NW * 64), kFly = 16 / kE;
     const float* const unit_po = a.po + unit * a.S * (NQ * HD);
-    float2 x[kFly];
-    auto fetch = [&](int e, int u0) {
+    float2 x[kFly][kE];
+    auto fetch = [&](int u0) {
 #pragma unroll
-        for (int u = 0; u < kFly; ++u) x[u] = published_pair(unit_po + min(u0 + u, ranges - 1) * (NQ * HD) + 2 * e);
+        for (int u = 0; u < kFly; ++u)
+#pragma unroll
+            for (int i = 0; i < kE; ++i) x[u][i] = published_pair(unit_po + min(u0 + u, ranges - 1) * (NQ * HD) + 2 * min(i * NW * 64 + tid, kPairs - 1));
     };
-    if (tid < kPairs) fetch(tid, 0);
+    fetch(0);
     static_assert(kMaxRanges == 64, "a lane each");
     for (int q = wave; q < NQ; q += NW) {
         const float* const ml = unit_ml + min(lane, ranges - 1) * (2 * NQ) + q;
@@ -758,19 +764,26 @@ __global__ __launch_bounds__(NW * 64) void k_attn_q8(AttnArgs a) {
         }
     }
     __syncthreads();
-    for (int e = tid; e < kPairs; e += NW * 64) {
-        const int q = e / (HD / 2), dim = e % (HD / 2) * 2;
-        float v0 = 0.f, v1 = 0.f;
-        for (int u0 = 0; u0 < ranges; u0 += kFly) {
-            if (e != tid || u0 > 0) fetch(e, u0);
+    float2 v[kE];
 #pragma unroll
-            for (int u = 0; u < kFly; ++u) {                
-                const float f = s_f[min(u0 + u, ranges - 1)][q];
-                v0 += u0 + u < ranges ? x[u].x * f : 0.f;
-                v1 += u0 + u < ranges ? x[u].y * f : 0.f;
+    for (int i = 0; i < kE; ++i) v[i] = make_float2(0.f, 0.f);
+    for (int u0 = 0; u0 < ranges; u0 += kFly) {
+        if (u0 > 0) fetch(u0);
+#pragma unroll
+        for (int u = 0; u < kFly; ++u) {
+            if (u0 + u >= ranges) break;
+#pragma unroll
+            for (int i = 0; i < kE; ++i) {
+                const float f = s_f[u0 + u][min(i * NW * 64 + tid, kPairs - 1) / (HD / 2)];
+                v[i].x += x[u][i].x * f;
+                v[i].y += x[u][i].y * f;
             }
         }
-        finish(q, dim, v0, v1);
+    }
+#pragma unroll
+    for (int i = 0; i < kE; ++i) {
+        const int e = i * NW * 64 + tid;
+        if (e < kPairs) finish(e / (HD / 2), e % (HD / 2) * 2, v[i].x, v[i].y);
     }
 }
 
