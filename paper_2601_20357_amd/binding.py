@@ -526,7 +526,7 @@ def _matrix(t, rows, cols, name, dtype=None):
         raise TabedError(f"{name} must be {dtype}, got {t.dtype}")
     if t.shape[1] > 1 and t.stride(1) != 1:
         raise TabedError(f"{name}: the values of a row must lie side by side")
-    stride = t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
+    stride = t.stride(0) if t.shape[0] > 1 else t.shape[1]
     if stride < t.shape[1]:
         raise TabedError(f"{name}: rows overlap")
     return t.data_ptr(), stride

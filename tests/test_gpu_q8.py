@@ -142,6 +142,30 @@ def test_linear_q8_longest_sums_and_larger_sizes(M, N, K):
     check_linear(linear_case(x, sx, w, sw, F32), x, sx, w, sw, F32)
 
 
+@pytest.mark.parametrize("M,N,K", [(3, 70001, 4112), (40, 40001, 1040), (17, 66000, 2064), (64, 33000, 2048)])
+def test_linear_q8_workgroups_that_go_on(M, N, K):
+    """More columns than the workgroups take at once, with X in one chunk and in several."""
+    g = torch.Generator(device=DEV).manual_seed(N)
+    x, w = (torch.randint(-127, 128, s, generator=g, dtype=torch.int8, device=DEV) for s in ((M, K), (N, K)))
+    sx, sw = torch.ones(M, device=DEV), torch.ones(N, device=DEV)
+    y = torch.empty((M, N), device=DEV)
+    binding.tabed_linear_q8(x, sx, w, sw, y)
+    want = x.double() @ w.double().t()
+    assert torch.equal(y, want.float())                            # one rounding of an exact integer
+
+
+def test_linear_q8_outputs_past_four_gigabytes():
+    M, N, K = 70, 2 ** 24, 16
+    w = torch.ones((N, K), dtype=torch.int8, device=DEV)
+    w[-3:] = torch.tensor([[2], [-3], [4]], dtype=torch.int8, device=DEV)
+    x = torch.ones((M, K), dtype=torch.int8, device=DEV)
+    x[-1] = 5
+    y = torch.zeros((M, N), device=DEV)
+    binding.tabed_linear_q8(x, torch.ones(M, device=DEV), w, torch.ones(N, device=DEV), y)
+    assert (y[:-1, :-3] == 16).all() and (y[-1, :-3] == 80).all()
+    assert y[0, -3:].tolist() == [32, -48, 64] and y[-1, -3:].tolist() == [160, -240, 320]
+
+
 def test_linear_q8_bad_rows_stay_their_own():
     g = gen(3)
     x, w = (torch.randint(-127, 128, s, generator=g, dtype=torch.int8) for s in ((9, 64), (70, 64)))
@@ -360,6 +384,68 @@ def test_attention_is_the_same_every_time_and_in_place_of_strided_views():
     torch.cuda.synchronize()
     assert torch.equal(res[:, :, 9:265].cpu().reshape(5, 2, 4, 64), first)
     assert (res[:, :, :9] == 55).all() and (res[:, :, 265:] == 55).all()
+
+
+@pytest.mark.parametrize("T", [1, 5])
+def test_attention_at_any_alignment_of_the_values(T):
+    """bf16 queries and outputs that begin at odd addresses of two bytes, tokens 2 bytes past a multiple of 16 apart."""
+    c = Cache(4, 6, 2, 96, seed=20)
+    q = randn(gen(21), 4, T, 6, 96, dtype=BF16)
+    ctx = [300, 5, 64, 200]
+    wide_q, wide_o = (torch.full((4, T, 6 * 96 + 9), 55.0, dtype=BF16, device=DEV) for _ in range(2))
+    wide_q[:, :, 3:3 + 576] = q.reshape(4, T, 576).to(DEV)
+    ws = binding.new_attention_workspace(c.gpu, 4, T, 6)
+    binding.tabed_attention_q8(c.gpu, ws, wide_q[:, :, 3:579], torch.tensor(ctx, dtype=torch.int32, device=DEV), wide_o[:, :, 1:577])
+    torch.cuda.synchronize()
+    assert (wide_o[:, :, 0] == 55).all() and (wide_o[:, :, 577:] == 55).all()
+    out, _ = attend(c, q, ctx, out_type=BF16, ws=ws)
+    assert torch.equal(wide_o[:, :, 1:577].cpu().reshape(4, T, 6, 96), out)
+    check_attention(c, q, ctx, None, out, None)
+
+
+def test_cache_past_four_gigabytes():
+    """Blocks behind the first 2^32 bytes of the pool: appended to and read."""
+    kvh, hd, blocks = 8, 128, 66000
+    k, v = (torch.empty((blocks, kvh, 64 * hd), dtype=torch.int8, device=DEV) for _ in range(2))
+    ks, vs = (torch.empty((blocks, kvh), device=DEV) for _ in range(2))
+    table = torch.tensor([[blocks - 1, 3], [65999 - 40, 65600]], dtype=torch.int32, device=DEV)
+    big = binding.CacheQ8(k, v, ks, vs, table, hd)
+    small = binding.CacheQ8.allocate(2, 128, kvh, hd)
+    g = gen(22)
+    x, y, q = (randn(g, 2, 100, kvh, hd, dtype=BF16).to(DEV) for _ in range(3))
+    outs = []
+    for cache in (big, small):
+        ctx = torch.zeros(2, dtype=torch.int32, device=DEV)
+        binding.tabed_cache_append_q8(cache, x, y, ctx)
+        out = torch.zeros((2, 100, kvh, hd), device=DEV)
+        binding.tabed_attention_q8(cache, binding.new_attention_workspace(cache, 2, 100, kvh), q, ctx, out)
+        outs.append(out)
+    assert torch.equal(*outs) and (outs[0][:, 0] != 0).any()
+    for name, pool in (("k", k), ("v", v)):                         # the tokens' bytes (what lies behind the 100th is nobody's)
+        where = torch.from_numpy(ref.layout(name, hd)).to(DEV)
+        at = [p[:, :, where].transpose(1, 2).reshape(2, 128, kvh, hd)[:, :100] for p in (pool[table.flatten().tolist()], getattr(small, name))]
+        assert torch.equal(*at)
+
+
+def test_two_streams_at_once():
+    """Calls with workspaces of their own on two streams, running side by side."""
+    c = Cache(4, 60, 2, 64, seed=23)
+    q = [randn(gen(24 + i), 4, 1, 4, 64).to(DEV) for i in range(2)]
+    ctx = torch.tensor([3000, 64, 3500, 1000], dtype=torch.int32, device=DEV)
+    ws = [binding.new_attention_workspace(c.gpu, 4, 1, 4) for _ in range(2)]
+    alone = []
+    for i in range(2):
+        out = torch.zeros((4, 1, 4, 64), device=DEV)
+        binding.tabed_attention_q8(c.gpu, ws[i], q[i], ctx, out)
+        alone.append(out)
+    torch.cuda.synchronize()
+    streams, outs = [torch.cuda.Stream() for _ in range(2)], [torch.zeros((4, 1, 4, 64), device=DEV) for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for i in range(2):
+            binding.tabed_attention_q8(c.gpu, ws[i], q[i], ctx, outs[i], stream=streams[i])
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], alone[0]) and torch.equal(outs[1], alone[1])
 
 
 def test_attention_reads_shared_blocks():
