@@ -467,17 +467,19 @@ CACHE_BLOCK = 64
 class DeviceCall(PreparedCall):
     """A PreparedCall that makes its tensors' device current and keeps the tensors (and its HOST structs) alive."""
 
-    __slots__ = ("device", "keep")
+    __slots__ = ("device", "keep", "current")
 
     def __init__(self, fn, args, what, device, keep):
-        super().__init__(fn, args, what)
-        self.device, self.keep = device, keep
+        import torch
+        simple = (int, float, type(None))                  # converted now, not at every call
+        super().__init__(fn, [t(a) if isinstance(a, simple) else a for t, a in zip(fn.argtypes, args)], what)
+        self.device, self.keep, self.current = device, keep, torch.cuda.current_device
 
     def __call__(self):
-        import torch
-        if torch.cuda.current_device() == self.device:
+        if self.current() == self.device:
             rc = self.fn(*self.args)
         else:
+            import torch
             with torch.cuda.device(self.device):
                 rc = self.fn(*self.args)
         if rc != 0:
