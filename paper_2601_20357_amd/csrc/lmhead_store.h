@@ -215,7 +215,7 @@ __device__ __forceinline__ void store_full_tiles(const f32x16 (&acc)[TV][TM], in
 }
 
 // ---------------------------------------------------------------- loads straight to LDS
-// Four (two) loads of 64 lanes x 16 bytes, from base + the lane's offset to LDS at `lds`, `step` further for each: lane l's bytes land at
+// Four (two, one) loads of 64 lanes x 16 bytes, from base + the lane's offset to LDS at `lds`, `step` further for each: lane l's bytes land at
 // l * 16.  In assembly, since they have no destination register: with the builtin the compiler waits for LDS reads in flight.
 // (M0 is put back: the compiler does not let it be named as clobbered, and keeps what it has in it.)
 __device__ __forceinline__ void dma_lines(const char* base, const uint32_t (&off)[4], uint32_t lds, uint32_t step) {
@@ -231,6 +231,11 @@ __device__ __forceinline__ void dma_lines(const char* base, const uint32_t (&off
     asm volatile("s_mov_b32 %0, m0\n\ts_nop 4\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %5\n\ts_add_u32 m0, m0, %2\n\t"
                  "s_nop 0\n\tglobal_load_lds_dwordx4 %4, %5\n\ts_mov_b32 m0, %0"
                  : "=&s"(m0) : "s"(lds), "s"(step), "v"(off[0]), "v"(off[1]), "s"(base) : "memory", "scc");
+}
+__device__ __forceinline__ void dma_lines(const char* base, const uint32_t (&off)[1], uint32_t lds, uint32_t) {
+    uint32_t m0;
+    asm volatile("s_mov_b32 %0, m0\n\ts_nop 4\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %0"
+                 : "=&s"(m0) : "s"(lds), "v"(off[0]), "s"(base) : "memory", "scc");
 }
 
 }  // namespace tabed

@@ -154,6 +154,21 @@ def test_linear_q8_workgroups_that_go_on(M, N, K):
     assert torch.equal(y, want.float())                            # one rounding of an exact integer
 
 
+@pytest.mark.parametrize("M,N,K", [(5, 90, 1008), (40, 100, 1040), (33, 65, 3088), (70, 129, 2032), (1, 8200, 16), (16, 8200, 528), (30, 8200, 1008),
+                                   (40, 9000, 16), (50, 9000, 240), (64, 8200, 528), (33, 17000, 16), (64, 17000, 784), (7, 17000, 4112),
+                                   (130, 8000, 16), (129, 8010, 400), (190, 6000, 128)])
+def test_linear_q8_ends_of_k_in_small_tiles(M, N, K):
+    """K that ends in each part of a block that several waves share, for every number of them."""
+    g = torch.Generator(device=DEV).manual_seed(K)
+    x, w = (torch.randint(-128, 128, s, generator=g, dtype=torch.int8, device=DEV) for s in ((M, K), (N, K)))
+    wide = torch.full((M, K + 16), 99, dtype=torch.int8, device=DEV)                     # what lies behind a row is not taken
+    wide[:, :K] = x
+    y = torch.full((M + 1, N + 3), 7.0, device=DEV)
+    binding.tabed_linear_q8(wide[:, :K], torch.ones(M, device=DEV), w, torch.ones(N, device=DEV), y[:M, :N])
+    want = x.double() @ w.double().t()
+    assert torch.equal(y[:M, :N], want.float()) and (y[M] == 7).all() and (y[:, N:] == 7).all()
+
+
 def test_linear_q8_outputs_past_four_gigabytes():
     M, N, K = 70, 2 ** 24, 16
     w = torch.ones((N, K), dtype=torch.int8, device=DEV)

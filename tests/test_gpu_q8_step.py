@@ -16,7 +16,7 @@ def bits(a):
 
 # ------------------------------------------------------------------ LM head and sampler
 @pytest.mark.parametrize("n,B,V,d", [(4, 1, 5000, 768), (3, 8, 4099, 80), (4, 16, 32000, 768), (5, 12, 1023, 2064), (4, 16, 777, 16), (8, 16, 9000, 512),
-                                     (2, 33, 6400, 144), (8, 64, 12288, 256), (4, 40, 50261, 1040), (16, 33, 2049, 768)])
+                                     (2, 33, 6400, 144), (8, 64, 12288, 256), (4, 40, 50261, 1040), (16, 33, 2049, 768), (2, 16, 17000, 4112), (1, 3, 8200, 1008)])
 def test_draft_step_q8_is_the_bf16_step_where_that_is_exact(n, B, V, d):
     """Small integers times powers of two are exact in bf16, and so are their products' sums in fp32: both steps then have the same logits
     bit for bit, and tokens that differ only where a decision is flagged."""
