@@ -39,7 +39,8 @@ constexpr int kLinearThreads = 512;
 // again and again; small tiles have too little to split, and there KW > 1 makes a k-block long and the barriers few (32 x 64, K = 4096:
 // 9.1 us with KW = 4 for 8192 columns, 64 x 128 with KW = 1 takes 14.3).  The KW integer sums of a block meet in LDS.
 // Operands go from memory straight to LDS in SW stages of W and SH of X; a stage has lines of 128 bytes, row r with its
-// 16-byte pieces in the order piece ^ (r % 8), which the lanes bring about by the address they load from.  One barrier per k-block, before the
+// 16-byte pieces in the order piece ^ (r / 2 % 8), which the lanes bring about by the address they load from: 16 rows' pieces lie in 64 different
+// banks (with r % 8 two of them share theirs, and a read of fragments takes 8 cycles instead of 4).  One barrier per k-block, before the
 // products of its last k-step: the next k-block's first fragments are read while those run.  Workgroups are numbered so that the row
 // blocks that share a column block run back to back on one XCD (workgroup w goes to XCD w % 8): W comes from memory once.
 // K past the last whole k-block: loads re-read its last 16 bytes, and X's fragments are zeroed there.
@@ -63,7 +64,7 @@ __global__ __launch_bounds__(kLinearThreads, 2) void k_linear_tile(LinearArgs a,
     const char* const wbase = reinterpret_cast<const char*>(a.W) + (size_t)n0 * K;
     const char* const xbase = reinterpret_cast<const char*>(a.X) + (size_t)m0 * a.ldx;
     // Load i of a wave: lines (i * 8 + wave) * 8 .. + 8 of a stage, which holds KW times 128 bytes of every row, one after the other.
-    const int line0 = wave * 8 + (lane >> 3), piece = (lane & 7) ^ (lane >> 3);
+    const int line0 = wave * 8 + (lane >> 3), piece = (lane & 7) ^ (line0 >> 1 & 7);
     uint32_t wo[WI], xo[XI];                                          // rows past the end re-read the last one
 #pragma unroll
     for (int i = 0; i < WI; ++i) wo[i] = (uint32_t)min((i * 64 + line0) % BN, N - 1 - n0) * (uint32_t)K + (i * 64 + line0) / BN * kLine + piece * 16;
@@ -91,7 +92,7 @@ __global__ __launch_bounds__(kLinearThreads, 2) void k_linear_tile(LinearArgs a,
         for (int b = 0; b < TM; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r) acc[p][b][r] = 0;
-    const uint32_t wrow = (uint32_t)(kw * BN + wn * 32 * TV + nn) * kLine, xrow = (uint32_t)(SW * kStW) + (uint32_t)(kw * BM + wm * (BM / kRows) + nn) * kLine, turn = (uint32_t)(nn & 7);
+    const uint32_t wrow = (uint32_t)(kw * BN + wn * 32 * TV + nn) * kLine, xrow = (uint32_t)(SW * kStW) + (uint32_t)(kw * BM + wm * (BM / kRows) + nn) * kLine, turn = (uint32_t)(nn >> 1 & 7);
     i32x4 wf[2][TV], xf[2][TM];                                       // fragments of two k-steps of 32
     int stw = 0, stx = 0;
     auto read_frags = [&](int ks, int set) {
