@@ -106,10 +106,9 @@ __device__ __forceinline__ u32x4_e4 pack_steps(const int (&s)[16]) {
 __device__ __forceinline__ int key_piece(int at, int c, int chunks) { return ((at / 4 % 4) * chunks + c) * 16 + at / 16 * 4 + at % 4; }      // 16 dims of a token
 __device__ __forceinline__ int value_piece(int g, int dim) { return (dim / 16 * 4 + g) * 16 + dim % 16; }                                     // 16 tokens of a dim
 
-// Up to kFew new tokens a row: a wave a task, a lane for every 64th dim, a byte stored for each value.  Latency bounds it: positions
+// Up to FEW new tokens a row: a wave a task, a lane for every 64th dim, a byte stored for each value.  Latency bounds it: positions
 // -> page -> scale.
-constexpr int kFew = 4;
-template <bool BF16, int hd>
+template <bool BF16, int hd, int FEW>
 __global__ __launch_bounds__(kBlock) void k_cache_append_few(AppendArgs a) {
     constexpr int chunks = hd / 16, kDims = (hd + 63) / 64;           // kDims: of a lane
     AppendTask t;
@@ -119,10 +118,10 @@ __global__ __launch_bounds__(kBlock) void k_cache_append_few(AppendArgs a) {
     float* const scale_at = (t.values ? a.c.vscale : a.c.kscale) + t.ph;
     const float before = t.off > 0 ? *scale_at : 0.f;
     const void* const src = t.values ? a.v : a.k;
-    float x[kFew][kDims];
+    float x[FEW][kDims];
     uint32_t most = 0;
 #pragma unroll
-    for (int n = 0; n < kFew; ++n)
+    for (int n = 0; n < FEW; ++n)
 #pragma unroll
         for (int i = 0; i < kDims; ++i) {
             const int dim = i * 64 + lane;
@@ -146,7 +145,7 @@ __global__ __launch_bounds__(kBlock) void k_cache_append_few(AppendArgs a) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");              // the new tokens' bytes, which share pieces with them, come after
     }
 #pragma unroll
-    for (int n = 0; n < kFew; ++n)
+    for (int n = 0; n < FEW; ++n)
 #pragma unroll
         for (int i = 0; i < kDims; ++i) {
             const int dim = i * 64 + lane, at = t.off + n;
@@ -266,12 +265,13 @@ int64_t append_workgroups(const tabed_cache_q8& c, int rows, int T) { return 2ll
 
 template <int hd>
 static void launch_append(const ProfScope* prof, int kv_dtype, unsigned tasks, const AppendArgs& a, hipStream_t s) {
-    const bool few = a.T <= kFew;
-    const dim3 grid(few ? (tasks + kWavesPerBlock - 1) / kWavesPerBlock : tasks);
-    if (few && kv_dtype == 1) launch(prof, k_cache_append_few<true, hd>, grid, dim3(kBlock), 0, s, a);
-    else if (few) launch(prof, k_cache_append_few<false, hd>, grid, dim3(kBlock), 0, s, a);
-    else if (kv_dtype == 1) launch(prof, k_cache_append<true, hd>, grid, dim3(kBlock), 0, s, a);
-    else launch(prof, k_cache_append<false, hd>, grid, dim3(kBlock), 0, s, a);
+    // A wave's own time grows with tokens times dims, a workgroup's hardly; but four times as many workgroups start.  Six tokens of 64 rows
+    // x 8 heads: 4.8 us against 7.2 with 64 dims, 6.8 against 7.5 with 128, 11.7 against 9.8 with 256; 16 rows 4.2 - 5.3, 5.8 - 5.2, 8.6 - 5.5.
+    const unsigned quarter = (tasks + kWavesPerBlock - 1) / kWavesPerBlock;
+    auto go = [&](auto kernel, unsigned workgroups) { launch(prof, kernel, dim3(workgroups), dim3(kBlock), 0, s, a); };
+    if (a.T <= 4) kv_dtype == 1 ? go(k_cache_append_few<true, hd, 4>, quarter) : go(k_cache_append_few<false, hd, 4>, quarter);
+    else if (hd <= 64 && a.T <= 8) kv_dtype == 1 ? go(k_cache_append_few<true, std::min(hd, 64), 8>, quarter) : go(k_cache_append_few<false, std::min(hd, 64), 8>, quarter);
+    else kv_dtype == 1 ? go(k_cache_append<true, hd>, tasks) : go(k_cache_append<false, hd>, tasks);
 }
 
 hipError_t launch_cache_append(const tabed_cache_q8& c, int rows, int T, int kv_dtype, const void* k, const void* v, int64_t row_stride,

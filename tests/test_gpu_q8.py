@@ -256,6 +256,20 @@ def test_cache_append_of_ragged_rows_and_missing_blocks():
     c.same()
 
 
+@pytest.mark.parametrize("hd", [32, 64, 128])
+@pytest.mark.parametrize("T,type", [(4, BF16), (8, BF16), (8, F32), (9, BF16)])
+def test_cache_append_of_a_few_ragged_tokens(hd, T, type):
+    """Rows that end inside a block, on its last token and behind it, at sizes that grow and do not grow a scale."""
+    c = Cache(8, 3, 2, hd, seed=T)
+    c.table[7, 0] = -1
+    c.push()
+    g = gen(T + hd)
+    for size, ctx in ((0.02, [0, 56, 60, 63, 64, 127, 190, 58]), (20.0, [3, 58, 62, 64, 71, 120, 191, 61]), (1.0, [1, 57, 61, 60, 68, 126, 185, 59])):
+        n_new = [T, T - 1, T, 2, 0, T, T, T]
+        c.append(randn(g, 8, T, 2, hd) * size, randn(g, 8, T, 2, hd) * size, ctx, n_new, type=type)
+        c.same()
+
+
 def test_cache_append_of_zeros_tiny_and_not_finite():
     c = Cache(4, 2, 2, 32, seed=4)
     k = torch.zeros(4, 1, 2, 32)
