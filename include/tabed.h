@@ -374,7 +374,7 @@ int tabed_linear_q8(int32_t M, int32_t N, int32_t K, const void* X, int64_t ldx,
  *                  keys   [token / 4 % 4][dim / 16][token / 16][token % 4][dim % 16]
  *                  values [dim / 16][token / 16][dim % 16][token % 16]
  *                  (the order in which v_mfma_i32_16x16x64_i8 takes them)
- *   kscale, vscale [blocks, kv_heads] fp32
+ *   kscale, vscale [blocks, kv_heads] fp32, none below 0 (appending leaves none)
  *   table          [rows, max_blocks] int32
  * A HOST struct of device pointers; k and v 16-byte aligned.
  */

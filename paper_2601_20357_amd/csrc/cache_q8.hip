@@ -173,7 +173,8 @@ __device__ __forceinline__ void transpose_bytes(const uint32_t (&r)[4], uint32_t
 }
 
 // More: a workgroup a task, a thread for pieces of 16 dims of a token.  Keys are stored as such a piece, values go through LDS, from
-// where a thread takes 16 tokens of four dims and transposes them.  Memory bounds a prompt.
+// where a thread takes 16 tokens of four dims and transposes them.  Memory bounds a prompt: 12000 tokens x 8 heads of 128 dims in 16 rows,
+// 74 MB, 23 us, 3.2 TB/s (a workgroup asks for its tokens once, waits for its largest and stores: nothing overlaps within it).
 template <bool BF16, int hd>
 __global__ __launch_bounds__(kBlock) void k_cache_append(AppendArgs a) {
     constexpr int chunks = hd / 16, row_bytes = hd + 16, kPer = (kCB * chunks + kBlock - 1) / kBlock;      // kPer: pieces of a thread
@@ -311,6 +312,8 @@ hipError_t launch_cache_append(const tabed_cache_q8& c, int rows, int T, int kv_
 //     v_mfma_f32_16x16x32_f16, and the values' bytes become halves on the way, five vector instructions for four of them.  Digits
 //     would take half as many instructions again for the sixteen, and four times as many with the layout above.  Vector instructions
 //     bound this form from about 1000 tokens a row on: 380 a block of 128 dims, of which converting the values is 160.
+// With few queries the bytes bound it: 120000 tokens x 8 heads of 128 dims, 246 MB, take 50 us, 4.9 TB/s; 64 rows x 12 heads of 64 dims and 500
+// tokens, 50 MB, 13.6 us, of which about 4 are the launch and the chain length -> page -> keys -> values.
 // The waves of a workgroup take blocks in turn and meet in LDS; a row's blocks are cut into S ranges where the rows and heads do
 // not fill the chip, and the last of its workgroups to arrive joins them (in range order: results do not depend on who is last).
 struct AttnArgs {
@@ -794,8 +797,11 @@ __global__ __launch_bounds__(NW * 64, HD <= 128 || !WIDE ? 2 : 1) void k_attn_q8
     }
 }
 
-// How a call is cut up.  Eight waves a workgroup and ranges where units (row, head, tile of queries) are few, so that ranges are
-// joined in LDS as far as possible.
+// How a call is cut up.  Units are rows x heads x tiles of queries.  Up to 256 of them have eight waves, whose shares meet in LDS (16 rows x 8 heads of
+// 128 dims, 24 queries, 2600 tokens: 21 us, with four waves 24.4); more, or heads too large for two such waves a SIMD, have four (64 rows x 12 heads of
+// 64, 500 tokens: 13.6 us, with eight 16.0).  Rows are cut into ranges until every compute unit has a workgroup and no further: a second round
+// of workgroups and the joins cost more than evener shares give (512 instead of 256: 16 rows of 2600 tokens 29.6 us instead of 21, of 300 to 5000 tokens
+// 37 instead of 30, one row of 120000 56 instead of 50).
 struct AttnPlan {
     bool wide;
     int nw, tiles, S;

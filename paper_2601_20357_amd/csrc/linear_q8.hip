@@ -1,7 +1,7 @@
 // Products of int8 rows with int8 weights (tabed_linear_q8): Y[m][n] = (sum_k X[m][k] W[n][k]) * sx[m] * sw[n], and the LM head in
 // 8 bits, which is the same with softmax partials.  The sum is in int32 and exact for the K allowed, so the order of its terms is
 // free: waves and k-steps share it as suits the memory; one rounding for the integer, one for each scale and one for storage.
-// One kernel in tiles of nine sizes: with few rows W's bytes bound it and small tiles give every compute unit some of them, with many
+// One kernel in tiles of several sizes: with few rows W's bytes bound it and small tiles give every compute unit some of them, with many
 // the matrix cores do and tiles are as large as registers and LDS hold.
 #include <algorithm>
 #include <mutex>
@@ -41,21 +41,24 @@ constexpr int kLinearThreads = 512;
 // Operands go from memory straight to LDS in SW stages of W and SH of X; a stage has lines of 128 bytes, row r with its
 // 16-byte pieces in the order piece ^ (r / 2 % 8), which the lanes bring about by the address they load from: 16 rows' pieces lie in 64 different
 // banks (with r % 8 two of them share theirs, and a read of fragments takes 8 cycles instead of 4).  One barrier per k-block, before the
-// products of its last k-step: the next k-block's first fragments are read while those run.  Workgroups are numbered so that the row
-// blocks that share a column block run back to back on one XCD (workgroup w goes to XCD w % 8): W comes from memory once.
+// products of its last k-step: the next k-block's first fragments are read while those run.  Workgroup w goes to XCD w % 8:
+// the row blocks that share a column block run back to back on one XCD, so W comes from memory once, and all XCDs have as many tiles but for one
+// (4150 x 5659, K = 2048: 87 us; dealt out in whole column blocks to the last, 108).
+// What bounds it: few rows W's bytes (64 x 32000, K = 768: 8.2 us for 33 MB; 16 x 32000, K = 8192 53 us, 4.95 TB/s), many rows the products at the
+// clock that the power leaves (4096 x 8192, K = 8192: 247 us, 2.2 POP/s; 512 x 128256, K = 2048 with 263 MB of W and as many of results 166 us).
 // K past the last whole k-block: loads re-read its last 16 bytes, and X's fragments are zeroed there.
 template <int BM, int BN, int KW, int SW, int SH, int EPI, bool PAST>
-__global__ __launch_bounds__(kLinearThreads, 2) void k_linear_tile(LinearArgs a, int mblocks) {
+__global__ __launch_bounds__(kLinearThreads, 2) void k_linear_tile(LinearArgs a, int mblocks, int whole, int share) {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     constexpr int kStW = KW * BN * kLine, kStX = KW * BM * kLine, kRows = (BM == 32 || KW > 2) ? 1 : 2, kCols = 8 / KW / kRows;
     constexpr int TV = BN / (32 * kCols), TM = BM / (32 * kRows), WI = KW * BN / 64, XI = KW * BM / 64;
     constexpr uint32_t kNext = 8 * 8 * kLine;                         // LDS bytes from one of a wave's loads to its next
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int nn = lane & 31, half = lane >> 5;
-    const int w = blockIdx.x, xcd = w & 7, slot = w >> 3;
-    const int mb = slot % mblocks, nb = (slot / mblocks) * 8 + xcd;
+    const int xcd = blockIdx.x & 7, slot = blockIdx.x >> 3, rest = slot - whole * mblocks, at = rest < 0 ? slot : xcd * share + rest;
+    const int mb = at % mblocks, nb = rest < 0 ? at / mblocks * 8 + xcd : whole * 8 + at / mblocks;
     const int M = a.M, N = a.N, K = a.K, m0 = mb * BM, n0 = nb * BN;
-    if (n0 >= N) return;                                              // uniform: padding workgroups of the last round of XCDs
+    if (n0 >= N) return;                                              // uniform: the last XCD's share of the rest may be smaller
     const int wm = wave / kCols % kRows, wn = wave % kCols, kw = wave / (kCols * kRows);
     const float my_sx = a.sx[min(m0 + (tid & (BM - 1)), M - 1)], my_sw = a.sw[min(n0 + (tid & (BN - 1)), N - 1)];      // used after the loop
     float my_temp = 1.f;
@@ -323,8 +326,13 @@ static hipError_t launch_tile_q8(const ProfScope* prof, const LinearArgs& a, hip
     static hipError_t rc[kMaxDevices];
     const hipError_t e = raise_on_device(&k_linear_tile<BM, BN, KW, SW, SH, EPI, PAST>, lds, once, rc);
     if (e != hipSuccess) return e;
-    const int mblocks = (a.M + BM - 1) / BM, nblocks = (a.N + BN - 1) / BN, nrounds = (nblocks + 7) / 8;
-    launch(prof, k_linear_tile<BM, BN, KW, SW, SH, EPI, PAST>, dim3(nrounds * mblocks * 8), dim3(kLinearThreads), lds, s, a, mblocks);
+    // Column blocks are dealt out one by one, what is left of the last round of them tile by tile.  Where rows of Y do not begin on 64 bytes neighbouring
+    // column blocks write parts of the same ones, and many rows' tiles are dealt out in eight runs instead, so that both are in one L2
+    // (2000 x 9000, K = 2048: 56.3 us against 61; 1000 x 50000, K = 512: 55.7, 64.4; but 2000 x 20000, K = 512 45.9, 43.8, and 16 x 32000, K = 4096 30.3, 28.6).
+    const int mblocks = (a.M + BM - 1) / BM, nblocks = (a.N + BN - 1) / BN;
+    const bool runs = a.M > 64 && a.ldy * (EPI == kOutB16 ? 2 : 4) % 64 != 0;
+    const int whole = runs ? 0 : nblocks / 8, share = (int)(((int64_t)(nblocks - 8 * whole) * mblocks + 7) / 8);
+    launch(prof, k_linear_tile<BM, BN, KW, SW, SH, EPI, PAST>, dim3((whole * mblocks + share) * 8), dim3(kLinearThreads), lds, s, a, mblocks, whole, share);
     return hipGetLastError();
 }
 
@@ -340,12 +348,17 @@ static hipError_t launch_tiles(const ProfScope* prof, const LinearArgs& a, hipSt
     if (tiles(32, 64) <= 256 || (a.M <= 32 && a.K >= 4096)) return launch_tile_q8<32, 64, 4, 3, 3, EPI, PAST>(prof, a, s);
     if (tiles(64, 64) <= 256) return launch_tile_q8<64, 64, 2, 3, 3, EPI, PAST>(prof, a, s);
     if (a.M <= 64) return launch_tile_q8<64, 64, 2, 2, 2, EPI, PAST>(prof, a, s);
-    if (tiles(64, 128) <= 256) return launch_tile_q8<64, 128, 1, 3, 3, EPI, PAST>(prof, a, s);
-    // Large tiles as long as nearly every compute unit gets one, or several; a second workgroup on a compute unit where 128 x 128 leaves more than one each.
-    if (a.M > 128 && (tiles(256, 256) >= 192 || tiles(128, 256) > 256)) return launch_tile_q8<256, 256, 1, 3, 2, EPI, PAST>(prof, a, s);
-    if (tiles(128, 256) >= 192) return launch_tile_q8<128, 256, 1, 3, 3, EPI, PAST>(prof, a, s);
-    if (tiles(128, 128) > 256) return launch_tile_q8<128, 128, 1, 2, 2, EPI, PAST>(prof, a, s);
-    return launch_tile_q8<128, 128, 1, 4, 4, EPI, PAST>(prof, a, s);
+    // Many tiles: time goes in rounds of as many workgroups as fit the chip, and a round's length with the tile (K = 4096: 57 us in 256 x 256, 36 in
+    // 128 x 256, 22 in 128 x 128, 18 in 64 x 128, or 29 where that has two workgroups a compute unit; K = 512: 15.7, 9.6, 5.8, 4.9, 7.9).  Taken is
+    // the least product of the two: 160 x 20000, K = 4096 30.5 us in 64 x 128, 32.7 in 128 x 256; 520 x 50000 144 in 128 x 256, 168 in
+    // 256 x 256; 1000 x 9000 53 in 256 x 256, 65 in 128 x 256; 520 x 4000 18.8 in 128 x 128, 20.9 in 64 x 128.
+    auto cost = [&](int bm, int bn, int length, int at_once) { return (tiles(bm, bn) + at_once - 1) / at_once * length; };
+    const long large = cost(256, 256, 16, 256), wide = cost(128, 256, 10, 256), mid = cost(128, 128, 6, 256);
+    const long narrow = std::min(cost(64, 128, 5, 256), cost(64, 128, 8, 512));
+    if (large <= std::min({wide, mid, narrow})) return launch_tile_q8<256, 256, 1, 3, 2, EPI, PAST>(prof, a, s);
+    if (wide <= std::min(mid, narrow)) return launch_tile_q8<128, 256, 1, 3, 3, EPI, PAST>(prof, a, s);
+    if (mid <= narrow) return launch_tile_q8<128, 128, 1, 4, 4, EPI, PAST>(prof, a, s);
+    return launch_tile_q8<64, 128, 1, 3, 3, EPI, PAST>(prof, a, s);
 }
 
 template <int EPI>

@@ -29,7 +29,9 @@ typedef uint32_t u32x2_e1 __attribute__((ext_vector_type(2), aligned(1)));
 enum { kF32 = 0, kB16 = 1, kNone = 2 };
 
 // TPR threads of a row, P pieces of 8 values each, as few as hold the row: 8192 rows of 4096 in bf16 with their deltas, 235 MB, took 58 us
-// with room for four pieces, 46 with the two that there are, which is what a copy of as many bytes takes.
+// with room for four pieces, 46 with the two that there are, which is what a copy of as many bytes takes.  Few rows are bound by latency: x, two
+// reductions, stores (4 rows of 768: 3.2 us, 1.5 of them between any two kernels; 333 rows of 2051: 4.8).  A wave a row needs no barrier, up to 2048
+// values; longer rows have more threads so that a row's registers stay few.
 template <int TPR, int P, int X, int D>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_q8(NormArgs a) {
     constexpr int kWaves = TPR / 64;
@@ -155,7 +157,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_q8(NormArgs a) {
 
 template <int TPR, int P>
 static void launch_norm_t(const ProfScope* prof, int xt, int dt, const NormArgs& a, hipStream_t s) {
-    const int per = (TPR == 64 && a.rows >= 1024) ? 4 : 1;             // rows of a workgroup, a wave each
+    constexpr int per = (TPR == 64) ? 4 : 1;                           // rows of a workgroup, a wave each
     const dim3 grid((a.rows + per - 1) / per), block(TPR * per);
     auto go = [&](auto kernel) { launch(prof, kernel, grid, block, 0, s, a); };
     if (xt == kF32) {
