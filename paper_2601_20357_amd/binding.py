@@ -471,6 +471,9 @@ class DeviceCall(PreparedCall):
 
     def __init__(self, fn, args, what, device, keep):
         import torch
+        for t, a in zip(fn.argtypes, args):
+            if t is C.c_int32 and isinstance(a, int) and not -1 << 31 <= a < 1 << 31:
+                raise TabedError(f"{what}: a size of {a} does not fit 32 bits")
         simple = (int, float, type(None))                  # converted now, not at every call
         super().__init__(fn, [t(a) if isinstance(a, simple) else a for t, a in zip(fn.argtypes, args)], what)
         self.device, self.keep, self.current = device, keep, torch.cuda.current_device
@@ -594,6 +597,8 @@ class CacheQ8:
         if table.dim() != 2:
             raise TabedError("table must be [rows, max_blocks]")
         blocks, kvh = k.shape[-3:-1]
+        if max(blocks, kvh, table.shape[0], table.shape[1]) >= 1 << 31:
+            raise TabedError("a cache's sizes must fit 32 bits")
         self.layers = k.shape[0] if k.dim() == 4 else 1
         self.rows, self.head_dim, self.kv_heads = table.shape[0], head_dim, kvh
         self.k, self.v, self.kscale, self.vscale, self.table = k, v, kscale, vscale, table
@@ -712,7 +717,6 @@ def tabed_attention_q8(cache: CacheQ8, ws, q, ctx_len, out, n_new=None, scale=No
 
 def prepare_attention_q8(cache: CacheQ8, ws, q, ctx_len, out, n_new=None, scale=None, lse=None, stream=None) -> PreparedCall:
     return _prepare_attention_q8(cache, ws, q, ctx_len, out, n_new, scale, lse, stream)
-
 
 
 def _one_layer(cache, what):

@@ -186,3 +186,11 @@ def test_body_step_q8_refuses(lib):
     assert lib.tabed_body_q8_workspace_init(body_ok()["cfg"], cache(), 3, None, None) == ENULL
     assert lib.tabed_body_q8_workspace_init(body_ok()["cfg"], cache(), 3, C.c_void_p(0x1008), None) == EALIGN
     assert lib.tabed_body_q8_workspace_init(body_ok()["cfg"], cache(kv_heads=1), 3, P, None) == EINVAL
+
+
+def test_sizes_past_32_bits_are_refused_by_the_binding(lib):
+    args = [1, 16, 16, 0x1000, 16, 0x1000, 0x1000, 0x1000, 0, 0x1000, 16, None]
+    assert binding.DeviceCall(lib.tabed_linear_q8, args, "tabed_linear_q8", 0, ()).device == 0
+    for at, size in ((0, 2 ** 32 + 1), (1, 2 ** 31), (2, -2 ** 31 - 1)):
+        with pytest.raises(binding.TabedError, match="32 bits"):
+            binding.DeviceCall(lib.tabed_linear_q8, args[:at] + [size] + args[at + 1:], "tabed_linear_q8", 0, ())
