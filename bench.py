@@ -29,7 +29,7 @@ def source_digest():
     """Short digest of the kernel sources: a traffic figure measured on other sources is not reported."""
     import hashlib
     h = hashlib.sha256()
-    for name in ("device_utils.h", "internal.h", "lmhead.hip", "vocab.hip"):
+    for name in ("device_utils.h", "internal.h", "lmhead.hip", "lmhead_store.h", "vocab.hip"):
         with open(os.path.join(ROOT, "paper_2601_20357_amd", "csrc", name), "rb") as f:
             h.update(f.read())
     return h.hexdigest()[:16]
