@@ -344,11 +344,12 @@ static hipError_t launch_tiles(const ProfScope* prof, const LinearArgs& a, hipSt
     // tile that every compute unit has at most one of (64 x 8192, K = 4096: 9.7 us in 32 x 64, 10.1 in 64 x 64, 14.7 in 64 x 128;
     // 128 rows: 13.7, 10.6, 14.8).  With one or two row blocks and more columns than that it is two workgroups a compute unit, or one after the other
     // with deeper stages where K is long enough to fill them (16 x 32000: K = 2048 14.1 us against 15.7, K = 4096 30.4 against 28.7), or one of
-    // 64 x 128 where K is short (the LM head of 64 x 32000, K = 768: 7.8 us against 8.8; 64 x 32000, K = 4096: 35.4 against 31.0).
+    // 64 x 128 where K is short and there are few results or softmax partials, which all eight waves then make (20000 columns, 32 rows, K = 1024 7.9 us
+    // against 8.5, LM head of 64 x 32000, K = 768 7.9 against 8.7; but its product alone 8.6 against 8.2, and with K = 4096 35.4 against 31.0).
     if (tiles(32, 32) <= 256 && tiles(32, 32) * a.K <= 3 << 18) return launch_tile_q8<32, 32, 8, 2, 2, EPI, PAST>(prof, a, s);
     if (tiles(32, 64) <= 256 || (a.M <= 32 && a.K >= 4096)) return launch_tile_q8<32, 64, 4, 3, 3, EPI, PAST>(prof, a, s);
     if (tiles(64, 64) <= 256) return launch_tile_q8<64, 64, 2, 3, 3, EPI, PAST>(prof, a, s);
-    if (a.M <= 64 && a.K <= 1024 && tiles(64, 128) <= 256) return launch_tile_q8<64, 128, 1, 3, 3, EPI, PAST>(prof, a, s);
+    if (a.M <= (EPI == kOutHead ? 64 : 32) && a.K <= 1024 && tiles(64, 128) <= 256) return launch_tile_q8<64, 128, 1, 3, 3, EPI, PAST>(prof, a, s);
     if (a.M <= 64) return launch_tile_q8<64, 64, 2, 2, 2, EPI, PAST>(prof, a, s);
     // Many tiles: time goes in rounds of as many workgroups as fit the chip, and a round's length with the tile (K = 4096: 57 us in 256 x 256, 36 in
     // 128 x 256, 22 in 128 x 128, 18 in 64 x 128, or 29 where that has two workgroups a compute unit; K = 512: 15.7, 9.6, 5.8, 4.9, 7.9).  Taken is
