@@ -144,7 +144,7 @@ def test_linear_q8_longest_sums_and_larger_sizes(M, N, K):
 
 @pytest.mark.parametrize("M,N,K", [(3, 70001, 4112), (40, 40001, 1040), (17, 66000, 2064), (64, 33000, 2048)])
 def test_linear_q8_workgroups_that_go_on(M, N, K):
-    """More columns than the workgroups take at once, with X in one chunk and in several."""
+    """More tiles than run at once."""
     g = torch.Generator(device=DEV).manual_seed(N)
     x, w = (torch.randint(-127, 128, s, generator=g, dtype=torch.int8, device=DEV) for s in ((M, K), (N, K)))
     sx, sw = torch.ones(M, device=DEV), torch.ones(N, device=DEV)
