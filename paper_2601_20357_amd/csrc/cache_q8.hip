@@ -555,7 +555,7 @@ __global__ __launch_bounds__(NW * 64, HD <= 128 || !WIDE ? 2 : 1) void k_attn_q8
 
     // One block, whose K and V are on their way; those of `next` are requested in between.
     auto block = [&](int b, float ksc, float vsc, int next, uint32_t mask) {
-        float s[16], step = worth * ksc;
+        float s[16], step = worth * ksc, vs = vsc;
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
             i32x4 acc[DG];
@@ -585,6 +585,7 @@ __global__ __launch_bounds__(NW * 64, HD <= 128 || !WIDE ? 2 : 1) void k_attn_q8
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = b * kCB + g * 16 + i > ctx + tok ? -INFINITY : s[i] * step;
             step = 1.f;
+            vs = b * kCB > ctx + tok ? 0.f : vsc;                      // (a query that sees none of the block: 0 times a bad scale is not 0)
         }
         float mx = s[0];
 #pragma unroll
@@ -620,7 +621,7 @@ __global__ __launch_bounds__(NW * 64, HD <= 128 || !WIDE ? 2 : 1) void k_attn_q8
             for (int ot = 0; ot < OT; ++ot) {
                 const i32x4 acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(vf[ot], pd, i32x4{0, 0, 0, 0}, 0, 0, 0);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) o[ot][i] = fmaf((float)acc[i], vsc, o[ot][i]);
+                for (int i = 0; i < 4; ++i) o[ot][i] = fmaf((float)acc[i], vs, o[ot][i]);
             }
         } else {
             f16x8 ph[2], pl[2];
@@ -643,7 +644,7 @@ __global__ __launch_bounds__(NW * 64, HD <= 128 || !WIDE ? 2 : 1) void k_attn_q8
 #pragma unroll
                 for (int i = 0; i < kSide; ++i)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) o[o0 + i][e] = fmaf(acc[i][e], vsc, o[o0 + i][e]);
+                    for (int e = 0; e < 4; ++e) o[o0 + i][e] = fmaf(acc[i][e], vs, o[o0 + i][e]);
             }
         }
         __builtin_amdgcn_sched_barrier(0);
