@@ -414,7 +414,7 @@ int tabed_cache_append_q8(const tabed_cache_q8* cache, int32_t rows, int32_t T, 
  *   scale > 0, commonly 1 / sqrt(head_dim)
  * A token that sees nothing (its blocks are not there) gets zeros and an lse of -inf.  Entries of tokens from n_new[r] on are left as
  * they were.  q_heads is a multiple of kv_heads, T * q_heads at most 2^20.
- * `ws`: tabed_attention_q8_workspace_bytes bytes, prepared once by ..._init, for calls with the same cache sizes, rows, T and q_heads.
+ * `ws`: tabed_attention_q8_workspace_bytes bytes, prepared once by ..._init; it then serves calls of any sizes that need no more bytes.
  * Calls that share a workspace must not overlap.
  */
 size_t tabed_attention_q8_workspace_bytes(const tabed_cache_q8* cache, int32_t rows, int32_t T, int32_t q_heads);   /* 0: invalid */
@@ -443,8 +443,8 @@ int tabed_draft_step_q8(const tabed_cfg* cfg, void* ws, uint64_t round, int32_t 
  *   H        [rows,d] bf16 out, or NULL      H8, h_scale  [rows,d] int8 and [rows] fp32 out, or both NULL (not with H NULL)
  * Other arguments and the positions as for tabed_draft_body_step, tabed_draft_body_rollback included; a ctx_len entry outside [0, max_ctx) is
  * an error of the caller: nothing is written outside the table's blocks, the results are not defined.
- * `ws`: tabed_body_q8_workspace_bytes bytes, prepared once by ..._init for these sizes and rows (not shared with other calls that
- * run at the same time).
+ * `ws`: tabed_body_q8_workspace_bytes bytes, prepared once by ..._init; it then serves steps of any sizes and rows that need no more bytes
+ * (not shared with other calls that run at the same time).
  */
 size_t tabed_body_q8_workspace_bytes(const tabed_body_cfg* cfg, const tabed_cache_q8* cache, int32_t rows);   /* 0: invalid */
 int tabed_body_q8_workspace_init(const tabed_body_cfg* cfg, const tabed_cache_q8* cache, int32_t rows, void* ws, void* stream);

@@ -680,7 +680,7 @@ def tabed_attention_q8_workspace_init(cache: CacheQ8, rows, T, q_heads, ws, stre
 
 
 def new_attention_workspace(cache: CacheQ8, rows, T, q_heads, stream=None):
-    """Allocate (torch) and prepare the workspace of tabed_attention_q8 for these sizes."""
+    """Allocate (torch) and prepare the workspace of tabed_attention_q8 for these sizes, or others that need no more bytes."""
     import torch
     nbytes = tabed_attention_q8_workspace_bytes(cache, rows, T, q_heads)
     if nbytes == 0:

@@ -461,7 +461,7 @@ int tabed_attention_q8_workspace_init(const tabed_cache_q8* cache, int32_t rows,
     if (rc != TABED_OK) return rc;
     if (ws == nullptr) return TABED_ENULL;
     if (misaligned(ws)) return TABED_EALIGN;
-    const hipError_t e = launch_attn_init(*cache, rows, T, q_heads, static_cast<char*>(ws), static_cast<hipStream_t>(stream));
+    const hipError_t e = launch_attn_init(static_cast<char*>(ws), static_cast<hipStream_t>(stream));
     return e == hipSuccess ? TABED_OK : fail_hip(e);
 }
 
@@ -524,7 +524,7 @@ int tabed_body_q8_workspace_init(const tabed_body_cfg* cfg, const tabed_cache_q8
     if (rc != TABED_OK) return rc;
     if (ws == nullptr) return TABED_ENULL;
     if (misaligned(ws)) return TABED_EALIGN;
-    const hipError_t e = launch_body_q8_init(*cfg, *cache, rows, static_cast<char*>(ws), static_cast<hipStream_t>(stream));
+    const hipError_t e = launch_attn_init(static_cast<char*>(ws), static_cast<hipStream_t>(stream));      // (the attention's workspace comes first)
     return e == hipSuccess ? TABED_OK : fail_hip(e);
 }
 

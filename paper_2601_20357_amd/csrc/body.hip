@@ -861,17 +861,13 @@ hipError_t launch_body_step(const tabed_body_cfg& c, const tabed_body_weights& w
 // from there they are appended to the blocks.  Six launches a layer.
 BodyQ8Layout body_q8_layout(const tabed_body_cfg& c, const tabed_cache_q8& cache, int rows) {
     BodyQ8Layout L;
+    size_t off = al256(attn_layout(cache, rows, 1, c.heads).total);
     L.body = body_layout(c, rows, true);
-    size_t off = L.body.total;
+    L.off_body = off; off += L.body.total;
     L.off_k = off;    off = al256(off + sizeof(uint16_t) * (size_t)rows * c.d);
     L.off_v = off;    off = al256(off + sizeof(uint16_t) * (size_t)rows * c.d);
-    L.off_attn = off; off = al256(off + attn_layout(cache, rows, 1, c.heads).total);
     L.total = off;
     return L;
-}
-
-hipError_t launch_body_q8_init(const tabed_body_cfg& c, const tabed_cache_q8& cache, int rows, char* ws, hipStream_t s) {
-    return launch_attn_init(cache, rows, 1, c.heads, ws + body_q8_layout(c, cache, rows).off_attn, s);
 }
 
 hipError_t launch_body_step_q8(const tabed_body_cfg& c, const tabed_body_weights& w, char* ws, int rows, const int32_t* token_src,
@@ -881,6 +877,7 @@ hipError_t launch_body_step_q8(const tabed_body_cfg& c, const tabed_body_weights
     const int d = c.d, hd = c.d / c.heads;
     uint16_t* kn = reinterpret_cast<uint16_t*>(ws + L.off_k);
     uint16_t* vn = reinterpret_cast<uint16_t*>(ws + L.off_v);
+    char* const body = ws + L.off_body;
     ProjArgs last;
     auto caches = [&](int, ProjArgs& a) {
         a.kc = kn; a.vc = vn; a.max_ctx = 1;
@@ -894,10 +891,10 @@ hipError_t launch_body_step_q8(const tabed_body_cfg& c, const tabed_body_weights
         layer.vscale = cache.vscale + heads;
         const hipError_t e = launch_cache_append(layer, rows, 1, 1, kn, vn, d, d, ctx_len, nullptr, s);
         if (e != hipSuccess) return e;
-        return launch_attention_q8(layer, ws + L.off_attn, rows, 1, c.heads, 0, a.q, d, d, ctx_len, nullptr, 1.f / std::sqrt((float)hd), 1,
-                                   ws + L.body.off_hb, d, d, nullptr, s);
+        return launch_attention_q8(layer, ws, rows, 1, c.heads, 0, a.q, d, d, ctx_len, nullptr, 1.f / std::sqrt((float)hd), 1,
+                                   body + L.body.off_hb, d, d, nullptr, s);
     };
-    hipError_t e = body_layers(c, w, ws, L.body, rows, 1, token_src, token_stride, rows_per_token, ctx_len, caches, attend, last, s);
+    hipError_t e = body_layers(c, w, body, L.body, rows, 1, token_src, token_stride, rows_per_token, ctx_len, caches, attend, last, s);
     if (e != hipSuccess) return e;
     if (H != nullptr && (e = launch_norm(last, H, H8 == nullptr ? ctx_len : nullptr, s)) != hipSuccess) return e;
     if (H8 == nullptr) return hipSuccess;

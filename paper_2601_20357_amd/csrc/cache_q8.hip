@@ -330,7 +330,7 @@ struct AttnArgs {
     const int32_t* ctx_len;
     const int32_t* n_new;
     float scale2;                // scale * log2(e)
-    uint32_t* arrivals;          // [rows, kv_heads, tiles]
+    uint32_t* arrivals;          // [rows, kv_heads, tiles], where there are several ranges
     float* po;                   // [rows, kv_heads, tiles, S][queries][hd]: sums of p v, at the range's own maximum
     float* pml;                  // the same [2][queries]: maxima (base 2), sums of p
 };
@@ -343,6 +343,7 @@ typedef float f32x2_any __attribute__((ext_vector_type(2), aligned(4)));
 typedef uint32_t u32_e2 __attribute__((aligned(2)));
 
 constexpr int kMaxRanges = 64;
+constexpr int kCutUnits = 256;   // rows x heads x tiles that are cut into ranges: fewer than this
 constexpr int kMinBlocks = 1;    // of a wave, where a row has several ranges
 constexpr int attn_queries(bool wide) { return wide ? 16 : 4; }        // of a workgroup
 
@@ -814,22 +815,21 @@ static AttnPlan attn_plan(const tabed_cache_q8& c, int rows, int T, int q_heads)
     p.tiles = (queries + attn_queries(p.wide) - 1) / attn_queries(p.wide);
     const long units = (long)rows * c.kv_heads * p.tiles;
     p.nw = units <= 256 && c.head_dim <= 128 ? 8 : 4;
-    const long want = (256 + units - 1) / units, most = std::max(1, c.max_blocks / (p.nw * kMinBlocks));
+    const long want = (kCutUnits + units - 1) / units, most = std::max(1, c.max_blocks / (p.nw * kMinBlocks));
     p.S = (int)std::min<long>({want, most, kMaxRanges});
     return p;
 }
 
+// All that a call expects to find is the arrival counters at 0, as the call before left them, and these are at the same place for all sizes: one
+// workspace serves calls of different sizes one after the other.
 AttnLayout attn_layout(const tabed_cache_q8& c, int rows, int T, int q_heads) {
     AttnLayout L;
     const AttnPlan p = attn_plan(c, rows, T, q_heads);
-    const size_t nq = attn_queries(p.wide);
-    L.tiles = p.tiles;
-    L.S = p.S;
-    L.units = (size_t)rows * c.kv_heads * p.tiles;
+    const size_t nq = attn_queries(p.wide), units = (size_t)rows * c.kv_heads * p.tiles;
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
-    size_t off = up(sizeof(uint32_t) * L.units);
-    L.off_po = off;  off = up(off + (L.S > 1 ? sizeof(float) * L.units * L.S * nq * c.head_dim : 0));
-    L.off_pml = off; off = up(off + (L.S > 1 ? sizeof(float) * L.units * L.S * nq * 2 : 0));
+    size_t off = sizeof(uint32_t) * kCutUnits;
+    L.off_po = off;  off = up(off + (p.S > 1 ? sizeof(float) * units * p.S * nq * c.head_dim : 0));
+    L.off_pml = off; off = up(off + (p.S > 1 ? sizeof(float) * units * p.S * nq * 2 : 0));
     L.total = off;
     return L;
 }
@@ -839,14 +839,10 @@ int64_t attn_workgroups(const tabed_cache_q8& c, int rows, int T, int q_heads) {
     return ((int64_t)rows * c.kv_heads * p.S + 7) / 8 * 8 * p.tiles;
 }
 
-__global__ void k_attn_init(uint32_t* arrivals, size_t n) {
-    const size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
-    if (i < n) arrivals[i] = 0u;
-}
+__global__ void k_attn_init(uint32_t* arrivals) { arrivals[threadIdx.x] = 0u; }
 
-hipError_t launch_attn_init(const tabed_cache_q8& c, int rows, int T, int q_heads, char* ws, hipStream_t s) {
-    const AttnLayout L = attn_layout(c, rows, T, q_heads);
-    launch(nullptr, k_attn_init, dim3((unsigned)((L.units + 255) / 256)), dim3(256), 0, s, reinterpret_cast<uint32_t*>(ws), L.units);
+hipError_t launch_attn_init(char* ws, hipStream_t s) {
+    launch(nullptr, k_attn_init, dim3(1), dim3(kCutUnits), 0, s, reinterpret_cast<uint32_t*>(ws));
     return hipGetLastError();
 }
 

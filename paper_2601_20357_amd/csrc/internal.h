@@ -148,28 +148,25 @@ hipError_t launch_linear_q8(int M, int N, int K, const int8_t* X, int64_t ldx, c
 int64_t append_workgroups(const tabed_cache_q8& c, int rows, int T);
 hipError_t launch_cache_append(const tabed_cache_q8& c, int rows, int T, int kv_dtype, const void* k, const void* v, int64_t row_stride,
                                int64_t tok_stride, const int32_t* ctx_len, const int32_t* n_new, hipStream_t s);
-struct AttnLayout {
-    int tiles, S;        // workgroups of a row and key / value head, times ranges of blocks
-    size_t units;        // uint32 [rows, kv_heads, tiles] arrival counters, first in the workspace
-    size_t off_po;       // float [units][S][queries of a workgroup][head_dim]: more than one range only
-    size_t off_pml;      // float [units][S][2][queries of a workgroup]
+struct AttnLayout {      // (arrival counters come first, as many for all sizes)
+    size_t off_po;       // float [rows, kv_heads, tiles][S][queries of a workgroup][head_dim]: more than one range only
+    size_t off_pml;      // float [rows, kv_heads, tiles][S][2][queries of a workgroup]
     size_t total;
 };
 AttnLayout attn_layout(const tabed_cache_q8& c, int rows, int T, int q_heads);
 int64_t attn_workgroups(const tabed_cache_q8& c, int rows, int T, int q_heads);
-hipError_t launch_attn_init(const tabed_cache_q8& c, int rows, int T, int q_heads, char* ws, hipStream_t s);
+hipError_t launch_attn_init(char* ws, hipStream_t s);
 hipError_t launch_attention_q8(const tabed_cache_q8& c, char* ws, int rows, int T, int q_heads, int q_dtype, const void* q, int64_t q_row,
                                int64_t q_tok, const int32_t* ctx_len, const int32_t* n_new, float scale, int out_dtype, void* out,
                                int64_t out_row, int64_t out_tok, float* lse, hipStream_t s);
 
-struct BodyQ8Layout {
+struct BodyQ8Layout {    // (the workspace of the attention comes first: what it expects to find is at the same place for all sizes)
+    size_t off_body;
     BodyLayout body;
     size_t off_k, off_v; // bf16 [rows,d] the layer's new keys and values
-    size_t off_attn;     // workspace of the attention
     size_t total;
 };
 BodyQ8Layout body_q8_layout(const tabed_body_cfg& c, const tabed_cache_q8& cache, int rows);
-hipError_t launch_body_q8_init(const tabed_body_cfg& c, const tabed_cache_q8& cache, int rows, char* ws, hipStream_t s);
 hipError_t launch_body_step_q8(const tabed_body_cfg& c, const tabed_body_weights& w, char* ws, int rows, const int32_t* token_src,
                                int token_stride, int rows_per_token, int32_t* ctx_len, const tabed_cache_q8& cache, uint16_t* H,
                                int8_t* H8, float* h_scale, hipStream_t s);

@@ -6,8 +6,9 @@ import numpy as np
 import pytest
 import torch
 
-from paper_2601_20357_amd import binding
+from paper_2601_20357_amd import binding, synth
 from test_gpu_q8 import BF16, DEV, F32, Cache, attend, check_attention, gen, randn
+from test_gpu_q8_step import Pair
 
 pytestmark = pytest.mark.gpu
 
@@ -54,3 +55,42 @@ def test_a_bad_token_leaves_earlier_tokens_of_its_call_alone():
     for out in outs[1:]:
         assert torch.isnan(out[0, 1]).all()
         assert torch.equal(out[0, 0], outs[0][0, 0]) and torch.equal(out[1], outs[0][1])
+
+
+def test_one_workspace_serves_calls_of_different_sizes():
+    """A loop that verifies blocks of six tokens and decodes single ones in between, over two caches: the largest call's workspace serves them all."""
+    caches = [Cache(2, 130, 2, 64, seed=31), Cache(5, 40, 1, 96, seed=32)]
+    ctx = [[8200, 3000], [2500, 17, 900, 64, 2000]]
+    calls = [(i, randn(gen(10 * T + i), caches[i].rows, T, 4, caches[i].hd)) for i in (0, 1) for T in (1, 2, 6, 40)]
+    need = [binding.tabed_attention_q8_workspace_bytes(caches[i].gpu, caches[i].rows, q.shape[1], 4) for i, q in calls]
+    assert len(set(need)) > 4
+    want = [attend(caches[i], q, ctx[i]) for i, q in calls]
+    check_attention(caches[0], calls[2][1], ctx[0], None, *want[2])
+    ws = torch.empty(max(need), dtype=torch.uint8, device=DEV)
+    ws.fill_(0xa5)
+    binding.tabed_attention_q8_workspace_init(caches[0].gpu, 2, 1, 4, ws)            # (prepared by the sizes of a small call)
+    for at in (0, 7, 3, 2, 0, 5, 6, 1, 4, 2, 3, 7, 0, 2, 0):
+        i, q = calls[at]
+        out, lse = attend(caches[i], q, ctx[i], ws=ws)
+        assert torch.equal(out, want[at][0]) and torch.equal(lse, want[at][1]), at
+
+
+def test_one_workspace_serves_body_steps_of_different_sizes():
+    bcs = [synth.BodyConfig(layers=2, d=256, heads=4, d_ff=512, V=300, max_ctx=1000), synth.BodyConfig(layers=1, d=128, heads=1, d_ff=256, V=300, max_ctx=640)]
+    sizes = [(0, 3), (0, 20), (1, 2), (1, 9)]
+    ctx = lambda i, rows: [(bcs[i].max_ctx - 10) // (1 + r) for r in range(rows)]
+    pairs = lambda: [Pair(bcs[i], rows, 40 + rows, ctx(i, rows)) for i, rows in sizes]
+    want = [p.step(np.arange(p.rows) * 7) for p in pairs()]
+    ps = pairs()
+    ws = max((p.ws for p in ps), key=lambda w: w.numel()).clone()
+    ws.fill_(0xa5)
+    binding.tabed_body_q8_workspace_init(ps[0].cfg, ps[0].gpu, 3, ws)
+    for at in (1, 0, 3, 2):
+        ps[at].ws = ws
+        for got, w in zip(ps[at].step(np.arange(ps[at].rows) * 7), want[at]):
+            assert torch.equal(got, w), at
+    for at in (2, 1, 3, 0):                                                         # again, from the first step's state
+        fresh = Pair(bcs[sizes[at][0]], sizes[at][1], 40 + sizes[at][1], ctx(*sizes[at]))
+        fresh.ws = ws
+        for got, w in zip(fresh.step(np.arange(fresh.rows) * 7), want[at]):
+            assert torch.equal(got, w), at
