@@ -582,7 +582,11 @@ __global__ __launch_bounds__(NW * 64, HD <= 128 || !WIDE ? 2 : 1) void k_attn_q8
             for (int i = 0; i < 16; ++i) s[i] += dpp_f32<kDppXor2>(s[i]);
             step = 1.f;
         }
-        if (b * kCB + kCB - 1 > ctx + t_first) {                       // uniform: some query does not see all of the block
+        // With many queries the maximum comes off a score in the addition that scales it: both roundings then are of the score's size, and past 2^25
+        // or so they would take the largest probability out of a half's range.  Where scores can be as large as 2^20 they are scaled before.
+        constexpr float kFar = 0x1p20f / (8355704.f * 127.f * HD);
+        const bool far = WIDE && __any(step > kFar);
+        if (far || b * kCB + kCB - 1 > ctx + t_first) {                // uniform: some query does not see all of the block
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = b * kCB + g * 16 + i > ctx + tok ? -INFINITY : s[i] * step;
             step = 1.f;
@@ -601,7 +605,12 @@ __global__ __launch_bounds__(NW * 64, HD <= 128 || !WIDE ? 2 : 1) void k_attn_q8
             for (int ot = 0; ot < OT; ++ot) o[ot] *= alpha;
         }
         constexpr float kOneExp = WIDE ? 14.f : 0.f;
-        const float off = kOneExp - base;
+        float off = kOneExp - base;
+        if (far) {                                                     // uniform
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] -= base;
+            off = kOneExp;
+        }
         float p[16], sum = 0.f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {

@@ -7,6 +7,7 @@ import pytest
 import torch
 
 from paper_2601_20357_amd import binding, synth
+from q8_reference import layout
 from test_gpu_q8 import BF16, DEV, F32, Cache, attend, check_attention, gen, randn
 from test_gpu_q8_step import Pair
 
@@ -94,3 +95,40 @@ def test_one_workspace_serves_body_steps_of_different_sizes():
         fresh.ws = ws
         for got, w in zip(fresh.step(np.arange(fresh.rows) * 7), want[at]):
             assert torch.equal(got, w), at
+
+
+@pytest.mark.parametrize("size", [300.0, 3e6, 7e6, 4.1e8, -1e10, 1e20, -1e30])
+@pytest.mark.parametrize("hd,group,T", [(64, 8, 1), (128, 5, 2), (256, 6, 1), (96, 1, 40), (64, 2, 1)])
+def test_attention_with_scores_of_any_size(hd, group, T, size):
+    """Queries of one direction: a score is a key's step times the same number, so tokens of the extreme step share the weight equally, and n others,
+    a step or more away, have at most n exp(-|size| / sqrt(hd)) of it, which moves outputs by at most the difference of two values, 254, times that
+    (a trace at the first size, nothing at the others).  Counted in half steps of fp32 (2^-24): probabilities are equal and exact; the sums over
+    blocks as in the reference (2 (blocks + 220)), scales, division and places 12.  At the first size, where scores are below 2^20, many queries
+    have them scaled in the addition that takes the maximum off, except in a block that is seen in part: the probabilities of equal scores are then off by
+    e = (a rounding each of score, maximum and difference, of the score's size, + 14 and exp2's 2) ln 2 or less, twice in their quotient.  The logarithm: a score is a product of six roundings
+    (query's step twice, scale, key's scale, score, base 2 to e), each of its own size, log2 and the sum two more, of the sum of at most 60 ties (below 6)."""
+    c = Cache(5, 70, 2, hd, seed=hd + T)
+    for n in ("k", "v"):
+        c.scale[n][:] = 1.0
+    c.push()
+    q = torch.zeros(5, T, 2 * group, hd)
+    for i in range(2 * group):
+        q[..., i, (7 * i + 3) % hd] = size
+    ctx = [0, 64 * 4 - 1, 64 * 69 - 1, 1000, 30]
+    out, lse = attend(c, q, ctx)
+    for r in range(5):
+        for t in range(T):
+            n = ctx[r] + t + 1
+            blocks = (n + 63) // 64
+            for i in range(2 * group):
+                h, dim = i // group, (7 * i + 3) % hd
+                k, v = (np.concatenate([c.pool[w][c.table[r, b], h][layout(w, hd)] for b in range(blocks)])[:n].astype(np.float64) for w in ("k", "v"))
+                score = k[:, dim] * float(np.float32(size)) * hd ** -0.5
+                best = score == score.max()
+                want, wlse = v[best].mean(0), score.max() + math.log(best.sum())
+                assert best.sum() <= 60
+                others = n * math.exp(-abs(size) * hd ** -0.5)
+                e = 3 * abs(wlse) + 20 if abs(size) < 1000 else 0
+                tol = (2 * (blocks + 220) + 12 + 2 * e) * 2.0 ** -24 * np.abs(v[best]).max(0) + 254 * others
+                assert (np.abs(out[r, t, i].double().numpy() - want) <= tol).all(), (r, t, i)
+                assert abs(float(lse[r, t, i]) - wlse) <= (8 * abs(wlse) + 8 * 6 + e) * 2.0 ** -24 + others, (r, t, i)
