@@ -90,21 +90,6 @@ __device__ __forceinline__ uint32_t word_again(uint32_t w, int keep /* of its fo
     }
     return pack_i8(s[0], s[1], s[2], s[3]);
 }
-// round(x / scale), the division as fp32 rounds it.  A product with the reciprocal is off by less than 1.6e-5 steps: only where
-// one comes that near to the middle between two steps is the division made (a dozen instructions each: half of a prompt's time).
-__device__ __forceinline__ void steps_of(const float (&x)[16], float scale, float inv, int (&s)[16]) {
-    float far = 0.f;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-        const float t = x[e] * inv, r = rintf(t);
-        far = fmaxf(far, fabsf(t - r));
-        s[e] = (int)r;
-    }
-    if (__any(far > 0.5f - 2e-5f)) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[e] = (int)rintf(x[e] / scale);
-    }
-}
 __device__ __forceinline__ u32x4_e4 pack_steps(const int (&s)[16]) {
     return u32x4_e4{pack_i8(s[0], s[1], s[2], s[3]), pack_i8(s[4], s[5], s[6], s[7]), pack_i8(s[8], s[9], s[10], s[11]), pack_i8(s[12], s[13], s[14], s[15])};
 }

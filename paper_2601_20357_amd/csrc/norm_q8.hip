@@ -133,13 +133,17 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_q8(NormArgs a) {
         for (int w = 0; w < kWaves; ++w) most = max(most, s_most[w]);
     }
     const float scale = scale_of(most);
-    const float inv = (scale > 0.f) ? 127.f / __builtin_bit_cast(float, most) : 0.f;
+    const float inv = (scale > 0.f) ? 1.f / scale : 0.f;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
         const int at = (p * TPR + t) * 8;
         int s[8];
+        if (scale > 0.f) {                                             // (uniform for a wave)
+            steps_of(v[p], scale, inv, s);
+        } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s[e] = (scale > 0.f) ? to_step(v[p][e] * inv) : 0;
+            for (int e = 0; e < 8; ++e) s[e] = 0;
+        }
         int8_t* out = a.q + row * a.ldq + at;
         if (at + 8 <= d) {
             *reinterpret_cast<u32x2_e1*>(out) = u32x2_e1{pack_i8(s[0], s[1], s[2], s[3]), pack_i8(s[4], s[5], s[6], s[7])};
