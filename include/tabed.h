@@ -346,8 +346,8 @@ int tabed_draft_body_rollback(int32_t rows, int32_t rows_per_seq, int32_t gamma,
  * tabed_norm_q8: residual addition, RMSNorm and int8 rows with a scale each.
  *   r = x + delta;  y = r / sqrt(mean r^2 + eps) * gain;  q = round(y / scale), ties to even
  *   x     [rows,d] x_dtype in, row stride ldx            delta [rows,d] delta_dtype in, row stride ldd; NULL: r = x
- *   sum   [rows,d] x_dtype out, row stride lds: r, rounded to that type (the norm is of r before that); may be x itself; NULL: not
- *                  stored; without delta: NULL
+ *   sum   [rows,d] x_dtype out, row stride lds: r, rounded to that type (the norm is of r before that); may be x itself, with
+ *                  lds = ldx; NULL: not stored; without delta: NULL
  *   gain  [d] fp32 in; NULL: no norm, y = r (quantises weights, or activations that are normalised already; eps is not read)
  *   q     [rows,d] int8 out, row stride ldq              scale [rows] fp32 out
  *   d 1 .. 32768, rows up to 2^20; strides at least d; a row whose squares exceed fp32 counts as not finite.

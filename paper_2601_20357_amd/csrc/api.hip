@@ -403,6 +403,7 @@ int tabed_norm_q8(int32_t rows, int32_t d, int32_t x_dtype, const void* x, int64
     if (rows < 1 || rows > (1 << 20) || d < 1 || d > 32768) return TABED_ERANGE;
     if (!storage_type(x_dtype) || (delta != nullptr && !storage_type(delta_dtype))) return TABED_EINVAL;
     if (sum != nullptr && delta == nullptr) return TABED_EINVAL;
+    if (sum == x && rows > 1 && lds != ldx) return TABED_EINVAL;       // a row's sum would go to where another's values are
     if (ldx < d || ldq < d || (delta != nullptr && ldd < d) || (sum != nullptr && lds < d)) return TABED_EINVAL;
     if (gain != nullptr && !(eps > 0.f)) return TABED_EINVAL;
     if (element_misaligned(x, x_dtype) || element_misaligned(sum, x_dtype) || element_misaligned(delta, delta_dtype) ||
