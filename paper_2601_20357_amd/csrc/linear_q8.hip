@@ -374,7 +374,7 @@ static hipError_t launch_product(const ProfScope* prof, const LinearArgs& a, hip
 hipError_t launch_linear_q8(int M, int N, int K, const int8_t* X, int64_t ldx, const float* sx, const int8_t* W, const float* sw, int y_dtype,
                             void* Y, int64_t ldy, hipStream_t s) {
     const LinearArgs a{M, N, K, X, (uint32_t)ldx, sx, W, sw, Y, ldy, 1, nullptr, nullptr, nullptr};
-    ProfScope prof(TABED_K_LMHEAD, s);
+    ProfScope prof(TABED_K_BODY, s);
     return y_dtype == 1 ? launch_product<kOutB16>(&prof, a, s) : launch_product<kOutF32>(&prof, a, s);
 }
 
