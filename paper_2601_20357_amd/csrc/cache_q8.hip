@@ -329,7 +329,6 @@ typedef uint32_t u32_e2 __attribute__((aligned(2)));
 
 constexpr int kMaxRanges = 64;
 constexpr int kCutUnits = 256;   // rows x heads x tiles that are cut into ranges: fewer than this
-constexpr int kMinBlocks = 1;    // of a wave, where a row has several ranges
 constexpr int attn_queries(bool wide) { return wide ? 16 : 4; }        // of a workgroup
 
 // The four lanes of a query add the same four products, each in its own order, and have to come to the same sum: they give the digits of one
@@ -448,7 +447,7 @@ __global__ __launch_bounds__(NW * 64, HD <= 128 || !WIDE ? 2 : 1) void k_attn_q8
     const int ctx = (int)min((int64_t)max(a.ctx_len[row], 0), cap);
     const int t_first = q0 / a.group, t_last = min(n - 1, (q0 + NQ - 1) / a.group);
     const int NB = (int)((min((int64_t)ctx + t_last + 1, cap) + kCB - 1) / kCB);       // that some query of the tile sees
-    const int ranges = min(a.S, max(1, NB / (NW * kMinBlocks)));
+    const int ranges = min(a.S, max(1, NB / NW));                      // (a block for every wave, where there are several)
     if (sp >= ranges) return;
     const int per = (NB + ranges - 1) / ranges, b_begin = min(sp * per, NB), b_end = min(b_begin + per, NB);
 
@@ -809,7 +808,7 @@ static AttnPlan attn_plan(const tabed_cache_q8& c, int rows, int T, int q_heads)
     p.tiles = (queries + attn_queries(p.wide) - 1) / attn_queries(p.wide);
     const long units = (long)rows * c.kv_heads * p.tiles;
     p.nw = units <= 256 && c.head_dim <= 128 ? 8 : 4;
-    const long want = (kCutUnits + units - 1) / units, most = std::max(1, c.max_blocks / (p.nw * kMinBlocks));
+    const long want = (kCutUnits + units - 1) / units, most = std::max(1, c.max_blocks / p.nw);
     p.S = (int)std::min<long>({want, most, kMaxRanges});
     return p;
 }
