@@ -427,6 +427,14 @@ int tabed_linear_q8(int32_t M, int32_t N, int32_t K, const void* X, int64_t ldx,
     return e == hipSuccess ? TABED_OK : fail_hip(e);
 }
 
+// For the tests, not declared in the header: the tile that a product (head: the LM head) of these sizes runs in: rows, columns, waves that share K, stages
+// of W and of X.
+int tabed_testing_linear_tile(int32_t M, int32_t N, int32_t K, int32_t head, int32_t* tile /* [5] */) {
+    if (M < 1 || N < 1 || K < 16) return TABED_ERANGE;
+    linear_q8_tile(M, N, K, head != 0, tile);
+    return TABED_OK;
+}
+
 int tabed_cache_append_q8(const tabed_cache_q8* cache, int32_t rows, int32_t T, int32_t kv_dtype, const void* k, const void* v,
                           int64_t row_stride, int64_t tok_stride, const int32_t* ctx_len, const int32_t* n_new, void* stream) {
     const int rc = validate_cache(cache, true);

@@ -145,6 +145,7 @@ hipError_t launch_norm_q8(int rows, int d, int x_dtype, const void* x, int64_t l
                           int64_t lds, const float* g, float eps, int8_t* q, int64_t ldq, float* scale, int32_t* advance, hipStream_t s);
 hipError_t launch_linear_q8(int M, int N, int K, const int8_t* X, int64_t ldx, const float* sx, const int8_t* W, const float* sw, int y_dtype,
                             void* Y, int64_t ldy, hipStream_t s);
+void linear_q8_tile(int M, int N, int K, bool head, int32_t* tile /* [5] */);
 int64_t append_workgroups(const tabed_cache_q8& c, int rows, int T);
 hipError_t launch_cache_append(const tabed_cache_q8& c, int rows, int T, int kv_dtype, const void* k, const void* v, int64_t row_stride,
                                int64_t tok_stride, const int32_t* ctx_len, const int32_t* n_new, hipStream_t s);

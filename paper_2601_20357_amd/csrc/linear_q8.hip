@@ -336,9 +336,12 @@ static hipError_t launch_tile_q8(const ProfScope* prof, const LinearArgs& a, hip
     return hipGetLastError();
 }
 
-template <int EPI, bool PAST>
-static hipError_t launch_tiles(const ProfScope* prof, const LinearArgs& a, hipStream_t s) {
-    auto tiles = [&](int bm, int bn) { return (long)((a.M + bm - 1) / bm) * ((a.N + bn - 1) / bn); };
+// The tile for a product of these sizes, handed to `go`.
+template <int BM_, int BN_, int KW_, int SW_, int SH_>
+struct Tile { static constexpr int BM = BM_, BN = BN_, KW = KW_, SW = SW_, SH = SH_; };
+template <typename Go>
+static hipError_t with_tile(int M, int N, int K, bool head, Go&& go) {
+    auto tiles = [&](int bm, int bn) { return (long)((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
     // Few tiles: the smaller they are, the more compute units load.  32 x 32 reads X as often as W, so only while all tiles together
     // read little (200 x 1024, K = 2048: 4.7 us against 5.2 in 32 x 64; 16 x 8192, K = 8192: 20.1 against 12.4).  Then the smallest
     // tile that every compute unit has at most one of (64 x 8192, K = 4096: 9.7 us in 32 x 64, 10.1 in 64 x 64, 14.7 in 64 x 128;
@@ -346,11 +349,11 @@ static hipError_t launch_tiles(const ProfScope* prof, const LinearArgs& a, hipSt
     // with deeper stages where K is long enough to fill them (16 x 32000: K = 2048 14.1 us against 15.7, K = 4096 30.4 against 28.7), or one of
     // 64 x 128 where K is short and there are few results or softmax partials, which all eight waves then make (20000 columns, 32 rows, K = 1024 7.9 us
     // against 8.5, LM head of 64 x 32000, K = 768 7.9 against 8.7; but its product alone 8.6 against 8.2, and with K = 4096 35.4 against 31.0).
-    if (tiles(32, 32) <= 256 && tiles(32, 32) * a.K <= 3 << 18) return launch_tile_q8<32, 32, 8, 2, 2, EPI, PAST>(prof, a, s);
-    if (tiles(32, 64) <= 256 || (a.M <= 32 && a.K >= 4096)) return launch_tile_q8<32, 64, 4, 3, 3, EPI, PAST>(prof, a, s);
-    if (tiles(64, 64) <= 256) return launch_tile_q8<64, 64, 2, 3, 3, EPI, PAST>(prof, a, s);
-    if (a.M <= (EPI == kOutHead ? 64 : 32) && a.K <= 1024 && tiles(64, 128) <= 256) return launch_tile_q8<64, 128, 1, 3, 3, EPI, PAST>(prof, a, s);
-    if (a.M <= 64) return launch_tile_q8<64, 64, 2, 2, 2, EPI, PAST>(prof, a, s);
+    if (tiles(32, 32) <= 256 && tiles(32, 32) * K <= 3 << 18) return go(Tile<32, 32, 8, 2, 2>{});
+    if (tiles(32, 64) <= 256 || (M <= 32 && K >= 4096)) return go(Tile<32, 64, 4, 3, 3>{});
+    if (tiles(64, 64) <= 256) return go(Tile<64, 64, 2, 3, 3>{});
+    if (M <= (head ? 64 : 32) && K <= 1024 && tiles(64, 128) <= 256) return go(Tile<64, 128, 1, 3, 3>{});
+    if (M <= 64) return go(Tile<64, 64, 2, 2, 2>{});
     // Many tiles: time goes in rounds of as many workgroups as fit the chip, and a round's length with the tile (K = 4096: 57 us in 256 x 256, 36 in
     // 128 x 256, 22 in 128 x 128, 18 in 64 x 128, or 29 where that has two workgroups a compute unit; K = 512: 15.7, 9.6, 5.8, 4.9, 7.9).  Taken is
     // the least product of the two: 160 x 20000, K = 4096 30.5 us in 64 x 128, 32.7 in 128 x 256; 520 x 50000 144 in 128 x 256, 168 in
@@ -358,10 +361,26 @@ static hipError_t launch_tiles(const ProfScope* prof, const LinearArgs& a, hipSt
     auto cost = [&](int bm, int bn, int length, int at_once) { return (tiles(bm, bn) + at_once - 1) / at_once * length; };
     const long large = cost(256, 256, 16, 256), wide = cost(128, 256, 10, 256), mid = cost(128, 128, 6, 256);
     const long narrow = std::min(cost(64, 128, 5, 256), cost(64, 128, 8, 512));
-    if (large <= std::min({wide, mid, narrow})) return launch_tile_q8<256, 256, 1, 3, 2, EPI, PAST>(prof, a, s);
-    if (wide <= std::min(mid, narrow)) return launch_tile_q8<128, 256, 1, 3, 3, EPI, PAST>(prof, a, s);
-    if (mid <= narrow) return launch_tile_q8<128, 128, 1, 4, 4, EPI, PAST>(prof, a, s);
-    return launch_tile_q8<64, 128, 1, 3, 3, EPI, PAST>(prof, a, s);
+    if (large <= std::min({wide, mid, narrow})) return go(Tile<256, 256, 1, 3, 2>{});
+    if (wide <= std::min(mid, narrow)) return go(Tile<128, 256, 1, 3, 3>{});
+    if (mid <= narrow) return go(Tile<128, 128, 1, 4, 4>{});
+    return go(Tile<64, 128, 1, 3, 3>{});
+}
+
+template <int EPI, bool PAST>
+static hipError_t launch_tiles(const ProfScope* prof, const LinearArgs& a, hipStream_t s) {
+    return with_tile(a.M, a.N, a.K, EPI == kOutHead, [&](auto t) {
+        using T = decltype(t);
+        return launch_tile_q8<T::BM, T::BN, T::KW, T::SW, T::SH, EPI, PAST>(prof, a, s);
+    });
+}
+
+void linear_q8_tile(int M, int N, int K, bool head, int32_t* tile) {
+    (void)with_tile(M, N, K, head, [&](auto t) {
+        using T = decltype(t);
+        tile[0] = T::BM; tile[1] = T::BN; tile[2] = T::KW; tile[3] = T::SW; tile[4] = T::SH;
+        return hipSuccess;
+    });
 }
 
 template <int EPI>
