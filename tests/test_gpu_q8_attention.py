@@ -132,3 +132,73 @@ def test_attention_with_scores_of_any_size(hd, group, T, size):
                 tol = (2 * (blocks + 220) + 12 + 2 * e) * 2.0 ** -24 * np.abs(v[best]).max(0) + 254 * others
                 assert (np.abs(out[r, t, i].double().numpy() - want) <= tol).all(), (r, t, i)
                 assert abs(float(lse[r, t, i]) - wlse) <= (8 * abs(wlse) + 8 * 6 + e) * 2.0 ** -24 + others, (r, t, i)
+
+
+@pytest.mark.parametrize("hd", [32, 64, 96, 128])
+@pytest.mark.parametrize("group,T,n_new", [(1, 1, None), (4, 1, [1, 0] * 17), (3, 6, [6, 0, 3, 5, 1, 2, 6, 4, 6, 6] * 3 + [6, 6, 0, 6]), (8, 1, None), (2, 33, None)])
+def test_rows_and_heads_that_fill_the_chip(hd, group, T, n_new):
+    """More than 256 rows x heads x tiles of queries: workgroups of four waves, one range a row."""
+    rows, kvh = 34, 8
+    c = Cache(rows, 7, kvh, hd, seed=hd + T)
+    c.table[3, 1], c.table[4, :], c.table[5, 0] = -1, -1, 10 ** 7
+    c.push()
+    assert rows * kvh * 1 > 256
+    q = randn(gen(hd + T), rows, T, kvh * group, hd, dtype=BF16 if group == 4 else F32)
+    ctx = [int(x) for x in np.random.default_rng(T).integers(0, 380, rows)]
+    ctx[:3] = [0, 63, 64]
+    out, lse = attend(c, q, ctx, n_new)
+    check_attention(c, q, ctx, n_new, out, lse)
+
+
+@pytest.mark.parametrize("hd,kvh,group,T,rows,blocks", [(64, 4, 1, 1, 65, 530), (64, 4, 2, 3, 65, 530), (32, 2, 8, 1, 129, 300), (256, 1, 1, 1, 257, 270), (256, 1, 6, 1, 257, 259)])
+def test_waves_that_open_more_than_64_blocks(hd, kvh, group, T, rows, blocks):
+    """Rows in one range with more blocks than a wave of four opens at a time, from a small pool, missing ones around the border of the 64th of a wave and
+    of a whole opening among them."""
+    assert blocks > 4 * 64 and rows * kvh > 256
+    c = Cache(4, 3, kvh, hd, seed=hd + blocks)
+    g = np.random.default_rng(blocks)
+    pool = c.pool["k"].shape[0]
+    c.rows, c.width = rows, blocks
+    c.table = g.integers(0, pool, (rows, blocks)).astype(np.int32)
+    c.table[1, 250:262] = -1
+    c.table[2, :256] = -1                                              # a whole opening is missing
+    c.table[3, 256:] = -1
+    c.table[5, 253::4] = pool                                          # one wave's
+    c.push()
+    q = randn(gen(T), rows, T, kvh * group, hd)
+    ctx = [int(x) for x in g.integers(255 * 64, blocks * 64 - T, rows)]
+    ctx[:8] = [256 * 64 - 1, blocks * 64 - T, blocks * 64 - T, blocks * 64 - T, 256 * 64, blocks * 64 - T, 70, 0]
+    out, lse = attend(c, q, ctx)
+    few = [0, 1, 2, 3, 4, 5, 6, 7, rows - 1]                           # (the definition takes its time: these rows, and that equal rows are equal)
+    c.rows, c.table = len(few), c.table[few]
+    check_attention(c, q[few], [ctx[r] for r in few], None, out[few], lse[few])
+    assert torch.isfinite(out).all()
+
+
+@pytest.mark.parametrize("rows", [200, 256])
+def test_eight_waves_that_open_more_than_64_blocks(rows):
+    """Workgroups of eight waves with more than 512 blocks: one long row among short ones, in two ranges (200 rows) and in one (256)."""
+    hd, blocks = 64, 1100
+    c = Cache(4, 3, 1, hd, seed=3)
+    g = np.random.default_rng(5)
+    c.rows, c.width = rows, blocks
+    c.table = g.integers(0, c.pool["k"].shape[0], (rows, blocks)).astype(np.int32)
+    c.table[0, 500:530], c.table[0, 1060:1066] = -1, -1
+    c.push()
+    q = randn(gen(3), rows, 1, 2, hd)
+    ctx = [blocks * 64 - 1] + [int(x) for x in g.integers(0, 300, rows - 1)]
+    out, lse = attend(c, q, ctx)
+    few = [0, 1, 2, rows - 1]
+    c.rows, c.table = len(few), c.table[few]
+    check_attention(c, q[few], [ctx[r] for r in few], None, out[few], lse[few])
+
+
+@pytest.mark.parametrize("hd,kvh,group,T,qt", [(64, 1, 4, 700, F32), (128, 2, 2, 333, BF16), (256, 1, 3, 130, F32), (32, 1, 1, 1500, BF16)])
+def test_a_prompt(hd, kvh, group, T, qt):
+    """Hundreds of new tokens a row: many tiles of queries over the same blocks, each with an end of its own."""
+    width = (T + 200) // 64 + 1
+    c = Cache(2, width, kvh, hd, seed=T)
+    q = randn(gen(T), 2, T, kvh * group, hd, dtype=qt)
+    ctx, n_new = [0, 137], [T, T - 61]
+    out, lse = attend(c, q, ctx, n_new)
+    check_attention(c, q, ctx, n_new, out, lse)
