@@ -64,8 +64,10 @@ def parse():
     ap.add_argument("--steps", type=int, default=400)
     ap.add_argument("--warmup", type=int, default=40)
     ap.add_argument("--workload", default="serving", choices=["tiny", "llava", "serving", "lvlm", "stress"])
-    ap.add_argument("--pool", type=int, default=8, help="distinct pre-generated rounds (and W copies) cycled through")
-    ap.add_argument("--w-copies", type=int, default=8, help="device copies of W rotated per round (1 = warm cache)")
+    ap.add_argument("--pool", type=int, default=0, help="distinct pre-generated rounds cycled through (0 = 8, or 16 with --bits 8)")
+    ap.add_argument("--w-copies", type=int, default=0,
+                    help="device copies of W rotated per round (0 = 8, or 16 with --bits 8, whose copies are half as large: together they have "
+                         "to exceed the last-level cache; 1 = warm cache)")
     ap.add_argument("--no-cpu-baseline", action="store_true")
     ap.add_argument("--cpu-rounds", type=int, default=0,
                     help="rounds of the oracle's timed sample (0 = a workload-dependent default of 10-30 s)")
@@ -93,7 +95,10 @@ def parse():
     ap.add_argument("--calibrate-copy", type=int, default=0, metavar="MB",
                     help="only run a plain device copy of MB megabytes 10 times: the known-size kernel against "
                          "which rocprofv3's FETCH_SIZE / WRITE_SIZE counters are scaled")
-    return ap.parse_args()
+    args = ap.parse_args()
+    args.pool = args.pool or (16 if args.bits == 8 else 8)
+    args.w_copies = args.w_copies or (16 if args.bits == 8 else 8)
+    return args
 
 
 def gen_inputs(wl, pool, w_copies, device):
