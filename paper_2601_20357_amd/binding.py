@@ -630,8 +630,8 @@ def _heads_view(t, rows, T, heads, hd, name):
         raise TabedError(f"{name} must be [{rows}, {T}, {heads}, {hd}], got {tuple(t.shape)}")
     if t.shape[:2] != (rows, T) or t.stride(-1) != 1:
         raise TabedError(f"{name} must be [{rows}, {T}, {heads}, {hd}] with values side by side, got {tuple(t.shape)}, strides {t.stride()}")
-    row = t.stride(0) if rows > 1 else max(t.stride(0), T * heads * hd)
-    tok = t.stride(1) if T > 1 else max(t.stride(1), heads * hd)
+    tok = t.stride(1) if T > 1 else heads * hd               # (a stride that leads nowhere does not count)
+    row = t.stride(0) if rows > 1 else T * tok
     if tok < heads * hd or row < heads * hd or (rows > 1 and T > 1 and min(row, tok) * (T if tok < row else rows) > max(row, tok)):
         raise TabedError(f"{name}: tokens overlap")
     return t.data_ptr(), row, tok
