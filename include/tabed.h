@@ -25,7 +25,7 @@
  *   tabed_draft_body_step, Sec. 5.1 "Ensemble learning via Batched Inference", Sec. 4.1 "Target and Draft
  *   tabed_draft_body_rollback   Models": one decode step of the shared LLaMA-style draft model for the n * B rows.
  *   tabed_draft_step_static     tabed_draft_step for callers that cannot allocate device memory.
- *   tabed_norm_q8, tabed_linear_q8,                The draft model in 8 bits: norm, product, key / value cache and
+ *   tabed_norm_q8, tabed_linear_q8,                The draft side in 8 bits: norm, product, key / value cache and
  *   tabed_cache_append_q8, tabed_attention_q8      the attention over it; a draft step and a body step of them:
  *   tabed_draft_step_q8, tabed_draft_body_step_q8
  *
@@ -336,10 +336,10 @@ int tabed_draft_body_rollback(int32_t rows, int32_t rows_per_seq, int32_t gamma,
                               const int32_t* accept_len, int32_t* ctx_len, void* stream);
 
 /*
- * The draft model in 8 bits.  Weights, activations and the key / value cache as int8 (-127 .. 127) with fp32 scales: a value is
- * step * scale.  A scale is 1/127 of the largest magnitude it covers; it is 0, with all steps 0, where no magnitude reaches 2^-100,
- * and NaN, with all steps 0, where some value is not finite (what reads such a row or block gives NaN, not a number that looks
- * right).  Storage types of other operands are given as in tabed_cfg.w_dtype: 0 = fp32, 1 = bf16.  Strides count elements; rows
+ * The draft model's LM head and key / value cache in 8 bits, and the operators that they are made of.  Weights, activations and cached keys and
+ * values as int8 (-127 .. 127) with fp32 scales: a value is step * scale.  A scale is 1/127 of the largest magnitude it covers; it is 0, with all
+ * steps 0, where no magnitude reaches 2^-100, and NaN, with all steps 0, where some value is not finite (what reads such a row or block gives NaN,
+ * not a number that looks right).  Storage types of other operands are given as in tabed_cfg.w_dtype: 0 = fp32, 1 = bf16.  Strides count elements; rows
  * need no more than their type's own alignment unless said otherwise.  rows (M) = 0 and T = 0 are errors, as an empty batch is
  * everywhere in this library.
  *
@@ -407,8 +407,12 @@ int tabed_cache_append_q8(const tabed_cache_q8* cache, int32_t rows, int32_t T, 
 /*
  * tabed_attention_q8: causal attention of the T new tokens of every row over its cache, in which they are already
  * (tabed_cache_append_q8 with the same ctx_len and n_new).  Token t sees positions 0 .. ctx_len[r] + t; query head i reads
- * key / value head i / (q_heads / kv_heads).  Scores, softmax and sums are as accurate as in fp32: queries and probabilities enter
- * as 32-bit integers relative to their largest.
+ * key / value head i / (q_heads / kv_heads).  Scores, softmax and sums are in fp32 or exact; what is rounded before the products:
+ *   T * q_heads / kv_heads up to 4: a query to whole steps of its largest magnitude times 2^-30, probabilities to 2^-30 of the largest so far
+ *     (their sum is of the unrounded ones: n tokens below 2^-31 of the largest can be missing in an output, n 2^-31 max |v| at most)
+ *   more: a query to whole steps of its largest magnitude / 0x7f7f78, probabilities to 22 bits (and 2^-38 of the largest so far)
+ * A query with one dimension far larger than the others loses of these what fp32 would keep: the error of a score goes with max |q| sum |k|.
+ * A block whose scale is not finite makes the results of the tokens that see one of its positions NaN, and of no others.
  *   q    [rows, T, q_heads, head_dim] q_dtype in     out  the same, out_dtype, out; both with strides of a row and of a token
  *   lse  [rows, T, q_heads] fp32 out, optional: natural logarithm of the sum of exp(scale * score)
  *   scale > 0, commonly 1 / sqrt(head_dim)
@@ -436,7 +440,10 @@ int tabed_draft_step_q8(const tabed_cfg* cfg, void* ws, uint64_t round, int32_t 
 
 /*
  * tabed_draft_body_step over an 8-bit cache (half the bytes of keys and values, and blocks that rows may share), with the hidden
- * states in bf16, in int8 for tabed_draft_step_q8, or both.
+ * states in bf16, in int8 for tabed_draft_step_q8, or both.  Weights and projections stay in bf16.  It is six launches a layer for any number of
+ * rows, and pays from about 32 rows on: with fewer it saves memory, not time, above all where tabed_draft_body_step is one launch (up to 16 rows).  12 layers
+ * of d = 768, 256 to 768 positions, 8 / 16 bits in us: 351 / 215 at 4 rows, 402 / 264 at 16, 410 / 406 at 17, 464 / 468 at 32, 568 / 601 at 64; two layers 60 / 45,
+ * 64 / 52, 68 / 66, 75 / 71, 89 / 96.
  *   cache    k, v [layers, blocks, heads, 64 * head_dim], kscale, vscale [layers, blocks, heads], one table for all layers;
  *            kv_heads = heads, head_dim = d / heads (32, 64 or 128), max_blocks * 64 >= cfg->max_ctx.  The block that a row's next token goes to
  *            belongs to that row.

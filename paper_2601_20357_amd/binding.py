@@ -460,7 +460,7 @@ class PreparedCall:
             _check(rc, self.what)
 
 
-# ------------------------------------------------------------------ the draft model in 8 bits
+# ------------------------------------------------------------------ the draft side in 8 bits
 CACHE_BLOCK = 64
 
 
@@ -798,7 +798,8 @@ def _prepare_draft_body_step_q8(bcfg, weights, ws, rows, token_src, token_stride
 
 def tabed_draft_body_step_q8(bcfg, weights, ws, rows, token_src, token_stride, rows_per_token, ctx_len, cache, H=None, H8=None, h_scale=None,
                              stream=None):
-    """tabed_draft_body_step over an 8-bit cache (CacheQ8 with `layers`), writing H (bf16), H8 and h_scale (int8), or all three."""
+    """tabed_draft_body_step over an 8-bit cache (CacheQ8 with `layers`), writing H (bf16), H8 and h_scale (int8), or all three.  Faster from about
+    32 rows on; with fewer it saves memory, not time."""
     _prepare_draft_body_step_q8(bcfg, weights, ws, rows, token_src, token_stride, rows_per_token, ctx_len, cache, H, H8, h_scale, stream)()
 
 
