@@ -28,6 +28,8 @@
  *   tabed_norm_q8, tabed_linear_q8,                The draft side in 8 bits: norm, product, key / value cache and
  *   tabed_cache_append_q8, tabed_attention_q8      the attention over it; a draft step and a body step of them:
  *   tabed_draft_step_q8, tabed_draft_body_step_q8
+ *   tabed_cache_append_nodes, tabed_attention_nodes,   A tree of drafted tokens of any shape: its keys and values into a paged cache,
+ *   tabed_verify_nodes, tabed_cache_keep_nodes         the attention over it, its verification, the accepted path kept.
  *
  * Notation: n = number of drafting methods (the paper's m), B independent
  * sequences, V vocabulary size, d draft hidden size, gamma block length,
@@ -460,6 +462,129 @@ int tabed_draft_body_step_q8(const tabed_body_cfg* cfg, const tabed_body_weights
                              float* h_scale, void* stream);
 
 /*
+ * Trees of drafted tokens of any shape: the forward pass of a model over the nodes of a tree, and the tree's verification.  (The token tree above
+ * has candidates that only its trunk continues, and takes the target's logits as given.)
+ *
+ * A tree has up to TABED_MAX_NODES nodes, in an order in which parents come before their children.  Node 0 is the last token emitted, which the cache does
+ * not hold yet; the others are drafted tokens.
+ *   parents  [rows,N] int32 in   the node that node j follows, below j; anything else makes j a root of its own (node 0: -1).  NULL: chains, node j follows j - 1
+ *   n_nodes  [rows] int32 in     nodes of a row's tree, clamped to 0 .. N; NULL: N
+ * In the cache node j has position ctx_len[r] + j, in its own order of things position ctx_len[r] + the number of nodes above it.  It sees the positions
+ * before ctx_len[r], the nodes above it, and itself.  A ctx_len below 0 counts as 0.
+ *
+ * The cache: a pool of blocks of TABED_CACHE_BLOCK tokens in every layer and for every row a table of the blocks that hold its tokens, one table for
+ * all layers; position p is in entry p / TABED_CACHE_BLOCK.  Rows may share full blocks; the blocks that nodes are written to belong to one row.  A table
+ * entry outside [0, blocks) is no block: its positions are not there.
+ *   k, v           entry of (layer, block, head, token): head_dim values that lie side by side, at layer * layer_stride + block * block_stride +
+ *                  head * head_stride + token * tok_stride elements; entries must not overlap.  Every stride is at least head_dim and a multiple of 16 bytes.
+ *                  (The caches of tabed_draft_body_step are one, for a max_ctx that is a multiple of 64: blocks of a row side by side, block_stride 64 d,
+ *                  tok_stride d, head_stride head_dim.)
+ *   kscale, vscale [layers, blocks, kv_heads, 64] fp32, type 2 only: a value is e4m3 * scale, with a scale of 1/448 of the largest magnitude of the
+ *                  token in the head, so that a token can be moved without loss; the scale is 0, with all values 0, where no magnitude reaches 2^-100, and
+ *                  NaN, with all values 0, where some value is not finite.  Values are the division x / scale, rounded to even.
+ *   table          [rows, max_blocks] int32
+ * A HOST struct of device pointers; k and v 16-byte aligned.
+ */
+#define TABED_MAX_NODES 256
+typedef struct tabed_cache_paged {
+    int32_t layers;     /* 1..1024                                   */
+    int32_t kv_heads;   /* 1..1024                                   */
+    int32_t head_dim;   /* 32, 64, 96, 128 or 256                    */
+    int32_t blocks;     /* of the pool, >= 1                         */
+    int32_t max_blocks; /* entries of a row of the table, 1..2^24    */
+    int32_t type;       /* of k and v: 1 = bf16, 2 = e4m3 (8 bits, largest value 448) with scales */
+    int64_t layer_stride;
+    int64_t block_stride;
+    int64_t head_stride;
+    int64_t tok_stride;
+    void* k;
+    void* v;
+    float* kscale;
+    float* vscale;
+    const int32_t* table;
+} tabed_cache_paged;
+
+/*
+ * tabed_cache_append_nodes: rotates the queries and keys of a tree's nodes and writes keys and values into the cache.
+ *   layer        0 .. layers - 1
+ *   k, v         [rows,N,kv_heads,head_dim] dtype in; kv_row_stride, kv_tok_stride: of a row and of a node; a node's heads lie side by side
+ *   q            [rows,N,q_heads,head_dim] dtype in, q_out the same in bf16 out, each with strides of its own; both NULL: no queries.  q_out may be q itself
+ *                (dtype 1, the same strides)
+ *   rope_theta   rotary base: pairs (i, i + head_dim/2) turn by position * rope_theta^(-2 i / head_dim), the angles in 64 bits; 0: nothing turns
+ * What is turned is rounded once, to bf16 or to e4m3; dtype 0 = fp32, 1 = bf16.  Nodes from n_nodes[r] on are not written, in q_out neither; keys and values whose
+ * position is past the table, or in no block, are dropped.  Calling again with the same arguments changes nothing (unless q_out is q).
+ */
+int tabed_cache_append_nodes(const tabed_cache_paged* cache, int32_t layer, int32_t rows, int32_t N, int32_t dtype, const void* k, const void* v,
+                             int64_t kv_row_stride, int64_t kv_tok_stride, int32_t q_heads, const void* q, int64_t q_row_stride, int64_t q_tok_stride,
+                             void* q_out, int64_t out_row_stride, int64_t out_tok_stride, const int32_t* ctx_len, const int32_t* parents,
+                             const int32_t* n_nodes, float rope_theta, void* stream);
+
+/*
+ * tabed_attention_nodes: attention of a tree's nodes over the cache, in which they are already (tabed_cache_append_nodes with the same ctx_len, parents
+ * and n_nodes).  Query head i reads key / value head i / (q_heads / kv_heads).
+ *   q, out  [rows,N,q_heads,head_dim] bf16, strides of a row and of a node each
+ *   lse     [rows,N,q_heads] fp32 out, optional: natural logarithm of the sum of exp(scale * score)
+ *   scale   > 0, commonly 1 / sqrt(head_dim)
+ * Products of bf16 (and e4m3) values are exact, their sums, the softmax and its sum are in fp32; probabilities (with e4m3 values: times the values' scales)
+ * are rounded to bf16 before the product with the values.  What a node does not see has no influence, whatever it holds.  A node that
+ * sees nothing (its blocks are not there) gets zeros and an lse of -inf.  Entries of nodes from n_nodes[r] on are left as they were.
+ * q_heads is a multiple of kv_heads, at most 16384.
+ * `ws`: tabed_attention_nodes_workspace_bytes bytes, prepared once by ..._init; it then serves calls of any sizes and caches that need no more bytes.
+ * Calls that share a workspace must not overlap.
+ */
+size_t tabed_attention_nodes_workspace_bytes(const tabed_cache_paged* cache, int32_t rows, int32_t N, int32_t q_heads);   /* 0: invalid */
+int tabed_attention_nodes_workspace_init(const tabed_cache_paged* cache, int32_t rows, int32_t N, int32_t q_heads, void* ws, void* stream);
+int tabed_attention_nodes(const tabed_cache_paged* cache, int32_t layer, void* ws, int32_t rows, int32_t N, int32_t q_heads, const void* q,
+                          int64_t q_row_stride, int64_t q_tok_stride, const int32_t* ctx_len, const int32_t* parents, const int32_t* n_nodes, float scale,
+                          void* out, int64_t out_row_stride, int64_t out_tok_stride, float* lse, void* stream);
+
+/*
+ * tabed_verify_nodes: verification of a tree by multi-round rejection sampling, from its root down.  At a node, with p the target's distribution
+ * there and q = sum_j w_j q^(j) the mixture that its children were drawn from (independently, in index order):  f_0 = p, Z_0 = 1; child c is accepted iff
+ * u_c q(y_c) Z_c < f_c(y_c), and the walk goes on there; else f_{c+1} = max(0, f_c / Z_c - q), Z_{c+1} = sum f_{c+1}, and the next child is tried.  Where no child
+ * is accepted, or there is none, one more token is drawn from f / Z: the smallest v with sum_{v' <= v} f(v') > u Z.  An f without mass is replaced by p for that
+ * draw and flagged.  Greedy rows: a child is accepted iff it is arg-max p; else that arg-max is the token.  The emitted sequence is distributed as the
+ * target's.  A chain of N = gamma + 1 nodes is verified as tabed_verify does it.  Decisions are in fp64.
+ *   cfg           V, n, B, gamma, distance, policy and seed are read
+ *   target_logits [B,N,V] fp32 in   target's logits after every node
+ *   draft_logits  [N,B,n,V] fp32, draft_lse [N,B,n] fp64 in   of the drafts after every node, slot j as tabed_draft_step writes slot pos; only those of
+ *                 nodes that have children are read
+ *   tokens        [B,N] int32 in    the nodes' tokens (node 0's is not read); a token outside [0,V) is rejected and flagged TABED_FLAG_DEGENERATE
+ *   node_q        [B,N] fp32 in     q(token) in the mixture of the node's parent (node 0's is not read), as draft_q of tabed_draft_step, sib_q
+ *   parents, n_nodes   as above, rows = B; a root other than node 0 is not reached.  A row without nodes emits nothing
+ *   weights [B,n], temperature [B]  as passed to the draft steps
+ *   u_acc         [B,N] fp32 in     optional uniforms of the nodes' tests (node 0's is not read); NULL: word 1 of the Philox block of counter (round, b, j - 1)
+ *   u_res         [B] fp32 in       optional uniform of the last draw; NULL: word 0 of the block of counter (round, b, N - 1)
+ *   path          [B,N] int32 out   node 0 and the nodes accepted, in order, then -1: what tabed_cache_keep_nodes takes
+ *   n_path        [B] int32 out     nodes of the path = tokens emitted
+ *   out_tokens    [B,N] int32 out   tokens of the nodes accepted, the one token drawn, then -1
+ *   flags         [B,N] uint8 out   of the test of node j; entry 0: of the last draw; 0 for nodes that were not tested.  Greedy decisions compare
+ *                 fp32 inputs and are never near ties
+ *   dev           [B,gamma,n] fp32 out   D(p, q^(j)) at the path's nodes that have children, the first gamma of them; other entries are left as they were
+ *   n_valid       [B] int32 out     how many: what tabed_update_weights takes.  dev and n_valid may both be NULL.  cfg->distance 0 or 1 and policies other
+ *                 than the grid (2) then; else TABED_EUNSUPPORTED
+ * `ws`: tabed_verify_nodes_workspace_bytes bytes, prepared once by ..._init; it then serves calls of any sizes that need no more bytes.  It belongs to the
+ * library from the preparation on; calls that share it must not overlap.
+ */
+size_t tabed_verify_nodes_workspace_bytes(const tabed_cfg* cfg, int32_t N);   /* 0: invalid */
+int tabed_verify_nodes_workspace_init(const tabed_cfg* cfg, int32_t N, void* ws, void* stream);
+int tabed_verify_nodes(const tabed_cfg* cfg, void* ws, uint64_t round, int32_t N, const float* target_logits, const float* draft_logits,
+                       const double* draft_lse, const int32_t* tokens, const float* node_q, const int32_t* parents, const int32_t* n_nodes,
+                       const float* weights, const float* temperature, const float* u_acc, const float* u_res, int32_t* path, int32_t* n_path,
+                       int32_t* out_tokens, uint8_t* flags, float* dev, int32_t* n_valid, void* stream);
+
+/*
+ * tabed_cache_keep_nodes: after verification the cache keeps the path: in all layers the entry of position ctx_base[r] + path[r][i] moves to
+ * ctx_base[r] + i, and ctx_len[r] = ctx_base[r] + the number of nodes kept.
+ *   path    [rows,N] int32 in   ascending nodes (path[r][0] = 0 as a rule); the path ends where an entry is not above the one before it, or not below N
+ *   n_path  [rows] int32 in     entries of the path, clamped to 0 .. N
+ *   ctx_len [rows] int32 out    must not be ctx_base
+ * Entries whose source or destination is past the table or in no block are not moved (the positions count all the same).
+ */
+int tabed_cache_keep_nodes(const tabed_cache_paged* cache, int32_t rows, int32_t N, const int32_t* ctx_base, const int32_t* path, const int32_t* n_path,
+                           int32_t* ctx_len, void* stream);
+
+/*
  * The uniforms tabed_draft_step and tabed_verify would draw: out[b,pos,word] for b < B,
  * pos <= gamma, word in {0,1}.  out is [B,gamma+1,2] fp32.
  */
@@ -478,8 +603,8 @@ int tabed_philox_uniforms(const tabed_cfg* cfg, uint64_t round, float* out, void
 #define TABED_K_RESID 3   /* corrected / bonus token            */
 #define TABED_K_WEIGHTS 4 /* window + weights                   */
 #define TABED_K_DIST 5    /* the launch that holds total variation (RESID's) or hard labels (STATS'), counted there too */
-#define TABED_K_TREE 6    /* token tree: the first pass of the walk (the second, of width 3, is not timed) */
-#define TABED_K_BODY 7    /* draft-model body: every kernel of tabed_draft_body_step and ..._q8; the 8-bit operators called by themselves */
+#define TABED_K_TREE 6    /* token tree: the first pass of the walk (the second, of width 3, is not timed); tabed_verify_nodes */
+#define TABED_K_BODY 7    /* draft-model body: every kernel of tabed_draft_body_step and ..._q8; the 8-bit operators and those of a tree's nodes called by themselves */
 #define TABED_K_NULL 8    /* empty kernel, see tabed_prof_null  */
 #define TABED_K_COUNT 9
 int tabed_prof_enable(int on);

@@ -19,6 +19,8 @@ EXPORTS = [
     "tabed_norm_q8", "tabed_linear_q8", "tabed_cache_append_q8",
     "tabed_attention_q8", "tabed_attention_q8_workspace_bytes", "tabed_attention_q8_workspace_init",
     "tabed_draft_step_q8", "tabed_body_q8_workspace_bytes", "tabed_body_q8_workspace_init", "tabed_draft_body_step_q8",
+    "tabed_cache_append_nodes", "tabed_attention_nodes", "tabed_attention_nodes_workspace_bytes", "tabed_attention_nodes_workspace_init",
+    "tabed_verify_nodes", "tabed_verify_nodes_workspace_bytes", "tabed_verify_nodes_workspace_init", "tabed_cache_keep_nodes",
     "tabed_prof_enable", "tabed_prof_read", "tabed_prof_reset", "tabed_kernel_name", "tabed_prof_null",
 ]
 
@@ -50,6 +52,13 @@ class TabedCacheQ8(C.Structure):
     """Mirror of `tabed_cache_q8`."""
     _fields_ = [("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("blocks", C.c_int32), ("max_blocks", C.c_int32),
                 ("k", C.c_void_p), ("v", C.c_void_p), ("kscale", C.c_void_p), ("vscale", C.c_void_p), ("table", C.c_void_p)]
+
+
+class TabedCachePaged(C.Structure):
+    """Mirror of `tabed_cache_paged`."""
+    _fields_ = [(name, C.c_int32) for name in ("layers", "kv_heads", "head_dim", "blocks", "max_blocks", "type")] + [
+        (name, C.c_int64) for name in ("layer_stride", "block_stride", "head_stride", "tok_stride")] + [
+        (name, C.c_void_p) for name in ("k", "v", "kscale", "vscale", "table")]
 
 
 class TabedError(RuntimeError):
@@ -123,6 +132,23 @@ def load():
     lib.tabed_body_q8_workspace_init.argtypes = [bcfgp, cachep, i32, vp, vp]
     lib.tabed_draft_body_step_q8.restype = C.c_int
     lib.tabed_draft_body_step_q8.argtypes = [bcfgp, C.POINTER(TabedBodyWeights), vp, i32, vp, i32, i32, vp, cachep] + [vp] * 4
+    pagedp = C.POINTER(TabedCachePaged)
+    lib.tabed_cache_append_nodes.restype = C.c_int
+    lib.tabed_cache_append_nodes.argtypes = [pagedp, i32, i32, i32, i32, vp, vp, i64, i64, i32, vp, i64, i64, vp, i64, i64, vp, vp, vp, f32, vp]
+    lib.tabed_attention_nodes_workspace_bytes.restype = C.c_size_t
+    lib.tabed_attention_nodes_workspace_bytes.argtypes = [pagedp, i32, i32, i32]
+    lib.tabed_attention_nodes_workspace_init.restype = C.c_int
+    lib.tabed_attention_nodes_workspace_init.argtypes = [pagedp, i32, i32, i32, vp, vp]
+    lib.tabed_attention_nodes.restype = C.c_int
+    lib.tabed_attention_nodes.argtypes = [pagedp, i32, vp, i32, i32, i32, vp, i64, i64, vp, vp, vp, f32, vp, i64, i64, vp, vp]
+    lib.tabed_verify_nodes_workspace_bytes.restype = C.c_size_t
+    lib.tabed_verify_nodes_workspace_bytes.argtypes = [cfgp, i32]
+    lib.tabed_verify_nodes_workspace_init.restype = C.c_int
+    lib.tabed_verify_nodes_workspace_init.argtypes = [cfgp, i32, vp, vp]
+    lib.tabed_verify_nodes.restype = C.c_int
+    lib.tabed_verify_nodes.argtypes = [cfgp, vp, u64, i32] + [vp] * 18
+    lib.tabed_cache_keep_nodes.restype = C.c_int
+    lib.tabed_cache_keep_nodes.argtypes = [pagedp, i32, i32] + [vp] * 5
     lib.tabed_prof_enable.restype = C.c_int
     lib.tabed_prof_enable.argtypes = [C.c_int]
     lib.tabed_prof_read.restype = C.c_int
@@ -801,6 +827,263 @@ def tabed_draft_body_step_q8(bcfg, weights, ws, rows, token_src, token_stride, r
     """tabed_draft_body_step over an 8-bit cache (CacheQ8 with `layers`), writing H (bf16), H8 and h_scale (int8), or all three.  Faster from about
     32 rows on; with fewer it saves memory, not time."""
     _prepare_draft_body_step_q8(bcfg, weights, ws, rows, token_src, token_stride, rows_per_token, ctx_len, cache, H, H8, h_scale, stream)()
+
+
+# ------------------------------------------------------------------ trees given by parents
+MAX_NODES = 256
+
+
+class CachePaged:
+    """Paged key / value cache over tensors of the caller's: k, v [(layers,) blocks, kv_heads, 64, head_dim] bfloat16 or float8_e4m3fn, of the same
+    strides, with the values of a token in a head side by side; for e4m3 kscale, vscale [(layers,) blocks, kv_heads, 64] fp32; table
+    [rows, max_blocks] int32, one for all layers (entries outside [0, blocks): no block).  The struct holds the tensors' addresses: the object keeps them alive."""
+
+    def __init__(self, k, v, table, kscale=None, vscale=None):
+        import torch
+        self.device = _device_of(dict(k=k, v=v, kscale=kscale, vscale=vscale, table=table))
+        if k.dim() not in (4, 5) or k.shape[-2] != CACHE_BLOCK:
+            raise TabedError(f"k must be [(layers,) blocks, kv_heads, {CACHE_BLOCK}, head_dim], got {tuple(k.shape)}")
+        types = {torch.bfloat16: 1, torch.float8_e4m3fn: 2}
+        if k.dtype not in types:
+            raise TabedError(f"k must be bfloat16 or float8_e4m3fn, got {k.dtype}")
+        if v.dtype != k.dtype or v.shape != k.shape or table.dim() != 2:
+            raise TabedError("v must have the type and shape of k, table must be [rows, max_blocks]")
+        if any(n > 1 and x != y for n, x, y in zip(k.shape, k.stride(), v.stride())):
+            raise TabedError("k and v must have the same strides")
+        kind, k5 = types[k.dtype], k if k.dim() == 5 else k[None]
+        if 0 in k5.shape or 0 in table.shape or max(*k5.shape, *table.shape) >= 1 << 31:
+            raise TabedError("a cache's sizes must not be 0, and fit 32 bits")
+        layers, blocks, kvh, _, hd = k5.shape
+        if hd > 1 and k5.stride(4) != 1:
+            raise TabedError("k and v: the values of a token in a head must lie side by side")
+        # Strides that lead nowhere do not count; the others must keep entries apart.
+        strides, reach = [0] * 4, hd
+        for i in sorted((i for i in range(4) if k5.shape[i] > 1), key=lambda i: k5.stride(i)):
+            if k5.stride(i) < reach:
+                raise TabedError("k and v: entries overlap")
+            strides[i], reach = k5.stride(i), k5.stride(i) * k5.shape[i]
+        piece = 16 // k.element_size()
+        strides = [x if x else (hd + piece - 1) // piece * piece for x in strides]
+        if (kscale is None) != (vscale is None) or (kscale is None) != (kind == 1):
+            raise TabedError("kscale and vscale go with e4m3, and with it alone")
+        self.layers, self.rows, self.kv_heads, self.head_dim = layers, table.shape[0], kvh, hd
+        self.k, self.v, self.kscale, self.vscale, self.table = k, v, kscale, vscale, table
+        count = layers * blocks * kvh * CACHE_BLOCK
+        self.struct = TabedCachePaged(layers, kvh, hd, blocks, table.shape[1], kind, *strides, k.data_ptr(), v.data_ptr(),
+                                      _ptr(kscale, torch.float32, count, "kscale"), _ptr(vscale, torch.float32, count, "vscale"),
+                                      _ptr(table, torch.int32, None, "table"))
+
+    @classmethod
+    def allocate(cls, rows, tokens, kv_heads, head_dim, layers=1, dtype=None, device="cuda:0"):
+        """An empty cache with room for `tokens` tokens in every row, blocks dealt to the rows in order; dtype: bfloat16 (None) or float8_e4m3fn."""
+        import torch
+        dtype = torch.bfloat16 if dtype is None else dtype
+        width = (tokens + CACHE_BLOCK - 1) // CACHE_BLOCK
+        k = torch.zeros((layers, rows * width, kv_heads, CACHE_BLOCK, head_dim), dtype=dtype, device=device)
+        ks = torch.zeros(k.shape[:-1], dtype=torch.float32, device=device) if dtype != torch.bfloat16 else None
+        table = torch.arange(rows * width, dtype=torch.int32, device=device).view(rows, width)
+        return cls(k, torch.zeros_like(k), table, ks, None if ks is None else torch.zeros_like(ks))
+
+    @classmethod
+    def of_body(cls, kcache, vcache, heads):
+        """The caches of tabed_draft_body_step, [layers, rows, max_ctx, d] with max_ctx a multiple of 64, seen as a paged one."""
+        import torch
+        if kcache.dim() != 4 or kcache.shape[2] % CACHE_BLOCK or kcache.shape[3] % heads or not kcache.is_contiguous() or not vcache.is_contiguous():
+            raise TabedError(f"kcache and vcache must be contiguous [layers, rows, max_ctx, d], max_ctx a multiple of {CACHE_BLOCK}, got {tuple(kcache.shape)}")
+        layers, rows, ctx, d = kcache.shape
+        k, v = (x.view(layers, rows * ctx // CACHE_BLOCK, CACHE_BLOCK, heads, d // heads).transpose(2, 3) for x in (kcache, vcache))
+        table = torch.arange(rows * ctx // CACHE_BLOCK, dtype=torch.int32, device=kcache.device).view(rows, ctx // CACHE_BLOCK)
+        return cls(k, v, table)
+
+
+def _tree_args(rows, N, parents, n_nodes):
+    import torch
+    if parents is not None and tuple(parents.shape) != (rows, N):
+        raise TabedError(f"parents must be [{rows}, {N}], got {tuple(parents.shape)}")
+    return _ptr(parents, torch.int32, rows * N, "parents"), _ptr(n_nodes, torch.int32, rows, "n_nodes")
+
+
+def _prepare_cache_append_nodes(cache, k, v, ctx_len, parents, n_nodes, q, q_out, rope_theta, layer, stream):
+    import torch
+    dev = _device_of({"cache": cache.k, "k": k, "v": v, "ctx_len": ctx_len, "parents": parents, "n_nodes": n_nodes, "q": q, "q_out": q_out})
+    hd = cache.head_dim
+    N = _new_tokens(k, cache.kv_heads, hd)
+    kp, row, tok = _heads_view(k, cache.rows, N, cache.kv_heads, hd, "k")
+    vp_, vrow, vtok = _heads_view(v, cache.rows, N, cache.kv_heads, hd, "v")
+    if (row, tok) != (vrow, vtok) or k.dtype != v.dtype:
+        raise TabedError("k and v must have the same type and strides")
+    heads, qp, qrow, qtok, op, orow, otok = 0, None, 0, 0, None, 0, 0
+    if (q is None) != (q_out is None):
+        raise TabedError("q and q_out go together")
+    if q is not None:
+        heads = q.shape[2] if q.dim() == 4 else q.shape[-1] // hd
+        if q.dtype != k.dtype or q_out.dtype != torch.bfloat16:
+            raise TabedError("q must have the type of k, q_out must be bfloat16")
+        qp, qrow, qtok = _heads_view(q, cache.rows, N, heads, hd, "q")
+        op, orow, otok = _heads_view(q_out, cache.rows, N, heads, hd, "q_out")
+    pp, np_ = _tree_args(cache.rows, N, parents, n_nodes)
+    args = [C.byref(cache.struct), layer, cache.rows, N, _storage_type(k, "k"), kp, vp_, row, tok, heads, qp, qrow, qtok, op, orow, otok,
+            _ptr(ctx_len, torch.int32, cache.rows, "ctx_len"), pp, np_, rope_theta, _stream_on(dev, stream)]
+    return DeviceCall(load().tabed_cache_append_nodes, args, "tabed_cache_append_nodes", dev, (cache, k, v, ctx_len, parents, n_nodes, q, q_out))
+
+
+def tabed_cache_append_nodes(cache: CachePaged, k, v, ctx_len, parents=None, n_nodes=None, q=None, q_out=None, rope_theta=0.0, layer=0, stream=None):
+    """Writes k, v [rows, N, kv_heads, head_dim] of a tree's nodes into the cache at positions ctx_len[r] + j, turned (with rope_theta > 0) by
+    ctx_len[r] + the node's depth, and q [rows, N, q_heads, head_dim], turned likewise, to q_out (bfloat16).  parents [rows, N] (None: chains), n_nodes [rows]."""
+    _prepare_cache_append_nodes(cache, k, v, ctx_len, parents, n_nodes, q, q_out, rope_theta, layer, stream)()
+
+
+def prepare_cache_append_nodes(cache: CachePaged, k, v, ctx_len, parents=None, n_nodes=None, q=None, q_out=None, rope_theta=0.0, layer=0,
+                               stream=None) -> PreparedCall:
+    return _prepare_cache_append_nodes(cache, k, v, ctx_len, parents, n_nodes, q, q_out, rope_theta, layer, stream)
+
+
+def tabed_attention_nodes_workspace_bytes(cache: CachePaged, rows, N, q_heads) -> int:
+    return int(load().tabed_attention_nodes_workspace_bytes(C.byref(cache.struct), rows, N, q_heads))
+
+
+def tabed_attention_nodes_workspace_init(cache: CachePaged, rows, N, q_heads, ws, stream=None):
+    import torch
+    dev = _device_of(dict(cache=cache.k, ws=ws))
+    need = tabed_attention_nodes_workspace_bytes(cache, rows, N, q_heads)
+    if need == 0 or ws.numel() * ws.element_size() < need:
+        raise TabedError(f"attention workspace holds {ws.numel() * ws.element_size()} bytes, {need} needed (0: invalid sizes)")
+    with torch.cuda.device(dev):
+        _check(load().tabed_attention_nodes_workspace_init(C.byref(cache.struct), rows, N, q_heads, _ptr(ws, torch.uint8, None, "ws"),
+                                                           _stream_on(dev, stream)), "tabed_attention_nodes_workspace_init")
+
+
+def new_attention_nodes_workspace(cache: CachePaged, rows, N, q_heads, stream=None):
+    """Allocate (torch) and prepare the workspace of tabed_attention_nodes for these sizes, or others that need no more bytes."""
+    import torch
+    nbytes = tabed_attention_nodes_workspace_bytes(cache, rows, N, q_heads)
+    if nbytes == 0:
+        raise TabedError("invalid or unsupported attention sizes")
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=cache.k.device)
+    tabed_attention_nodes_workspace_init(cache, rows, N, q_heads, ws, stream)
+    return ws
+
+
+def _prepare_attention_nodes(cache, ws, q, ctx_len, out, parents, n_nodes, scale, lse, layer, stream):
+    import torch
+    dev = _device_of(dict(cache=cache.k, ws=ws, q=q, ctx_len=ctx_len, out=out, parents=parents, n_nodes=n_nodes, lse=lse))
+    hd = cache.head_dim
+    N = _new_tokens(q, None, hd)
+    heads = q.shape[2] if q.dim() == 4 else q.shape[-1] // hd
+    if q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16:
+        raise TabedError(f"q and out must be bfloat16, got {q.dtype}, {out.dtype}")
+    qp, qrow, qtok = _heads_view(q, cache.rows, N, heads, hd, "q")
+    op, orow, otok = _heads_view(out, cache.rows, N, heads, hd, "out")
+    need = tabed_attention_nodes_workspace_bytes(cache, cache.rows, N, heads)
+    if ws.numel() * ws.element_size() < need:
+        raise TabedError(f"attention workspace holds {ws.numel() * ws.element_size()} bytes, {need} needed")
+    pp, np_ = _tree_args(cache.rows, N, parents, n_nodes)
+    args = [C.byref(cache.struct), layer, _ptr(ws, torch.uint8, None, "ws"), cache.rows, N, heads, qp, qrow, qtok,
+            _ptr(ctx_len, torch.int32, cache.rows, "ctx_len"), pp, np_, hd ** -0.5 if scale is None else scale, op, orow, otok,
+            _ptr(lse, torch.float32, cache.rows * N * heads, "lse"), _stream_on(dev, stream)]
+    return DeviceCall(load().tabed_attention_nodes, args, "tabed_attention_nodes", dev, (cache, ws, q, ctx_len, out, parents, n_nodes, lse))
+
+
+def tabed_attention_nodes(cache: CachePaged, ws, q, ctx_len, out, parents=None, n_nodes=None, scale=None, lse=None, layer=0, stream=None):
+    """out [rows, N, q_heads, head_dim]: attention of a tree's nodes over the cache: node j sees the positions before ctx_len[r], the nodes above it and
+    itself, which tabed_cache_append_nodes has written.  scale: 1 / sqrt(head_dim) unless given; lse [rows, N, q_heads]: optional."""
+    _prepare_attention_nodes(cache, ws, q, ctx_len, out, parents, n_nodes, scale, lse, layer, stream)()
+
+
+def prepare_attention_nodes(cache: CachePaged, ws, q, ctx_len, out, parents=None, n_nodes=None, scale=None, lse=None, layer=0, stream=None) -> PreparedCall:
+    return _prepare_attention_nodes(cache, ws, q, ctx_len, out, parents, n_nodes, scale, lse, layer, stream)
+
+
+def tabed_verify_nodes_workspace_bytes(cfg: TabedCfg, N) -> int:
+    return int(load().tabed_verify_nodes_workspace_bytes(C.byref(cfg), N))
+
+
+def tabed_verify_nodes_workspace_init(cfg: TabedCfg, N, ws, stream=None):
+    import torch
+    dev = _device_of(dict(ws=ws))
+    need = tabed_verify_nodes_workspace_bytes(cfg, N)
+    if need == 0 or ws.numel() * ws.element_size() < need:
+        raise TabedError(f"verification workspace holds {ws.numel() * ws.element_size()} bytes, {need} needed (0: invalid sizes)")
+    with torch.cuda.device(dev):
+        _check(load().tabed_verify_nodes_workspace_init(C.byref(cfg), N, _ptr(ws, torch.uint8, None, "ws"), _stream_on(dev, stream)),
+               "tabed_verify_nodes_workspace_init")
+
+
+def new_verify_nodes_workspace(cfg: TabedCfg, N, device="cuda:0", stream=None):
+    """Allocate (torch) and prepare the workspace of tabed_verify_nodes for these sizes, or others that need no more bytes."""
+    import torch
+    nbytes = tabed_verify_nodes_workspace_bytes(cfg, N)
+    if nbytes == 0:
+        raise TabedError("invalid or unsupported verification sizes")
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    tabed_verify_nodes_workspace_init(cfg, N, ws, stream)
+    return ws
+
+
+def _prepare_verify_nodes(cfg, ws, rnd, target_logits, draft_logits, draft_lse, tokens, node_q, weights, temperature, path, n_path, out_tokens, flags,
+                          parents, n_nodes, u_acc, u_res, dev, n_valid, stream):
+    import torch
+    index = _device_of(dict(ws=ws, target_logits=target_logits, draft_logits=draft_logits, draft_lse=draft_lse, tokens=tokens, node_q=node_q, weights=weights,
+                            temperature=temperature, path=path, n_path=n_path, out_tokens=out_tokens, flags=flags, parents=parents, n_nodes=n_nodes,
+                            u_acc=u_acc, u_res=u_res, dev=dev, n_valid=n_valid))
+    if tokens.dim() != 2 or tokens.shape[0] != cfg.B:
+        raise TabedError(f"tokens must be [{cfg.B}, N], got {tuple(tokens.shape)}")
+    B, N, V, n = cfg.B, tokens.shape[1], cfg.V, cfg.n
+    slots = draft_logits.shape[0]                        # (slots behind the last node with children may be missing)
+    if tuple(draft_logits.shape) != (slots, B, n, V) or tuple(draft_lse.shape) != (slots, B, n) or not (slots >= N or (parents is None and slots == N - 1)):
+        raise TabedError(f"draft_logits and draft_lse must be [{N}, {B}, {n}, {V}] and [{N}, {B}, {n}], got {tuple(draft_logits.shape)}, {tuple(draft_lse.shape)}")
+    need = tabed_verify_nodes_workspace_bytes(cfg, N)
+    if ws.numel() * ws.element_size() < need:
+        raise TabedError(f"verification workspace holds {ws.numel() * ws.element_size()} bytes, {need} needed")
+    f, i = torch.float32, torch.int32
+    pp, np_ = _tree_args(B, N, parents, n_nodes)
+    vp = C.c_void_p
+    args = [C.byref(cfg), vp(_ptr(ws, torch.uint8, None, "ws")), C.c_uint64(rnd), C.c_int32(N), vp(_ptr(target_logits, f, B * N * V, "target_logits")),
+            vp(_ptr(draft_logits, f, None, "draft_logits")), vp(_ptr(draft_lse, torch.float64, None, "draft_lse")), vp(_ptr(tokens, i, B * N, "tokens")),
+            vp(_ptr(node_q, f, B * N, "node_q")), vp(pp), vp(np_), vp(_ptr(weights, f, B * n, "weights")), vp(_ptr(temperature, f, B, "temperature")),
+            vp(_ptr(u_acc, f, B * N, "u_acc")), vp(_ptr(u_res, f, B, "u_res")), vp(_ptr(path, i, B * N, "path")), vp(_ptr(n_path, i, B, "n_path")),
+            vp(_ptr(out_tokens, i, B * N, "out_tokens")), vp(_ptr(flags, torch.uint8, B * N, "flags")), vp(_ptr(dev, f, B * cfg.gamma * n, "dev")),
+            vp(_ptr(n_valid, i, B, "n_valid")), vp(_stream_on(index, stream))]
+    call = DeviceCall(load().tabed_verify_nodes, args, "tabed_verify_nodes", index,
+                      (cfg, ws, target_logits, draft_logits, draft_lse, tokens, node_q, weights, temperature, path, n_path, out_tokens, flags, parents,
+                       n_nodes, u_acc, u_res, dev, n_valid))
+    call.round_arg = args[2]
+    return call
+
+
+def tabed_verify_nodes(cfg, ws, rnd, target_logits, draft_logits, draft_lse, tokens, node_q, weights, temperature, path, n_path, out_tokens, flags,
+                       parents=None, n_nodes=None, u_acc=None, u_res=None, dev=None, n_valid=None, stream=None):
+    """Verification of a tree of drafted tokens by multi-round rejection sampling: target_logits [B, N, V], draft_logits [N, B, n, V] and draft_lse [N, B, n]
+    as the draft steps write them, tokens and node_q [B, N].  path, out_tokens, flags [B, N], n_path [B]; dev [B, gamma, n] and n_valid [B] for tabed_update_weights."""
+    _prepare_verify_nodes(cfg, ws, rnd, target_logits, draft_logits, draft_lse, tokens, node_q, weights, temperature, path, n_path, out_tokens, flags,
+                          parents, n_nodes, u_acc, u_res, dev, n_valid, stream)()
+
+
+def prepare_verify_nodes(cfg, ws, rnd, target_logits, draft_logits, draft_lse, tokens, node_q, weights, temperature, path, n_path, out_tokens, flags,
+                         parents=None, n_nodes=None, u_acc=None, u_res=None, dev=None, n_valid=None, stream=None) -> PreparedCall:
+    return _prepare_verify_nodes(cfg, ws, rnd, target_logits, draft_logits, draft_lse, tokens, node_q, weights, temperature, path, n_path, out_tokens, flags,
+                                 parents, n_nodes, u_acc, u_res, dev, n_valid, stream)
+
+
+def _prepare_cache_keep_nodes(cache, ctx_base, path, n_path, ctx_len, stream):
+    import torch
+    dev = _device_of(dict(cache=cache.k, ctx_base=ctx_base, path=path, n_path=n_path, ctx_len=ctx_len))
+    if path.dim() != 2 or path.shape[0] != cache.rows:
+        raise TabedError(f"path must be [{cache.rows}, N], got {tuple(path.shape)}")
+    N = path.shape[1]
+    args = [C.byref(cache.struct), cache.rows, N, _ptr(ctx_base, torch.int32, cache.rows, "ctx_base"), _ptr(path, torch.int32, cache.rows * N, "path"),
+            _ptr(n_path, torch.int32, cache.rows, "n_path"), _ptr(ctx_len, torch.int32, cache.rows, "ctx_len"), _stream_on(dev, stream)]
+    return DeviceCall(load().tabed_cache_keep_nodes, args, "tabed_cache_keep_nodes", dev, (cache, ctx_base, path, n_path, ctx_len))
+
+
+def tabed_cache_keep_nodes(cache: CachePaged, ctx_base, path, n_path, ctx_len, stream=None):
+    """After verification: in all layers the entries of positions ctx_base[r] + path[r][i] move to ctx_base[r] + i, i < n_path[r]; ctx_len[r] becomes
+    ctx_base[r] + their number."""
+    _prepare_cache_keep_nodes(cache, ctx_base, path, n_path, ctx_len, stream)()
+
+
+def prepare_cache_keep_nodes(cache: CachePaged, ctx_base, path, n_path, ctx_len, stream=None) -> PreparedCall:
+    return _prepare_cache_keep_nodes(cache, ctx_base, path, n_path, ctx_len, stream)
 
 
 class BodyBuffers:

@@ -121,6 +121,22 @@ static int validate_cache(const tabed_cache_q8* c, bool pointers) {
     return TABED_OK;
 }
 
+static int validate_paged(const tabed_cache_paged* c, bool pointers) {
+    if (c == nullptr) return TABED_ENULL;
+    if (c->layers < 1 || c->layers > 1024 || c->kv_heads < 1 || c->kv_heads > 1024 || c->blocks < 1 || c->max_blocks < 1 || c->max_blocks > (1 << 24))
+        return TABED_ERANGE;
+    if (c->head_dim != 32 && c->head_dim != 64 && c->head_dim != 96 && c->head_dim != 128 && c->head_dim != 256) return TABED_EINVAL;
+    if (c->type != 1 && c->type != 2) return TABED_EINVAL;
+    const int64_t piece = c->type == 2 ? 16 : 8;
+    for (int64_t stride : {c->layer_stride, c->block_stride, c->head_stride, c->tok_stride})
+        if (stride < c->head_dim || stride % piece != 0 || stride > (1ll << 44)) return TABED_EINVAL;
+    if (!pointers) return TABED_OK;
+    if (!c->k || !c->v || !c->table || (c->type == 2 && (!c->kscale || !c->vscale))) return TABED_ENULL;
+    if (misaligned(c->k) || misaligned(c->v) || element_misaligned(c->table, 0)) return TABED_EALIGN;
+    if (c->type == 2 && (element_misaligned(c->kscale, 0) || element_misaligned(c->vscale, 0))) return TABED_EALIGN;
+    return TABED_OK;
+}
+
 // ---------------------------------------------------------------- built-in scratch of tabed_draft_step_static
 // One array per GPU, part of the loaded code object, so no call ever allocates it.  `scratch` is only a
 // host-side handle: the array's device address on the current GPU comes from hipGetSymbolAddress, looked up once
@@ -549,6 +565,130 @@ int tabed_draft_body_step_q8(const tabed_body_cfg* cfg, const tabed_body_weights
     if (misaligned(ws) || misaligned(H) || misaligned(H8) || element_misaligned(h_scale, 0)) return TABED_EALIGN;
     const hipError_t e = launch_body_step_q8(*cfg, *weights, static_cast<char*>(ws), rows, token_src, token_stride, rows_per_token, ctx_len, *cache,
                                              static_cast<uint16_t*>(H), static_cast<int8_t*>(H8), h_scale, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? TABED_OK : fail_hip(e);
+}
+
+// ---------------------------------------------------------------- trees given by parents
+static int validate_nodes(int32_t rows, int32_t N) {
+    return rows < 1 || rows > 65535 || N < 1 || N > TABED_MAX_NODES ? TABED_ERANGE : TABED_OK;
+}
+
+int tabed_cache_append_nodes(const tabed_cache_paged* cache, int32_t layer, int32_t rows, int32_t N, int32_t dtype, const void* k, const void* v,
+                             int64_t kv_row_stride, int64_t kv_tok_stride, int32_t q_heads, const void* q, int64_t q_row_stride, int64_t q_tok_stride,
+                             void* q_out, int64_t out_row_stride, int64_t out_tok_stride, const int32_t* ctx_len, const int32_t* parents,
+                             const int32_t* n_nodes, float rope_theta, void* stream) {
+    int rc = validate_paged(cache, true);
+    if (rc == TABED_OK) rc = validate_nodes(rows, N);
+    if (rc != TABED_OK) return rc;
+    if (layer < 0 || layer >= cache->layers) return TABED_ERANGE;
+    if (!k || !v || !ctx_len || (q == nullptr) != (q_out == nullptr)) return TABED_ENULL;
+    const int64_t heads = (int64_t)cache->kv_heads * cache->head_dim;
+    if (!storage_type(dtype) || kv_row_stride < heads || kv_tok_stride < heads) return TABED_EINVAL;
+    if (!(rope_theta == 0.f || (rope_theta > 0.f && rope_theta < INFINITY))) return TABED_EINVAL;
+    if (q != nullptr) {
+        if (q_heads < 1 || q_heads > 16384) return TABED_ERANGE;
+        const int64_t qh = (int64_t)q_heads * cache->head_dim;
+        if (q_row_stride < qh || q_tok_stride < qh || out_row_stride < qh || out_tok_stride < qh) return TABED_EINVAL;
+        if (q == q_out && (dtype != 1 || q_row_stride != out_row_stride || q_tok_stride != out_tok_stride)) return TABED_EINVAL;
+    }
+    if (element_misaligned(k, dtype) || element_misaligned(v, dtype) || element_misaligned(q, dtype) || element_misaligned(q_out, 1) ||
+        element_misaligned(ctx_len, 0) || element_misaligned(parents, 0) || element_misaligned(n_nodes, 0))
+        return TABED_EALIGN;
+    const hipError_t e = launch_append_nodes(*cache, layer, rows, N, dtype, k, v, kv_row_stride, kv_tok_stride, q_heads, q, q_row_stride, q_tok_stride, q_out,
+                                             out_row_stride, out_tok_stride, ctx_len, parents, n_nodes, rope_theta, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? TABED_OK : fail_hip(e);
+}
+
+static int validate_attention_nodes(const tabed_cache_paged* cache, int32_t rows, int32_t N, int32_t q_heads, bool pointers) {
+    int rc = validate_paged(cache, pointers);
+    if (rc == TABED_OK) rc = validate_nodes(rows, N);
+    if (rc != TABED_OK) return rc;
+    if (q_heads < 1 || q_heads > 16384) return TABED_ERANGE;
+    return q_heads % cache->kv_heads != 0 ? TABED_EINVAL : TABED_OK;
+}
+
+size_t tabed_attention_nodes_workspace_bytes(const tabed_cache_paged* cache, int32_t rows, int32_t N, int32_t q_heads) {
+    if (validate_attention_nodes(cache, rows, N, q_heads, false) != TABED_OK) return 0;
+    return nodes_attn_layout(*cache, rows, N, q_heads).total;
+}
+
+int tabed_attention_nodes_workspace_init(const tabed_cache_paged* cache, int32_t rows, int32_t N, int32_t q_heads, void* ws, void* stream) {
+    const int rc = validate_attention_nodes(cache, rows, N, q_heads, false);
+    if (rc != TABED_OK) return rc;
+    if (ws == nullptr) return TABED_ENULL;
+    if (misaligned(ws)) return TABED_EALIGN;
+    const hipError_t e = launch_nodes_attn_init(static_cast<char*>(ws), static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? TABED_OK : fail_hip(e);
+}
+
+int tabed_attention_nodes(const tabed_cache_paged* cache, int32_t layer, void* ws, int32_t rows, int32_t N, int32_t q_heads, const void* q,
+                          int64_t q_row_stride, int64_t q_tok_stride, const int32_t* ctx_len, const int32_t* parents, const int32_t* n_nodes, float scale,
+                          void* out, int64_t out_row_stride, int64_t out_tok_stride, float* lse, void* stream) {
+    const int rc = validate_attention_nodes(cache, rows, N, q_heads, true);
+    if (rc != TABED_OK) return rc;
+    if (layer < 0 || layer >= cache->layers) return TABED_ERANGE;
+    if (!ws || !q || !ctx_len || !out) return TABED_ENULL;
+    const int64_t heads = (int64_t)q_heads * cache->head_dim;
+    if (!(scale > 0.f) || !(scale < INFINITY)) return TABED_EINVAL;
+    if (q_row_stride < heads || q_tok_stride < heads || out_row_stride < heads || out_tok_stride < heads) return TABED_EINVAL;
+    if (misaligned(ws) || element_misaligned(q, 1) || element_misaligned(out, 1) || element_misaligned(ctx_len, 0) || element_misaligned(parents, 0) ||
+        element_misaligned(n_nodes, 0) || element_misaligned(lse, 0))
+        return TABED_EALIGN;
+    const hipError_t e = launch_attention_nodes(*cache, layer, static_cast<char*>(ws), rows, N, q_heads, static_cast<const uint16_t*>(q), q_row_stride,
+                                                q_tok_stride, ctx_len, parents, n_nodes, scale, static_cast<uint16_t*>(out), out_row_stride,
+                                                out_tok_stride, lse, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? TABED_OK : fail_hip(e);
+}
+
+static int validate_verify_nodes(const tabed_cfg* cfg, int32_t N) {
+    int rc = validate_cfg(cfg);
+    if (rc == TABED_OK) rc = validate_nodes(cfg->B, N);
+    if (rc != TABED_OK) return rc;
+    return nodes_verify_layout(*cfg, N).G * (int64_t)cfg->B > kMaxWorkgroups ? TABED_ERANGE : TABED_OK;
+}
+
+size_t tabed_verify_nodes_workspace_bytes(const tabed_cfg* cfg, int32_t N) {
+    if (validate_verify_nodes(cfg, N) != TABED_OK) return 0;
+    return nodes_verify_layout(*cfg, N).total;
+}
+
+int tabed_verify_nodes_workspace_init(const tabed_cfg* cfg, int32_t N, void* ws, void* stream) {
+    const int rc = validate_verify_nodes(cfg, N);
+    if (rc != TABED_OK) return rc;
+    if (ws == nullptr) return TABED_ENULL;
+    if (misaligned(ws)) return TABED_EALIGN;
+    const hipError_t e = launch_nodes_verify_init(*cfg, N, static_cast<char*>(ws), static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? TABED_OK : fail_hip(e);
+}
+
+int tabed_verify_nodes(const tabed_cfg* cfg, void* ws, uint64_t round, int32_t N, const float* target_logits, const float* draft_logits,
+                       const double* draft_lse, const int32_t* tokens, const float* node_q, const int32_t* parents, const int32_t* n_nodes,
+                       const float* weights, const float* temperature, const float* u_acc, const float* u_res, int32_t* path, int32_t* n_path,
+                       int32_t* out_tokens, uint8_t* flags, float* dev, int32_t* n_valid, void* stream) {
+    const int rc = validate_verify_nodes(cfg, N);
+    if (rc != TABED_OK) return rc;
+    if (!ws || !target_logits || !draft_logits || !draft_lse || !tokens || !node_q || !weights || !temperature || !path || !n_path || !out_tokens || !flags)
+        return TABED_ENULL;
+    if ((dev == nullptr) != (n_valid == nullptr)) return TABED_ENULL;
+    if (dev != nullptr && (cfg->distance == 2 || cfg->policy == 2)) return TABED_EUNSUPPORTED;
+    if (misaligned(ws) || misaligned(target_logits) || misaligned(draft_logits) || misaligned(draft_lse)) return TABED_EALIGN;
+    for (const void* p : std::initializer_list<const void*>{tokens, node_q, parents, n_nodes, weights, temperature, u_acc, u_res, path, n_path, out_tokens, dev, n_valid})
+        if (element_misaligned(p, 0)) return TABED_EALIGN;
+    const hipError_t e = launch_verify_nodes(*cfg, static_cast<char*>(ws), round, N, target_logits, draft_logits, draft_lse, tokens, node_q, parents, n_nodes,
+                                             weights, temperature, u_acc, u_res, path, n_path, out_tokens, flags, dev, n_valid,
+                                             static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? TABED_OK : fail_hip(e);
+}
+
+int tabed_cache_keep_nodes(const tabed_cache_paged* cache, int32_t rows, int32_t N, const int32_t* ctx_base, const int32_t* path, const int32_t* n_path,
+                           int32_t* ctx_len, void* stream) {
+    int rc = validate_paged(cache, true);
+    if (rc == TABED_OK) rc = validate_nodes(rows, N);
+    if (rc != TABED_OK) return rc;
+    if (!ctx_base || !path || !n_path || !ctx_len) return TABED_ENULL;
+    if (ctx_len == ctx_base) return TABED_EINVAL;
+    if (element_misaligned(ctx_base, 0) || element_misaligned(path, 0) || element_misaligned(n_path, 0) || element_misaligned(ctx_len, 0)) return TABED_EALIGN;
+    const hipError_t e = launch_keep_nodes(*cache, rows, N, ctx_base, path, n_path, ctx_len, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? TABED_OK : fail_hip(e);
 }
 

@@ -1,0 +1,537 @@
+// Verification of a tree of drafted tokens: multi-round rejection sampling from the root down, one launch.
+//
+// The walk is sequential: which node comes next follows from the rows of the one before it, and only the rows of the nodes on the way are
+// read.  So that each of these steps has the chip's bandwidth all the same, a sequence's vocabulary is cut into pieces of kVerPiece, a workgroup
+// each, which walk together: at a step every workgroup reduces its piece, stores what it found, reads what the others found, and comes to
+// the same decision as they do from the same numbers in the same order.  A piece stays in registers: the target's row is read once at a node, the
+// drafts' once for the distances and once more, out of a cache, where a child is rejected; f is kept from level to level.  The masses of the
+// pieces, needed for the sum, are also the prefix in which the last draw is found.
+//
+// Decisions are in fp64: a draw among 10^5 tokens is decided by sums whose rounding in fp32 exceeds many tokens' probability.
+//
+// What crosses workgroups is stored past the caches in words of 32 bits of payload and 32 bits of the launch's number, so that a word says by
+// itself whether it is this launch's: one trip, no order among stores needed.  Every step has a place of its own (at most N steps: each visits a node
+// or rejects one).
+//
+// Why nothing waits for ever: workgroups are numbered as they start, sequence by sequence, so that a sequence's workgroups wait for
+// ones that run already or start as soon as any other sequence, or another kernel, ends; launches on several streams each hold back less than one
+// sequence's workgroups (at most 128 of the 1024 and more that run at a time).  A workspace that was never prepared is known by a mark.  A wait has a bound of
+// some seconds all the same; a row whose wait ended unanswered is left without a token, flagged.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "internal.h"
+#include "nodes.h"
+
+namespace tabed {
+
+constexpr int kVerThreads = 256, kVerWaves = kVerThreads / 64, kVerE = 8, kVerPiece = kVerThreads * kVerE;
+constexpr int kVerMaxPieces = 262144 / kVerPiece;
+constexpr int kVerDraftsAtOnce = 4;
+constexpr int kVerLine = 32;                                             // words of a line of the control block: ticket, exits, launch, mark
+constexpr size_t kVerControl = 512;
+constexpr uint32_t kVerMark = 0x7ab3d0deu;
+constexpr int kVerSpins = 1 << 24;
+
+struct VerifyArgs {
+    int V, n, B, N, G, gamma, tvd;
+    uint64_t seed, round;
+    const float* target;
+    const float* drafts;
+    const double* dlse;
+    const int32_t* tokens;
+    const float* node_q;
+    const int32_t* parents;
+    const int32_t* n_nodes;
+    const float* weights;
+    const float* temperature;
+    const float* u_acc;
+    const float* u_res;
+    int32_t* path;
+    int32_t* n_path;
+    int32_t* out_tokens;
+    uint8_t* flags;
+    float* dev;
+    int32_t* n_valid;
+    uint32_t* ctl;
+    uint64_t* rec;
+    uint64_t* devrec;
+};
+
+__device__ __forceinline__ void say(uint64_t* p, uint32_t v, uint32_t launch) {
+    __hip_atomic_store(p, (uint64_t)launch << 32 | v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ uint32_t lo32(double v) { return (uint32_t)__builtin_bit_cast(uint64_t, v); }
+__device__ __forceinline__ uint32_t hi32(double v) { return (uint32_t)(__builtin_bit_cast(uint64_t, v) >> 32); }
+__device__ __forceinline__ double from32(uint32_t lo, uint32_t hi) { return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo); }
+__device__ __forceinline__ float as_float(uint32_t v) { return __builtin_bit_cast(float, v); }
+// The word at p once it is this launch's; ok turns false where it does not come.
+__device__ __forceinline__ uint32_t hear(const uint64_t* p, uint32_t launch, bool& ok) {
+    for (int i = 0; i < kVerSpins; ++i) {
+        const uint64_t w = __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if ((uint32_t)(w >> 32) == launch) return (uint32_t)w;
+        if (i > 64) __builtin_amdgcn_s_sleep(1);
+    }
+    ok = false;
+    return 0;
+}
+
+struct VerifyShared {
+    int parent[TABED_MAX_NODES], token[TABED_MAX_NODES];
+    float q[TABED_MAX_NODES], u[TABED_MAX_NODES];
+    uint32_t rec[kVerMaxPieces][4];                                      // the step's records
+    double p_mass[kVerMaxPieces], mass[kVerMaxPieces];                   // of the pieces: p at the node, f of the last level
+    double red[kVerWaves][kVerDraftsAtOnce];
+    float redf[kVerWaves];
+    int redi[kVerWaves], redk[kVerWaves];
+    int ticket;
+    uint32_t launch;
+    uint8_t flag[TABED_MAX_NODES];
+    int path[TABED_MAX_NODES];
+};
+
+// Sum over the workgroup, the same in all threads.
+__device__ __forceinline__ double group_sum(double v, VerifyShared& s) {
+    v = wave_sum(v);
+    if ((threadIdx.x & 63) == 0) s.red[threadIdx.x >> 6][0] = v;
+    __syncthreads();
+    const double t = (s.red[0][0] + s.red[1][0]) + (s.red[2][0] + s.red[3][0]);
+    __syncthreads();
+    return t;
+}
+
+// The first child of `node` behind `after`, -1: none.  Uniform.
+__device__ __forceinline__ int next_child(const VerifyShared& s, int node, int after, int count) {
+    for (int j0 = after + 1; j0 < count; j0 += 64) {
+        const int j = j0 + (threadIdx.x & 63);
+        const uint64_t who = __ballot(j < count && s.parent[min(j, count - 1)] == node);
+        if (who) return __builtin_amdgcn_readfirstlane(j0 + __ffsll((long long)who) - 1);
+    }
+    return -1;
+}
+
+struct Piece {                                                           // a workgroup's part of a row: a thread has two groups of four elements
+    int v0[2], at[2];
+};
+__device__ __forceinline__ void load_piece(const float* row, int V, const Piece& p, float4 (&x)[2]) {
+    with_row_loads(V, [&](auto load) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) x[i] = load(row, p.at[i]);
+    });
+#pragma unroll
+    for (int i = 0; i < 2; ++i) mask_group(x[i], p.at[i], p.v0[i]);      // (what belongs to other threads, or lies past the row: -inf)
+}
+
+__global__ __launch_bounds__(kVerThreads, 2) void k_verify_nodes(VerifyArgs a) {
+    __shared__ VerifyShared s;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = a.V, n = a.n;
+    if (tid == 0) {
+        const uint32_t mark = __hip_atomic_load(a.ctl + 3 * kVerLine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        s.launch = __hip_atomic_load(a.ctl + 2 * kVerLine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        s.ticket = mark == kVerMark ? (int)__hip_atomic_fetch_add(a.ctl, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : -1;
+    }
+    __syncthreads();
+    const uint32_t launch = __builtin_amdgcn_readfirstlane(s.launch);
+    int ticket = __builtin_amdgcn_readfirstlane(s.ticket);
+    const bool prepared = ticket >= 0 && ticket < a.B * a.G;
+    if (!prepared) ticket = blockIdx.x;
+    const int b = ticket / a.G, c = ticket % a.G;
+    const int count = nodes_of(a.n_nodes, b, a.N);
+    if (tid < a.N) {
+        const size_t j = (size_t)b * a.N + tid;
+        s.parent[tid] = tid == 0 ? -1 : parent_of(a.parents, b, tid, a.N);
+        s.token[tid] = a.tokens[j];
+        s.q[tid] = a.node_q[j];
+        s.u[tid] = a.u_acc != nullptr ? a.u_acc[j] : tabed_uniform(a.seed, a.round, (uint32_t)b, (uint32_t)(tid - 1), 1);
+        s.flag[tid] = 0;
+    }
+    __syncthreads();
+    const float T = a.temperature[b];
+    const bool greedy = !(T > 0.f);
+    const double inv_t = greedy ? 1.0 : 1.0 / (double)T;
+    uint64_t* const rec_b = a.rec + (size_t)b * a.N * a.G * 4;
+    uint64_t* const dev_b = a.devrec + (size_t)b * a.gamma * a.G * n * 2;
+    Piece piece;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        piece.v0[i] = c * kVerPiece + i * kVerThreads * 4 + tid * 4;
+        piece.at[i] = group_at(min(piece.v0[i], V - 1), V);
+    }
+
+    // A step's records, read by all into s.rec; false, for all, where one does not come.
+    auto collect = [&](int step) {
+        bool ok = true;
+        const uint64_t* from = rec_b + (size_t)step * a.G * 4;
+        for (int w = tid; w < a.G * 4; w += kVerThreads) s.rec[w / 4][w % 4] = hear(from + w, launch, ok);
+        return __syncthreads_or(!ok) == 0;
+    };
+    auto publish = [&](int step, uint32_t w0, uint32_t w1, double z) {   // by one thread
+        uint64_t* to = rec_b + ((size_t)step * a.G + c) * 4;
+        say(to + 0, w0, launch);
+        say(to + 1, w1, launch);
+        say(to + 2, lo32(z), launch);
+        say(to + 3, hi32(z), launch);
+    };
+
+    int cur = 0, depth = 0, step = 0, valid = 0, best = 0, level = 0;
+    bool fine = prepared;
+    double f[kVerE], q[kVerE], total = 0.0, scale = 0.0;                 // f times scale is p, at level 0
+    while (count > 0 && fine) {
+        if (tid == 0) s.path[depth] = cur;
+        int child = next_child(s, cur, cur, count);
+        const bool want_dev = child >= 0 && a.dev != nullptr && depth < a.gamma;
+        const float* const row = a.target + ((size_t)b * a.N + cur) * V;
+        const float* const drafts = a.drafts + ((size_t)cur * a.B + b) * n * V;
+        const double* const dlse = a.dlse + ((size_t)cur * a.B + b) * n;
+        float4 x[2];
+        load_piece(row, V, piece, x);
+        int y = child >= 0 ? s.token[child] : -1;
+        const float ly = row[(unsigned)y < (unsigned)V ? y : 0];
+
+        // ---- the piece's maximum, and the sum of exp
+        ArgMax top{-INFINITY, 0x7fffffff};
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float v = f4get(x[i], e);
+                if (v > top.v) top = ArgMax{v, piece.at[i] + e};         // (ascending within a thread)
+            }
+        top = wave_argmax(top);
+        if (lane == 0) { s.redf[wave] = top.v; s.redi[wave] = top.i; }
+        __syncthreads();
+        top = argmax_merge(argmax_merge(ArgMax{s.redf[0], s.redi[0]}, ArgMax{s.redf[1], s.redi[1]}),
+                           argmax_merge(ArgMax{s.redf[2], s.redi[2]}, ArgMax{s.redf[3], s.redi[3]}));
+        double sum = 0.0;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float v = f4get(x[i], e);
+                f[i * 4 + e] = v == -INFINITY ? 0.0 : exp(((double)v - (double)top.v) * inv_t);
+                sum += f[i * 4 + e];
+            }
+        sum = group_sum(sum, s);
+        if (tid == 0) publish(step, __builtin_bit_cast(uint32_t, top.v), (uint32_t)top.i, sum);
+
+        // ---- KL: the piece's sum of exp * ((l - max) / T - log q_j)
+        if (want_dev && !a.tvd) {
+            for (int j0 = 0; j0 < n; j0 += kVerDraftsAtOnce) {
+                float4 d[kVerDraftsAtOnce][2];
+#pragma unroll
+                for (int j = 0; j < kVerDraftsAtOnce; ++j) load_piece(drafts + (size_t)min(j0 + j, n - 1) * V, V, piece, d[j]);
+#pragma unroll
+                for (int j = 0; j < kVerDraftsAtOnce; ++j) {
+                    const double lse = dlse[min(j0 + j, n - 1)];
+                    double kl = 0.0;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const double w = f[i * 4 + e];
+                            const double t = ((double)f4get(x[i], e) - (double)top.v - (double)f4get(d[j][i], e)) * inv_t + lse;
+                            kl += w == 0.0 ? 0.0 : w * t;
+                        }
+                    kl = wave_sum(kl);
+                    if (lane == 0) s.red[wave][j] = kl;
+                }
+                __syncthreads();
+                if (tid < kVerDraftsAtOnce && j0 + tid < n) {
+                    const double kl = (s.red[0][tid] + s.red[1][tid]) + (s.red[2][tid] + s.red[3][tid]);
+                    uint64_t* to = dev_b + (((size_t)depth * a.G + c) * n + j0 + tid) * 2;
+                    say(to, lo32(kl), launch);
+                    say(to + 1, hi32(kl), launch);
+                }
+                __syncthreads();
+            }
+        }
+
+        // ---- all pieces: maximum, arg-max, sum
+        fine = collect(step);
+        if (!fine) break;
+        ++step;
+        ArgMax all{-INFINITY, 0x7fffffff};
+        for (int g = lane; g < a.G; g += 64) all = argmax_merge(all, ArgMax{as_float(s.rec[g][0]), (int)s.rec[g][1]});
+        all = wave_argmax(all);
+        double z = 0.0;
+        for (int g = lane; g < a.G; g += 64) {
+            const float mg = as_float(s.rec[g][0]);
+            const double w = mg == -INFINITY ? 0.0 : exp(((double)mg - (double)all.v) * inv_t) * from32(s.rec[g][2], s.rec[g][3]);
+            z += w;
+            if (wave == 0) s.p_mass[g] = w;                              // (times 1 / z below)
+        }
+        z = wave_sum(z);
+        if (wave == 0)
+            for (int g = lane; g < a.G; g += 64) s.p_mass[g] /= z;
+        best = all.i < V ? all.i : 0;                                    // (a row of -inf and NaN: 0)
+        scale = top.v == -INFINITY ? 0.0 : exp(((double)top.v - (double)all.v) * inv_t) / z;
+
+        if (want_dev) {
+            valid = depth + 1;
+            if (a.tvd) {
+                for (int j = 0; j < n; ++j) {
+                    float4 d[2];
+                    load_piece(drafts + (size_t)j * V, V, piece, d);
+                    const double lse = dlse[j];
+                    double tv = 0.0;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) tv += fabs(f[i * 4 + e] * scale - exp((double)f4get(d[i], e) * inv_t - lse));
+                    tv = group_sum(tv, s);
+                    if (tid == 0) {
+                        uint64_t* to = dev_b + (((size_t)depth * a.G + c) * n + j) * 2;
+                        say(to, lo32(tv), launch);
+                        say(to + 1, hi32(tv), launch);
+                    }
+                }
+            }
+            if (c == 0) {                                                // has all pieces' maxima and sums at hand: finishes the distances
+                bool ok = true;
+                for (int j = wave; j < n; j += kVerWaves) {
+                    double t = 0.0;
+                    for (int g = lane; g < a.G; g += 64) {
+                        const uint64_t* from = dev_b + (((size_t)depth * a.G + g) * n + j) * 2;
+                        const uint32_t lo = hear(from, launch, ok), hi = hear(from + 1, launch, ok);
+                        const float mg = as_float(s.rec[g][0]);
+                        const double up = ((double)mg - (double)all.v) * inv_t;
+                        if (a.tvd) t += from32(lo, hi);
+                        else if (mg != -INFINITY) t += exp(up) * (from32(lo, hi) + up * from32(s.rec[g][2], s.rec[g][3]));
+                    }
+                    t = wave_sum(t);
+                    if (lane == 0) a.dev[((size_t)b * a.gamma + depth) * n + j] = (float)(a.tvd ? 0.5 * t : t / z - log(z));
+                }
+                fine = ok;
+            }
+            fine = __syncthreads_or(!fine) == 0;
+            if (!fine) break;
+        }
+        __syncthreads();                                                 // p_mass is whole, s.rec has been read
+
+        // ---- the children, in order
+        level = 0;
+        total = 1.0;
+        double fy = (unsigned)y < (unsigned)V ? exp(((double)ly - (double)all.v) * inv_t) / z : 0.0;
+        int hit = -1;
+        while (child >= 0) {
+            const bool there = (unsigned)y < (unsigned)V;
+            uint8_t flag = there ? 0 : TABED_FLAG_DEGENERATE;
+            bool yes = there && y == best;
+            if (!greedy) {
+                const double want = (double)s.u[child] * (double)s.q[child] * total;
+                yes = there && want < fy;
+                if (there && fabs(want - fy) < (double)kMargin * fmax(want, fy)) flag |= TABED_FLAG_ACCEPT_MARGIN;
+            }
+            if (c == 0 && tid == 0) s.flag[child] = flag;
+            if (yes) {
+                hit = child;
+                break;
+            }
+            child = next_child(s, cur, child, count);
+            y = child >= 0 ? s.token[child] : -1;
+            if (greedy) continue;
+            if (level == 0) {
+#pragma unroll
+                for (int e = 0; e < kVerE; ++e) {
+                    f[e] *= scale;
+                    q[e] = 0.0;
+                }
+                for (int j0 = 0; j0 < n; j0 += kVerDraftsAtOnce) {
+                    float4 d[kVerDraftsAtOnce][2];
+#pragma unroll
+                    for (int j = 0; j < kVerDraftsAtOnce; ++j) load_piece(drafts + (size_t)min(j0 + j, n - 1) * V, V, piece, d[j]);
+#pragma unroll
+                    for (int j = 0; j < kVerDraftsAtOnce; ++j) {
+                        if (j0 + j >= n) break;
+                        const double lse = dlse[j0 + j], w = (double)a.weights[(size_t)b * n + j0 + j];
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) q[i * 4 + e] += w * exp((double)f4get(d[j][i], e) * inv_t - lse);
+                    }
+                }
+            }
+            const double inv = total > 0.0 ? 1.0 / total : 0.0;
+            double zsum = 0.0, fn = 0.0;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    double& fe = f[i * 4 + e];
+                    fe = fmax(0.0, fe * inv - q[i * 4 + e]);
+                    zsum += fe;
+                    if (piece.at[i] + e == y) fn += fe;                  // (an element that is another thread's is 0 here)
+                }
+            zsum = wave_sum(zsum);
+            fn = wave_sum(fn);
+            if (lane == 0) { s.red[wave][0] = zsum; s.red[wave][1] = fn; }
+            __syncthreads();
+            if (tid == 0) {
+                const double ft = (s.red[0][1] + s.red[1][1]) + (s.red[2][1] + s.red[3][1]);
+                publish(step, lo32(ft), hi32(ft), (s.red[0][0] + s.red[1][0]) + (s.red[2][0] + s.red[3][0]));
+            }
+            fine = collect(step);
+            if (!fine) break;
+            ++step;
+            ++level;
+            double zt = 0.0;
+            for (int g = lane; g < a.G; g += 64) {
+                const double zg = from32(s.rec[g][2], s.rec[g][3]);
+                zt += zg;
+                if (wave == 0) s.mass[g] = zg;
+            }
+            total = wave_sum(zt);
+            fy = 0.0;
+            if ((unsigned)y < (unsigned)V) fy = from32(s.rec[y / kVerPiece][0], s.rec[y / kVerPiece][1]);
+            __syncthreads();                                             // mass is whole, s.rec has been read
+        }
+        if (!fine || hit < 0) break;
+        cur = hit;
+        ++depth;
+    }
+
+    // ---- the last draw: the piece that it falls into by the masses, in it the token
+    if (count > 0 && fine && !greedy) {
+        const bool gone = level > 0 && !(total > 0.0);                   // nothing is left of f: p again
+        if (gone) {
+            float4 x[2];
+            load_piece(a.target + ((size_t)b * a.N + cur) * V, V, piece, x);
+            float m = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) m = fmaxf(m, f4get(x[i], e));
+            m = block_max(m, s.redf);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float v = f4get(x[i], e);
+                    f[i * 4 + e] = v == -INFINITY ? 0.0 : exp(((double)v - (double)m) * inv_t) * scale;
+                }
+        } else if (level == 0) {
+#pragma unroll
+            for (int e = 0; e < kVerE; ++e) f[e] *= scale;
+        }
+        const double* const mass = level == 0 || gone ? s.p_mass : s.mass;
+        const float u = a.u_res != nullptr ? a.u_res[b] : tabed_uniform(a.seed, a.round, (uint32_t)b, (uint32_t)(a.N - 1), 0);
+        // Every wave of every workgroup the same: the first piece in which the prefix exceeds u Z, else the last with any mass, else the first.
+        double whole = 0.0;
+        for (int g0 = 0; g0 < a.G; g0 += 64) whole += wave_sum(g0 + lane < a.G ? mass[g0 + lane] : 0.0);
+        const double goal = (double)u * whole;
+        double run = 0.0, before = 0.0;
+        int owner = 0;
+        bool crossed = false;
+        for (int g0 = 0; g0 < a.G && !crossed; g0 += 64) {
+            const double mg = g0 + lane < a.G ? mass[g0 + lane] : 0.0;
+            const double incl = run + wave_inclusive_scan(mg);
+            const uint64_t over = __ballot(mg > 0.0 && incl > goal), some = __ballot(mg > 0.0);
+            const int at = over ? __ffsll((long long)over) - 1 : some ? 63 - __clzll((long long)some) : -1;
+            if (at >= 0) {
+                owner = g0 + at;
+                before = lane_f64(incl, at) - lane_f64(mg, at);
+            }
+            crossed = over != 0;
+            run = lane_f64(incl, 63);
+        }
+        if (c == owner) {
+            int first = 0x7fffffff, last = -1;
+            double lo[kVerE];
+            for (int i = 0; i < 2; ++i) {                                // (the groups one after the other: the order of the row)
+                double part, at = 0.0;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) at += f[i * 4 + e];
+                at = before + block_exclusive_scan(at, &s.red[0][0], &part);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const double fe = f[i * 4 + e];
+                    lo[i * 4 + e] = at;
+                    at += fe;
+                    if (fe > 0.0) {
+                        last = piece.at[i] + e;
+                        if (at > goal) first = min(first, last);
+                    }
+                }
+                before += part;
+            }
+            const int pick = block_pick_key(first, last, s.redi, s.redk);
+            uint8_t flag = (crossed ? 0 : TABED_FLAG_DEGENERATE) | (gone ? TABED_FLAG_DEGENERATE : 0);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (f[i * 4 + e] > 0.0 && piece.at[i] + e == pick) {
+                        const double l = lo[i * 4 + e], h = l + f[i * 4 + e];
+                        if (fmin(fabs(h - goal), fabs(goal - l)) < (double)kMargin * whole) flag |= TABED_FLAG_SAMPLE_MARGIN;
+                        a.out_tokens[(size_t)b * a.N + depth] = pick;
+                        a.flags[(size_t)b * a.N] = flag;
+                    }
+            if (pick < 0 && tid == 0) {                                  // no element has any mass (NaN)
+                a.out_tokens[(size_t)b * a.N + depth] = 0;
+                a.flags[(size_t)b * a.N] = TABED_FLAG_DEGENERATE;
+            }
+        }
+    }
+
+    // ---- the first workgroup tells the way
+    if (c == 0) {
+        __syncthreads();
+        const int said = count > 0 && fine ? depth + 1 : 0;              // nodes of the path
+        if (tid < a.N) {
+            const size_t at = (size_t)b * a.N + tid;
+            a.path[at] = tid < said ? s.path[tid] : -1;
+            if (tid + 1 != said) a.out_tokens[at] = tid + 1 < said ? s.token[s.path[tid + 1]] : -1;
+            else if (greedy) a.out_tokens[at] = best;
+            if (tid > 0) a.flags[at] = said > 0 ? s.flag[tid] : 0;
+            else if (said == 0 || greedy) a.flags[at] = fine ? 0 : TABED_FLAG_DEGENERATE;
+        }
+        if (tid == 0) {
+            a.n_path[b] = said;
+            if (a.n_valid != nullptr) a.n_valid[b] = said > 0 ? valid : 0;
+        }
+    }
+    if (prepared && tid == 0) {                                          // the last to leave makes the workspace ready for the next launch
+        if (__hip_atomic_fetch_add(a.ctl + kVerLine, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(a.B * a.G) - 1) {
+            __hip_atomic_store(a.ctl, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __hip_atomic_store(a.ctl + kVerLine, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __hip_atomic_store(a.ctl + 2 * kVerLine, launch + 1 == 0 ? 1u : launch + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+    }
+}
+
+NodesVerifyLayout nodes_verify_layout(const tabed_cfg& c, int N) {
+    auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+    NodesVerifyLayout L;
+    L.G = (c.V + kVerPiece - 1) / kVerPiece;
+    L.off_rec = kVerControl;
+    L.off_dev = L.off_rec + up((size_t)c.B * N * L.G * 4 * 8);
+    L.total = L.off_dev + up((size_t)c.B * c.gamma * L.G * c.n * 2 * 8);
+    return L;
+}
+
+__global__ void k_verify_nodes_init(uint32_t* ws, size_t words) {
+    for (size_t i = blockIdx.x * (size_t)blockDim.x + threadIdx.x; i < words; i += (size_t)gridDim.x * blockDim.x)
+        ws[i] = i == 2 * kVerLine ? 1u : i == 3 * kVerLine ? kVerMark : 0u;
+}
+hipError_t launch_nodes_verify_init(const tabed_cfg& c, int N, char* ws, hipStream_t s) {
+    const size_t words = nodes_verify_layout(c, N).total / 4;
+    hipLaunchKernelGGL(k_verify_nodes_init, dim3((unsigned)std::min<size_t>((words + 255) / 256, 2048)), dim3(256), 0, s, reinterpret_cast<uint32_t*>(ws), words);
+    return hipGetLastError();
+}
+
+hipError_t launch_verify_nodes(const tabed_cfg& c, char* ws, uint64_t round, int N, const float* target_logits, const float* draft_logits,
+                               const double* draft_lse, const int32_t* tokens, const float* node_q, const int32_t* parents, const int32_t* n_nodes,
+                               const float* weights, const float* temperature, const float* u_acc, const float* u_res, int32_t* path, int32_t* n_path,
+                               int32_t* out_tokens, uint8_t* flags, float* dev, int32_t* n_valid, hipStream_t s) {
+    ProfScope prof(TABED_K_TREE, s);
+    const NodesVerifyLayout L = nodes_verify_layout(c, N);
+    const VerifyArgs a{c.V, c.n, c.B, N, L.G, c.gamma, c.distance == 1, c.seed, round, target_logits, draft_logits, draft_lse, tokens, node_q, parents,
+                       n_nodes, weights, temperature, u_acc, u_res, path, n_path, out_tokens, flags, dev, n_valid, reinterpret_cast<uint32_t*>(ws),
+                       reinterpret_cast<uint64_t*>(ws + L.off_rec), reinterpret_cast<uint64_t*>(ws + L.off_dev)};
+    launch(&prof, k_verify_nodes, dim3((unsigned)(c.B * L.G)), dim3(kVerThreads), 0, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace tabed
