@@ -476,7 +476,7 @@ int tabed_draft_body_step_q8(const tabed_body_cfg* cfg, const tabed_body_weights
  * all layers; position p is in entry p / TABED_CACHE_BLOCK.  Rows may share full blocks; the blocks that nodes are written to belong to one row.  A table
  * entry outside [0, blocks) is no block: its positions are not there.
  *   k, v           entry of (layer, block, head, token): head_dim values that lie side by side, at layer * layer_stride + block * block_stride +
- *                  head * head_stride + token * tok_stride elements; entries must not overlap.  Every stride is at least head_dim and a multiple of 16 bytes.
+ *                  head * head_stride + token * tok_stride elements; entries must not overlap.  Every stride is at least head_dim and a multiple of 16 bytes, tok_stride at most 2^24.
  *                  (The caches of tabed_draft_body_step are one, for a max_ctx that is a multiple of 64: blocks of a row side by side, block_stride 64 d,
  *                  tok_stride d, head_stride head_dim.)
  *   kscale, vscale [layers, blocks, kv_heads, 64] fp32, type 2 only: a value is e4m3 * scale, with a scale of 1/448 of the largest magnitude of the

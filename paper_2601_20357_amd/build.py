@@ -11,7 +11,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtabed.so")
 SOURCES = ["api.hip", "lmhead.hip", "vocab.hip", "body.hip", "body_gang.hip", "norm_q8.hip", "linear_q8.hip", "cache_q8.hip",
-           "cache_nodes.hip", "attn_nodes.hip", "verify_nodes.hip"]
+           "cache_nodes.hip", "attn_nodes.hip", "attn_nodes_32.hip", "attn_nodes_64.hip", "attn_nodes_96.hip",
+           "attn_nodes_128.hip", "attn_nodes_256.hip", "verify_nodes.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     # keep the compiler from forming packed-fp32 instructions

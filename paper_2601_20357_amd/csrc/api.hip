@@ -130,6 +130,7 @@ static int validate_paged(const tabed_cache_paged* c, bool pointers) {
     const int64_t piece = c->type == 2 ? 16 : 8;
     for (int64_t stride : {c->layer_stride, c->block_stride, c->head_stride, c->tok_stride})
         if (stride < c->head_dim || stride % piece != 0 || stride > (1ll << 44)) return TABED_EINVAL;
+    if (c->tok_stride > (1 << 24)) return TABED_EINVAL;
     if (!pointers) return TABED_OK;
     if (!c->k || !c->v || !c->table || (c->type == 2 && (!c->kscale || !c->vscale))) return TABED_ENULL;
     if (misaligned(c->k) || misaligned(c->v) || element_misaligned(c->table, 0)) return TABED_EALIGN;

@@ -1,0 +1,5 @@
+// Attention over trees, heads of 96 dims.
+#include "attn_nodes.h"
+namespace tabed {
+TABED_NODES_HD(96)
+}

@@ -86,30 +86,6 @@ __device__ __forceinline__ void announce_f4(void* p, float a, float b, float c, 
 }
 __device__ __forceinline__ bool unset(const u32x4b& v) { return v[0] == kUnset || v[1] == kUnset || v[2] == kUnset || v[3] == kUnset; }
 
-// v combined with the v of the lane 16, or 32, away.  (The results are copied out first: a bit cast of an element of the
-// returned vector reads element 0.)
-template <typename F>
-__device__ __forceinline__ float with_lane16(float v, F f) {
-    const uint32_t x = __builtin_bit_cast(uint32_t, v);
-    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-    const uint32_t r0 = r[0], r1 = r[1];
-    return f(__builtin_bit_cast(float, r0), __builtin_bit_cast(float, r1));
-}
-template <typename F>
-__device__ __forceinline__ float with_lane32(float v, F f) {
-    const uint32_t x = __builtin_bit_cast(uint32_t, v);
-    const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
-    const uint32_t r0 = r[0], r1 = r[1];
-    return f(__builtin_bit_cast(float, r0), __builtin_bit_cast(float, r1));
-}
-__device__ __forceinline__ float add_lanes16_32(float v) {
-    auto add = [](float p, float q) { return p + q; };
-    return with_lane32(with_lane16(v, add), add);
-}
-__device__ __forceinline__ float max_lanes16_32(float v) {
-    auto larger = [](float p, float q) { return fmaxf(p, q); };
-    return with_lane32(with_lane16(v, larger), larger);
-}
 constexpr int kDppRor8 = 0x128;                      // row_ror:8 = lane ^ 8 within 16
 
 __device__ __forceinline__ void keep_order() { asm volatile("" ::: "memory"); }

@@ -181,7 +181,9 @@ hipError_t launch_append_nodes(const tabed_cache_paged& c, int layer, int rows, 
                                const int32_t* ctx_len, const int32_t* parents, const int32_t* n_nodes, float rope_theta, hipStream_t s);
 hipError_t launch_keep_nodes(const tabed_cache_paged& c, int rows, int N, const int32_t* ctx_base, const int32_t* path, const int32_t* n_path,
                              int32_t* ctx_len, hipStream_t s);
-struct NodesAttnLayout { // (arrival counters come first, as many for all sizes)
+struct NodesAttnLayout {
+    size_t off_ml;       // float2 [slots, kv_heads, tiles][queries of a workgroup] maxima and sums of ranges; before it the ranges of every row
+    size_t off_o;        // float [slots, kv_heads, tiles][queries of a workgroup][head_dim] their sums of values
     size_t total;
 };
 NodesAttnLayout nodes_attn_layout(const tabed_cache_paged& c, int rows, int N, int q_heads);
@@ -234,6 +236,16 @@ inline hipError_t raise_lds_limit(K kernel, size_t lds, std::once_flag& once, hi
         rc = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     });
     return rc;
+}
+
+// (... once for each device.)
+template <typename K>
+inline hipError_t raise_on_device(K kernel, size_t lds, std::once_flag (&once)[kMaxDevices], hipError_t (&rc)[kMaxDevices]) {
+    int dev = 0;
+    const hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return e;
+    if (dev < 0 || dev >= kMaxDevices) return hipErrorInvalidDevice;
+    return raise_lds_limit(kernel, lds, once[dev], rc[dev]);
 }
 
 template <typename K, typename... Args>

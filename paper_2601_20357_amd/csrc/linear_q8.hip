@@ -309,16 +309,6 @@ __global__ __launch_bounds__(kLinearThreads, 2) void k_linear_tile(LinearArgs a,
 }
 
 // ---------------------------------------------------------------- host side
-// (The limit of a kernel's LDS is raised once for each device.)
-template <typename K>
-static hipError_t raise_on_device(K kernel, size_t lds, std::once_flag (&once)[kMaxDevices], hipError_t (&rc)[kMaxDevices]) {
-    int dev = 0;
-    const hipError_t e = hipGetDevice(&dev);
-    if (e != hipSuccess) return e;
-    if (dev < 0 || dev >= kMaxDevices) return hipErrorInvalidDevice;
-    return raise_lds_limit(kernel, lds, once[dev], rc[dev]);
-}
-
 template <int BM, int BN, int KW, int SW, int SH, int EPI, bool PAST>
 static hipError_t launch_tile_q8(const ProfScope* prof, const LinearArgs& a, hipStream_t s) {
     constexpr size_t lds = std::max((size_t)KW * (SW * BN + SH * BM) * kLine, (size_t)16 * kPatchBytes + (2 * BM + BN) * 4 + 2 * BM * (BN / kTileV) * 4);

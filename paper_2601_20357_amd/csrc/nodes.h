@@ -32,6 +32,10 @@ struct PagedView {
         const int b = table[(int64_t)r * max_blocks + e];
         return b >= 0 && b < blocks ? b : -1;
     }
+    __device__ __forceinline__ int block_at(int r, int entry) const {
+        const int b = table[(int64_t)r * max_blocks + min(entry, max_blocks - 1)];
+        return entry < max_blocks && b >= 0 && b < blocks ? b : -1;
+    }
     __device__ __forceinline__ int64_t entry(int layer_, int block, int head, int slot) const {      // in elements
         return layer_ * layer_stride + block * block_stride + head * head_stride + slot * tok_stride;
     }

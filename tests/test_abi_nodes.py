@@ -42,7 +42,7 @@ def test_struct_matches_header():
 BAD_CACHES = [(dict(layers=0), ERANGE), (dict(layers=1025), ERANGE), (dict(kv_heads=0), ERANGE), (dict(kv_heads=1025), ERANGE), (dict(blocks=0), ERANGE),
               (dict(max_blocks=0), ERANGE), (dict(max_blocks=2 ** 24 + 1), ERANGE), (dict(head_dim=48), EINVAL), (dict(head_dim=0), EINVAL), (dict(type=0), EINVAL),
               (dict(type=3), EINVAL), (dict(tok_stride=63), EINVAL), (dict(tok_stride=68), EINVAL), (dict(head_stride=-4096), EINVAL), (dict(block_stride=0), EINVAL),
-              (dict(layer_stride=2 ** 45), EINVAL), (dict(type=2, tok_stride=72, kscale=0x1000, vscale=0x1000), EINVAL), (dict(k=None), ENULL), (dict(v=None), ENULL),
+              (dict(layer_stride=2 ** 45), EINVAL), (dict(tok_stride=2 ** 24 + 16), EINVAL), (dict(type=2, tok_stride=72, kscale=0x1000, vscale=0x1000), EINVAL), (dict(k=None), ENULL), (dict(v=None), ENULL),
               (dict(table=None), ENULL), (dict(type=2), ENULL), (dict(type=2, kscale=0x1000), ENULL), (dict(k=0x1008), EALIGN), (dict(v=0x1002), EALIGN),
               (dict(table=0x1002), EALIGN), (dict(type=2, kscale=0x1002, vscale=0x1000), EALIGN)]
 APPEND = "cache layer rows N dt k v row tok qh q qrow qtok out orow otok ctx parents nodes theta stream".split()
