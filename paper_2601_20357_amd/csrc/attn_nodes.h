@@ -324,8 +324,10 @@ __global__ __launch_bounds__(T::kThreads, 2) void k_attention_nodes(NodesAttnArg
         for (int d = 0; d < DT; ++d) acc[b][d] = f32x4b{0.f, 0.f, 0.f, 0.f};
     }
 
+    const bool idle = q0 >= queries;                                     // a wave without queries only helps with the tiles
     bool odd_any = false;
     auto compute = [&](int t, int stage, auto masked) {
+        if (idle) return;
         const unsigned char* const sk = area + stage * T::kStage;
         const unsigned char* const sv = sk + T::kTile;
         const float* const ss = reinterpret_cast<const float*>(sv + T::kTile);
@@ -688,7 +690,8 @@ inline auto with_nodes_variant(int queries, F&& f) {
     if (queries <= 32) return f(NodesVariant<HD, F8, 2, 1, kBig ? 2 : 4, 32, 2>{});
     if constexpr (HD * (F8 ? 1 : 2) % 64 == 0) {
         if (queries <= 64) return f(NodesVariant<HD, F8, 2, 2, HD == 256 ? 2 : 4, 32, 2>{});
-        return f(NodesVariant<HD, F8, 2, 4, 1, 64, kBig ? 2 : 3>{});
+        if (queries <= 128 || HD * (F8 ? 1 : 2) % 128 != 0) return f(NodesVariant<HD, F8, 2, 4, 1, 64, kBig ? 2 : 3>{});
+        return f(NodesVariant<HD, F8, 2, HD * (F8 ? 1 : 2) % 128 == 0 ? 8 : 4, 1, 64, kBig ? 2 : 3>{});
     } else {
         return f(NodesVariant<HD, F8, 2, 2, 4, 64, 2>{});
     }

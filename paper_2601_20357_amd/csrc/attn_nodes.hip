@@ -26,17 +26,18 @@ static NodesPlan plan_of(const tabed_cache_paged& c, int rows, int N, int q_head
             using T = decltype(v);
             p.queries = T::kQueries;
             kt = T::KT;
-            room = 256 * std::max(1, std::min<int>(163840 / (int)T::kLds, 2));
+            room = 256 * std::max(1, std::min(163840 / (int)T::kLds, 8 / T::kWaves));
             return 0;
         };
         return c.type == 2 ? with_nodes_variant<decltype(hd)::value, true>(queries, take) : with_nodes_variant<decltype(hd)::value, false>(queries, take);
     });
     p.tiles = (queries + p.queries - 1) / p.queries;
-    const int64_t units = (int64_t)c.kv_heads * p.tiles, each = room / units;        // slots that fill the chip
+    const int64_t units = (int64_t)c.kv_heads * p.tiles;                 // workgroups of a slot
+    const int64_t fill = room / units, each = std::max<int64_t>(fill, 2 * rows);
     p.slots = rows;
     p.min_tiles = 512 / kt;
     const int64_t most = ((int64_t)c.max_blocks * TABED_CACHE_BLOCK + kt - 1) / kt;   // tiles of the longest row there can be
-    if (rows <= kMaxSplitRows && each > rows && most > p.min_tiles) {
+    if (rows <= kMaxSplitRows && most > (fill > rows ? 1 : 8) * p.min_tiles) {
         p.split = 1;
         p.target = (int)std::max<int64_t>(1, each - rows / 2);
         p.slots = (int)std::min<int64_t>(p.target + rows, rows * ((most + p.min_tiles - 1) / p.min_tiles));

@@ -30,8 +30,7 @@ namespace tabed {
 constexpr int kVerThreads = 256, kVerWaves = kVerThreads / 64, kVerE = 8, kVerPiece = kVerThreads * kVerE;
 constexpr int kVerMaxPieces = 262144 / kVerPiece;
 constexpr int kVerDraftsAtOnce = 4;
-constexpr int kVerLine = 32;                                             // words of a line of the control block: ticket, exits, launch, mark
-constexpr size_t kVerControl = 512;
+constexpr size_t kVerControl = 256;                                      // uint64: the launch's number and the next workgroup's; uint32 in the next line: mark
 constexpr uint32_t kVerMark = 0x7ab3d0deu;
 constexpr int kVerSpins = 1 << 24;
 
@@ -55,7 +54,7 @@ struct VerifyArgs {
     uint8_t* flags;
     float* dev;
     int32_t* n_valid;
-    uint32_t* ctl;
+    uint64_t* ctl;
     uint64_t* rec;
     uint64_t* devrec;
 };
@@ -78,6 +77,26 @@ __device__ __forceinline__ uint32_t hear(const uint64_t* p, uint32_t launch, boo
     return 0;
 }
 
+// e^x in 64 bits: x = n ln 2 + r, |r| <= ln 2 / 2, the series of e^r up to r^11 / 11! (what is left out is below 7e-15 of the result, ln 2's rounding
+// takes n 2.4e-17), times 2^n.  A fifth of the instructions of the library's, which a rejection needs for every element of every draft.
+__device__ __forceinline__ double exp64(double x) {
+    x = x < -800.0 ? -800.0 : x;                                         // (-inf: 0; a NaN stays one)
+    const double n = rint(x * 1.4426950408889634074), r = fma(n, -0.69314718055994530942, x);
+    double p = 1.0 / 39916800.0;
+    p = fma(p, r, 1.0 / 3628800.0);
+    p = fma(p, r, 1.0 / 362880.0);
+    p = fma(p, r, 1.0 / 40320.0);
+    p = fma(p, r, 1.0 / 5040.0);
+    p = fma(p, r, 1.0 / 720.0);
+    p = fma(p, r, 1.0 / 120.0);
+    p = fma(p, r, 1.0 / 24.0);
+    p = fma(p, r, 1.0 / 6.0);
+    p = fma(p, r, 0.5);
+    p = fma(p, r, 1.0);
+    p = fma(p, r, 1.0);
+    return __builtin_amdgcn_ldexp(p, (int)n);
+}
+
 struct VerifyShared {
     int parent[TABED_MAX_NODES], token[TABED_MAX_NODES];
     float q[TABED_MAX_NODES], u[TABED_MAX_NODES];
@@ -86,19 +105,21 @@ struct VerifyShared {
     double red[kVerWaves][kVerDraftsAtOnce];
     float redf[kVerWaves];
     int redi[kVerWaves], redk[kVerWaves];
-    int ticket;
+    int ticket, bad;
     uint32_t launch;
+    float weight[TABED_MAX_N];
     uint8_t flag[TABED_MAX_NODES];
     int path[TABED_MAX_NODES];
+    int16_t at_step[TABED_MAX_NODES];                                    // of the path's nodes
 };
 
 // Sum over the workgroup, the same in all threads.
 __device__ __forceinline__ double group_sum(double v, VerifyShared& s) {
     v = wave_sum(v);
     if ((threadIdx.x & 63) == 0) s.red[threadIdx.x >> 6][0] = v;
-    __syncthreads();
+    lds_barrier();
     const double t = (s.red[0][0] + s.red[1][0]) + (s.red[2][0] + s.red[3][0]);
-    __syncthreads();
+    lds_barrier();
     return t;
 }
 
@@ -115,30 +136,49 @@ __device__ __forceinline__ int next_child(const VerifyShared& s, int node, int a
 struct Piece {                                                           // a workgroup's part of a row: a thread has two groups of four elements
     int v0[2], at[2];
 };
+template <bool SHORT>                                                    // rows of fewer than four elements
 __device__ __forceinline__ void load_piece(const float* row, int V, const Piece& p, float4 (&x)[2]) {
-    with_row_loads(V, [&](auto load) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) x[i] = load(row, p.at[i]);
-    });
+    for (int i = 0; i < 2; ++i) {
+        if constexpr (SHORT) x[i] = load_short_row(row, p.at[i], V);
+        else x[i] = load_group(row, p.at[i]);
+    }
 #pragma unroll
     for (int i = 0; i < 2; ++i) mask_group(x[i], p.at[i], p.v0[i]);      // (what belongs to other threads, or lies past the row: -inf)
 }
 
-__global__ __launch_bounds__(kVerThreads, 2) void k_verify_nodes(VerifyArgs a) {
+template <bool SHORT>
+__global__ __launch_bounds__(kVerThreads, 3) void k_verify_nodes(VerifyArgs a) {
     __shared__ VerifyShared s;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = a.V, n = a.n;
     if (tid == 0) {
-        const uint32_t mark = __hip_atomic_load(a.ctl + 3 * kVerLine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        s.launch = __hip_atomic_load(a.ctl + 2 * kVerLine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        s.ticket = mark == kVerMark ? (int)__hip_atomic_fetch_add(a.ctl, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : -1;
+        // One trip: the launch's number and this workgroup's.  The last one to come makes both ready for the next launch.
+        const uint32_t mark = __hip_atomic_load(reinterpret_cast<const uint32_t*>(a.ctl + 16), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const uint64_t got = __hip_atomic_fetch_add(a.ctl, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const uint32_t launch = (uint32_t)(got >> 32), at = (uint32_t)got, count = (uint32_t)(a.B * a.G);
+        if (mark == kVerMark && at == count - 1)
+            __hip_atomic_store(a.ctl, (uint64_t)(launch == 0xffffffffu ? 1u : launch + 1) << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        s.launch = launch;
+        s.bad = 0;
+        s.ticket = mark == kVerMark && at < count ? (int)at : -1;
     }
-    __syncthreads();
+    lds_barrier();
     const uint32_t launch = __builtin_amdgcn_readfirstlane(s.launch);
     int ticket = __builtin_amdgcn_readfirstlane(s.ticket);
-    const bool prepared = ticket >= 0 && ticket < a.B * a.G;
+    const bool prepared = ticket >= 0;
     if (!prepared) ticket = blockIdx.x;
     const int b = ticket / a.G, c = ticket % a.G;
+    Piece piece;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        piece.v0[i] = c * kVerPiece + i * kVerThreads * 4 + tid * 4;
+        piece.at[i] = group_at(min(piece.v0[i], V - 1), V);
+    }
+    float4 x[2], ahead[2];                                               // the node's row, and that of its first child
+    load_piece<SHORT>(a.target + (size_t)b * a.N * V, V, piece, ahead);
     const int count = nodes_of(a.n_nodes, b, a.N);
+    const float T = a.temperature[b], u_res = a.u_res != nullptr ? a.u_res[b] : tabed_uniform(a.seed, a.round, (uint32_t)b, (uint32_t)(a.N - 1), 0);
+    if (tid < n) s.weight[tid] = a.weights[(size_t)b * n + tid];
     if (tid < a.N) {
         const size_t j = (size_t)b * a.N + tid;
         s.parent[tid] = tid == 0 ? -1 : parent_of(a.parents, b, tid, a.N);
@@ -147,25 +187,20 @@ __global__ __launch_bounds__(kVerThreads, 2) void k_verify_nodes(VerifyArgs a) {
         s.u[tid] = a.u_acc != nullptr ? a.u_acc[j] : tabed_uniform(a.seed, a.round, (uint32_t)b, (uint32_t)(tid - 1), 1);
         s.flag[tid] = 0;
     }
-    __syncthreads();
-    const float T = a.temperature[b];
+    lds_barrier();
     const bool greedy = !(T > 0.f);
     const double inv_t = greedy ? 1.0 : 1.0 / (double)T;
     uint64_t* const rec_b = a.rec + (size_t)b * a.N * a.G * 4;
     uint64_t* const dev_b = a.devrec + (size_t)b * a.gamma * a.G * n * 2;
-    Piece piece;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        piece.v0[i] = c * kVerPiece + i * kVerThreads * 4 + tid * 4;
-        piece.at[i] = group_at(min(piece.v0[i], V - 1), V);
-    }
 
     // A step's records, read by all into s.rec; false, for all, where one does not come.
     auto collect = [&](int step) {
         bool ok = true;
         const uint64_t* from = rec_b + (size_t)step * a.G * 4;
         for (int w = tid; w < a.G * 4; w += kVerThreads) s.rec[w / 4][w % 4] = hear(from + w, launch, ok);
-        return __syncthreads_or(!ok) == 0;
+        if (!ok) s.bad = 1;                                              // (never taken back: who reads it behind the barrier reads it before the next)
+        lds_barrier();
+        return s.bad == 0;
     };
     auto publish = [&](int step, uint32_t w0, uint32_t w1, double z) {   // by one thread
         uint64_t* to = rec_b + ((size_t)step * a.G + c) * 4;
@@ -178,15 +213,29 @@ __global__ __launch_bounds__(kVerThreads, 2) void k_verify_nodes(VerifyArgs a) {
     int cur = 0, depth = 0, step = 0, valid = 0, best = 0, level = 0;
     bool fine = prepared;
     double f[kVerE], q[kVerE], total = 0.0, scale = 0.0;                 // f times scale is p, at level 0
+    float4 d[kVerDraftsAtOnce][2];                                       // the rows of the node's first drafts
+    double dl[kVerDraftsAtOnce];                                         // and their log-sum-exp
+    auto load_drafts = [&](const float* drafts, const double* dlse, int j0) {
+#pragma unroll
+        for (int j = 0; j < kVerDraftsAtOnce; ++j) {
+            load_piece<SHORT>(drafts + (size_t)min(j0 + j, n - 1) * V, V, piece, d[j]);
+            dl[j] = dlse[min(j0 + j, n - 1)];
+        }
+    };
     while (count > 0 && fine) {
-        if (tid == 0) s.path[depth] = cur;
+        if (tid == 0) {
+            s.path[depth] = cur;
+            s.at_step[depth] = (int16_t)step;
+        }
         int child = next_child(s, cur, cur, count);
+        const int first = child;
         const bool want_dev = child >= 0 && a.dev != nullptr && depth < a.gamma;
         const float* const row = a.target + ((size_t)b * a.N + cur) * V;
         const float* const drafts = a.drafts + ((size_t)cur * a.B + b) * n * V;
         const double* const dlse = a.dlse + ((size_t)cur * a.B + b) * n;
-        float4 x[2];
-        load_piece(row, V, piece, x);
+        x[0] = ahead[0];
+        x[1] = ahead[1];
+        if (want_dev) load_drafts(drafts, dlse, 0);
         int y = child >= 0 ? s.token[child] : -1;
         const float ly = row[(unsigned)y < (unsigned)V ? y : 0];
 
@@ -201,7 +250,7 @@ __global__ __launch_bounds__(kVerThreads, 2) void k_verify_nodes(VerifyArgs a) {
             }
         top = wave_argmax(top);
         if (lane == 0) { s.redf[wave] = top.v; s.redi[wave] = top.i; }
-        __syncthreads();
+        lds_barrier();
         top = argmax_merge(argmax_merge(ArgMax{s.redf[0], s.redi[0]}, ArgMax{s.redf[1], s.redi[1]}),
                            argmax_merge(ArgMax{s.redf[2], s.redi[2]}, ArgMax{s.redf[3], s.redi[3]}));
         double sum = 0.0;
@@ -210,44 +259,43 @@ __global__ __launch_bounds__(kVerThreads, 2) void k_verify_nodes(VerifyArgs a) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float v = f4get(x[i], e);
-                f[i * 4 + e] = v == -INFINITY ? 0.0 : exp(((double)v - (double)top.v) * inv_t);
+                f[i * 4 + e] = v == -INFINITY ? 0.0 : exp64(((double)v - (double)top.v) * inv_t);
                 sum += f[i * 4 + e];
             }
         sum = group_sum(sum, s);
         if (tid == 0) publish(step, __builtin_bit_cast(uint32_t, top.v), (uint32_t)top.i, sum);
+        if (first >= 0) load_piece<SHORT>(a.target + ((size_t)b * a.N + first) * V, V, piece, ahead);      // (on its way while the others are waited for)
 
-        // ---- KL: the piece's sum of exp * ((l - max) / T - log q_j)
-        if (want_dev && !a.tvd) {
-            for (int j0 = 0; j0 < n; j0 += kVerDraftsAtOnce) {
-                float4 d[kVerDraftsAtOnce][2];
+        if (want_dev) {
+            // KL: the piece's sum of exp * ((l - max) / T - log q_j); TVD: of |p - q_j|.  Added up when the walk is over.
+            if (!a.tvd) {
+                for (int j0 = 0; j0 < n; j0 += kVerDraftsAtOnce) {
+                    if (j0 > 0) load_drafts(drafts, dlse, j0);
 #pragma unroll
-                for (int j = 0; j < kVerDraftsAtOnce; ++j) load_piece(drafts + (size_t)min(j0 + j, n - 1) * V, V, piece, d[j]);
+                    for (int j = 0; j < kVerDraftsAtOnce; ++j) {
+                        double kl = 0.0;
 #pragma unroll
-                for (int j = 0; j < kVerDraftsAtOnce; ++j) {
-                    const double lse = dlse[min(j0 + j, n - 1)];
-                    double kl = 0.0;
+                        for (int i = 0; i < 2; ++i)
 #pragma unroll
-                    for (int i = 0; i < 2; ++i)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const double w = f[i * 4 + e];
-                            const double t = ((double)f4get(x[i], e) - (double)top.v - (double)f4get(d[j][i], e)) * inv_t + lse;
-                            kl += w == 0.0 ? 0.0 : w * t;
-                        }
-                    kl = wave_sum(kl);
-                    if (lane == 0) s.red[wave][j] = kl;
+                            for (int e = 0; e < 4; ++e) {
+                                const double w = f[i * 4 + e];
+                                const double t = ((double)f4get(x[i], e) - (double)top.v - (double)f4get(d[j][i], e)) * inv_t + dl[j];
+                                kl += w == 0.0 ? 0.0 : w * t;
+                            }
+                        kl = wave_sum(kl);
+                        if (lane == 0) s.red[wave][j] = kl;
+                    }
+                    lds_barrier();
+                    if (tid < kVerDraftsAtOnce && j0 + tid < n) {
+                        const double kl = (s.red[0][tid] + s.red[1][tid]) + (s.red[2][tid] + s.red[3][tid]);
+                        uint64_t* to = dev_b + (((size_t)depth * a.G + c) * n + j0 + tid) * 2;
+                        say(to, lo32(kl), launch);
+                        say(to + 1, hi32(kl), launch);
+                    }
+                    lds_barrier();
                 }
-                __syncthreads();
-                if (tid < kVerDraftsAtOnce && j0 + tid < n) {
-                    const double kl = (s.red[0][tid] + s.red[1][tid]) + (s.red[2][tid] + s.red[3][tid]);
-                    uint64_t* to = dev_b + (((size_t)depth * a.G + c) * n + j0 + tid) * 2;
-                    say(to, lo32(kl), launch);
-                    say(to + 1, hi32(kl), launch);
-                }
-                __syncthreads();
             }
         }
-
         // ---- all pieces: maximum, arg-max, sum
         fine = collect(step);
         if (!fine) break;
@@ -258,28 +306,28 @@ __global__ __launch_bounds__(kVerThreads, 2) void k_verify_nodes(VerifyArgs a) {
         double z = 0.0;
         for (int g = lane; g < a.G; g += 64) {
             const float mg = as_float(s.rec[g][0]);
-            const double w = mg == -INFINITY ? 0.0 : exp(((double)mg - (double)all.v) * inv_t) * from32(s.rec[g][2], s.rec[g][3]);
+            const double w = mg == -INFINITY ? 0.0 : exp64(((double)mg - (double)all.v) * inv_t) * from32(s.rec[g][2], s.rec[g][3]);
             z += w;
             if (wave == 0) s.p_mass[g] = w;                              // (times 1 / z below)
         }
-        z = wave_sum(z);
+        const double inv_z = 1.0 / wave_sum(z);
         if (wave == 0)
-            for (int g = lane; g < a.G; g += 64) s.p_mass[g] /= z;
+            for (int g = lane; g < a.G; g += 64) s.p_mass[g] *= inv_z;
         best = all.i < V ? all.i : 0;                                    // (a row of -inf and NaN: 0)
-        scale = top.v == -INFINITY ? 0.0 : exp(((double)top.v - (double)all.v) * inv_t) / z;
+        scale = top.v == -INFINITY ? 0.0 : exp64(((double)top.v - (double)all.v) * inv_t) * inv_z;
 
         if (want_dev) {
             valid = depth + 1;
             if (a.tvd) {
                 for (int j = 0; j < n; ++j) {
-                    float4 d[2];
-                    load_piece(drafts + (size_t)j * V, V, piece, d);
+                    float4 dj[2];
+                    load_piece<SHORT>(drafts + (size_t)j * V, V, piece, dj);
                     const double lse = dlse[j];
                     double tv = 0.0;
 #pragma unroll
                     for (int i = 0; i < 2; ++i)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) tv += fabs(f[i * 4 + e] * scale - exp((double)f4get(d[i], e) * inv_t - lse));
+                        for (int e = 0; e < 4; ++e) tv += fabs(f[i * 4 + e] * scale - exp64((double)f4get(dj[i], e) * inv_t - lse));
                     tv = group_sum(tv, s);
                     if (tid == 0) {
                         uint64_t* to = dev_b + (((size_t)depth * a.G + c) * n + j) * 2;
@@ -288,32 +336,13 @@ __global__ __launch_bounds__(kVerThreads, 2) void k_verify_nodes(VerifyArgs a) {
                     }
                 }
             }
-            if (c == 0) {                                                // has all pieces' maxima and sums at hand: finishes the distances
-                bool ok = true;
-                for (int j = wave; j < n; j += kVerWaves) {
-                    double t = 0.0;
-                    for (int g = lane; g < a.G; g += 64) {
-                        const uint64_t* from = dev_b + (((size_t)depth * a.G + g) * n + j) * 2;
-                        const uint32_t lo = hear(from, launch, ok), hi = hear(from + 1, launch, ok);
-                        const float mg = as_float(s.rec[g][0]);
-                        const double up = ((double)mg - (double)all.v) * inv_t;
-                        if (a.tvd) t += from32(lo, hi);
-                        else if (mg != -INFINITY) t += exp(up) * (from32(lo, hi) + up * from32(s.rec[g][2], s.rec[g][3]));
-                    }
-                    t = wave_sum(t);
-                    if (lane == 0) a.dev[((size_t)b * a.gamma + depth) * n + j] = (float)(a.tvd ? 0.5 * t : t / z - log(z));
-                }
-                fine = ok;
-            }
-            fine = __syncthreads_or(!fine) == 0;
-            if (!fine) break;
         }
-        __syncthreads();                                                 // p_mass is whole, s.rec has been read
+        lds_barrier();                                                 // p_mass is whole, s.rec has been read
 
         // ---- the children, in order
         level = 0;
         total = 1.0;
-        double fy = (unsigned)y < (unsigned)V ? exp(((double)ly - (double)all.v) * inv_t) / z : 0.0;
+        double fy = (unsigned)y < (unsigned)V ? exp64(((double)ly - (double)all.v) * inv_t) * inv_z : 0.0;
         int hit = -1;
         while (child >= 0) {
             const bool there = (unsigned)y < (unsigned)V;
@@ -339,17 +368,15 @@ __global__ __launch_bounds__(kVerThreads, 2) void k_verify_nodes(VerifyArgs a) {
                     q[e] = 0.0;
                 }
                 for (int j0 = 0; j0 < n; j0 += kVerDraftsAtOnce) {
-                    float4 d[kVerDraftsAtOnce][2];
-#pragma unroll
-                    for (int j = 0; j < kVerDraftsAtOnce; ++j) load_piece(drafts + (size_t)min(j0 + j, n - 1) * V, V, piece, d[j]);
+                    if (!want_dev || n > kVerDraftsAtOnce) load_drafts(drafts, dlse, j0);
 #pragma unroll
                     for (int j = 0; j < kVerDraftsAtOnce; ++j) {
                         if (j0 + j >= n) break;
-                        const double lse = dlse[j0 + j], w = (double)a.weights[(size_t)b * n + j0 + j];
+                        const double w = (double)s.weight[j0 + j];
 #pragma unroll
                         for (int i = 0; i < 2; ++i)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) q[i * 4 + e] += w * exp((double)f4get(d[j][i], e) * inv_t - lse);
+                            for (int e = 0; e < 4; ++e) q[i * 4 + e] += w * exp64((double)f4get(d[j][i], e) * inv_t - dl[j]);
                     }
                 }
             }
@@ -367,7 +394,7 @@ __global__ __launch_bounds__(kVerThreads, 2) void k_verify_nodes(VerifyArgs a) {
             zsum = wave_sum(zsum);
             fn = wave_sum(fn);
             if (lane == 0) { s.red[wave][0] = zsum; s.red[wave][1] = fn; }
-            __syncthreads();
+            lds_barrier();
             if (tid == 0) {
                 const double ft = (s.red[0][1] + s.red[1][1]) + (s.red[2][1] + s.red[3][1]);
                 publish(step, lo32(ft), hi32(ft), (s.red[0][0] + s.red[1][0]) + (s.red[2][0] + s.red[3][0]));
@@ -385,9 +412,10 @@ __global__ __launch_bounds__(kVerThreads, 2) void k_verify_nodes(VerifyArgs a) {
             total = wave_sum(zt);
             fy = 0.0;
             if ((unsigned)y < (unsigned)V) fy = from32(s.rec[y / kVerPiece][0], s.rec[y / kVerPiece][1]);
-            __syncthreads();                                             // mass is whole, s.rec has been read
+            lds_barrier();                                             // mass is whole, s.rec has been read
         }
         if (!fine || hit < 0) break;
+        if (hit != first) load_piece<SHORT>(a.target + ((size_t)b * a.N + hit) * V, V, piece, ahead);
         cur = hit;
         ++depth;
     }
@@ -396,8 +424,6 @@ __global__ __launch_bounds__(kVerThreads, 2) void k_verify_nodes(VerifyArgs a) {
     if (count > 0 && fine && !greedy) {
         const bool gone = level > 0 && !(total > 0.0);                   // nothing is left of f: p again
         if (gone) {
-            float4 x[2];
-            load_piece(a.target + ((size_t)b * a.N + cur) * V, V, piece, x);
             float m = -INFINITY;
 #pragma unroll
             for (int i = 0; i < 2; ++i)
@@ -409,18 +435,17 @@ __global__ __launch_bounds__(kVerThreads, 2) void k_verify_nodes(VerifyArgs a) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float v = f4get(x[i], e);
-                    f[i * 4 + e] = v == -INFINITY ? 0.0 : exp(((double)v - (double)m) * inv_t) * scale;
+                    f[i * 4 + e] = v == -INFINITY ? 0.0 : exp64(((double)v - (double)m) * inv_t) * scale;
                 }
         } else if (level == 0) {
 #pragma unroll
             for (int e = 0; e < kVerE; ++e) f[e] *= scale;
         }
         const double* const mass = level == 0 || gone ? s.p_mass : s.mass;
-        const float u = a.u_res != nullptr ? a.u_res[b] : tabed_uniform(a.seed, a.round, (uint32_t)b, (uint32_t)(a.N - 1), 0);
         // Every wave of every workgroup the same: the first piece in which the prefix exceeds u Z, else the last with any mass, else the first.
         double whole = 0.0;
         for (int g0 = 0; g0 < a.G; g0 += 64) whole += wave_sum(g0 + lane < a.G ? mass[g0 + lane] : 0.0);
-        const double goal = (double)u * whole;
+        const double goal = (double)u_res * whole;
         double run = 0.0, before = 0.0;
         int owner = 0;
         bool crossed = false;
@@ -477,7 +502,7 @@ __global__ __launch_bounds__(kVerThreads, 2) void k_verify_nodes(VerifyArgs a) {
 
     // ---- the first workgroup tells the way
     if (c == 0) {
-        __syncthreads();
+        lds_barrier();
         const int said = count > 0 && fine ? depth + 1 : 0;              // nodes of the path
         if (tid < a.N) {
             const size_t at = (size_t)b * a.N + tid;
@@ -492,11 +517,40 @@ __global__ __launch_bounds__(kVerThreads, 2) void k_verify_nodes(VerifyArgs a) {
             if (a.n_valid != nullptr) a.n_valid[b] = said > 0 ? valid : 0;
         }
     }
-    if (prepared && tid == 0) {                                          // the last to leave makes the workspace ready for the next launch
-        if (__hip_atomic_fetch_add(a.ctl + kVerLine, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)(a.B * a.G) - 1) {
-            __hip_atomic_store(a.ctl, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            __hip_atomic_store(a.ctl + kVerLine, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            __hip_atomic_store(a.ctl + 2 * kVerLine, launch + 1 == 0 ? 1u : launch + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+
+    // ---- the distances: the positions are dealt to the workgroups, a wave adds up a draft's
+    if (!fine) return;
+    lds_barrier();
+    for (int i = c; i < valid; i += a.G) {
+        const uint64_t* const from = rec_b + (size_t)s.at_step[i] * a.G * 4;
+        bool ok = true;
+        for (int j = wave; j < n; j += kVerWaves) {
+            float m[2] = {-INFINITY, -INFINITY};
+            double sum[2] = {0.0, 0.0}, part[2] = {0.0, 0.0};
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int g = h * 64 + lane;
+                if (g >= a.G) continue;
+                const uint64_t* const dev = dev_b + (((size_t)i * a.G + g) * n + j) * 2;
+                m[h] = as_float(hear(from + g * 4, launch, ok));
+                sum[h] = from32(hear(from + g * 4 + 2, launch, ok), hear(from + g * 4 + 3, launch, ok));
+                part[h] = from32(hear(dev, launch, ok), hear(dev + 1, launch, ok));
+            }
+            const float top = wave_max(fmaxf(m[0], m[1]));
+            double z = 0.0, t = 0.0;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const double up = ((double)m[h] - (double)top) * inv_t;
+                if (a.tvd) t += part[h];
+                else if (m[h] != -INFINITY) {
+                    const double w = exp64(up);
+                    z += w * sum[h];
+                    t += w * (part[h] + up * sum[h]);
+                }
+            }
+            z = wave_sum(z);
+            t = wave_sum(t);
+            if (lane == 0) a.dev[((size_t)b * a.gamma + i) * n + j] = (float)(a.tvd ? 0.5 * t : t / z - log(z));
         }
     }
 }
@@ -513,7 +567,7 @@ NodesVerifyLayout nodes_verify_layout(const tabed_cfg& c, int N) {
 
 __global__ void k_verify_nodes_init(uint32_t* ws, size_t words) {
     for (size_t i = blockIdx.x * (size_t)blockDim.x + threadIdx.x; i < words; i += (size_t)gridDim.x * blockDim.x)
-        ws[i] = i == 2 * kVerLine ? 1u : i == 3 * kVerLine ? kVerMark : 0u;
+        ws[i] = i == 1 ? 1u : i == 32 ? kVerMark : 0u;                    // (launch 1, workgroup 0)
 }
 hipError_t launch_nodes_verify_init(const tabed_cfg& c, int N, char* ws, hipStream_t s) {
     const size_t words = nodes_verify_layout(c, N).total / 4;
@@ -528,9 +582,9 @@ hipError_t launch_verify_nodes(const tabed_cfg& c, char* ws, uint64_t round, int
     ProfScope prof(TABED_K_TREE, s);
     const NodesVerifyLayout L = nodes_verify_layout(c, N);
     const VerifyArgs a{c.V, c.n, c.B, N, L.G, c.gamma, c.distance == 1, c.seed, round, target_logits, draft_logits, draft_lse, tokens, node_q, parents,
-                       n_nodes, weights, temperature, u_acc, u_res, path, n_path, out_tokens, flags, dev, n_valid, reinterpret_cast<uint32_t*>(ws),
+                       n_nodes, weights, temperature, u_acc, u_res, path, n_path, out_tokens, flags, dev, n_valid, reinterpret_cast<uint64_t*>(ws),
                        reinterpret_cast<uint64_t*>(ws + L.off_rec), reinterpret_cast<uint64_t*>(ws + L.off_dev)};
-    launch(&prof, k_verify_nodes, dim3((unsigned)(c.B * L.G)), dim3(kVerThreads), 0, s, a);
+    launch(&prof, c.V < 4 ? k_verify_nodes<true> : k_verify_nodes<false>, dim3((unsigned)(c.B * L.G)), dim3(kVerThreads), 0, s, a);
     return hipGetLastError();
 }
 
