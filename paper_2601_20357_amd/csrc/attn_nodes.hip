@@ -17,30 +17,36 @@ static auto with_hd(int hd, F&& f) {
     }
 }
 
+struct NodesPlan {
+    int tiles, per_tile, slots, split, fill, min_tiles;
+};
 static NodesPlan plan_of(const tabed_cache_paged& c, int rows, int N, int q_heads) {
     const int queries = N * (q_heads / c.kv_heads);
     NodesPlan p{};
-    int room = 0, kt = 32;                                               // workgroups that run at a time
+    int room = 0, tokens = 0, unit = 1;                                  // workgroups that run at a time, tokens of a tile, queries of a wave
     with_hd(c.head_dim, [&](auto hd) {
         auto take = [&](auto v) {
             using T = decltype(v);
-            p.queries = T::kQueries;
-            kt = T::KT;
-            room = 256 * std::max(1, std::min(163840 / (int)T::kLds, 8 / T::kWaves));
+            p.per_tile = T::kQueries;
+            tokens = T::kTokens;
+            unit = T::kUnit;
+            room = 256 * std::max(1, std::min(163840 / (int)(T::kLds + sizeof(NodesShared)), 512 / T::kThreads));
             return 0;
         };
         return c.type == 2 ? with_nodes_variant<decltype(hd)::value, true>(queries, take) : with_nodes_variant<decltype(hd)::value, false>(queries, take);
     });
-    p.tiles = (queries + p.queries - 1) / p.queries;
+    p.tiles = (queries + p.per_tile - 1) / p.per_tile;
+    if (p.tiles > 1) p.per_tile = ((queries + p.tiles - 1) / p.tiles + unit - 1) / unit * unit;      // (as even as whole units of a wave leave them)
     const int64_t units = (int64_t)c.kv_heads * p.tiles;                 // workgroups of a slot
-    const int64_t fill = room / units, each = std::max<int64_t>(fill, 2 * rows);
+    const int64_t most = ((int64_t)c.max_blocks * TABED_CACHE_BLOCK + tokens - 1) / tokens;      // tiles of the longest row there can be
+    p.min_tiles = std::max(1, 1024 / tokens);
     p.slots = rows;
-    p.min_tiles = 512 / kt;
-    const int64_t most = ((int64_t)c.max_blocks * TABED_CACHE_BLOCK + kt - 1) / kt;   // tiles of the longest row there can be
-    if (rows <= kMaxSplitRows && most > (fill > rows ? 1 : 8) * p.min_tiles) {
+    p.fill = (int)std::max<int64_t>(room / units, 2 * rows);
+    // Ranges of 1024 tokens or more (shorter ones cost more in the second launch than they save).  Where rows alone fill the chip they are cut only if one can be so long
+    // that the others would wait for it.
+    if (rows <= kMaxSplitRows && most > (room / units > rows ? 1 : 8) * p.min_tiles) {
         p.split = 1;
-        p.target = (int)std::max<int64_t>(1, each - rows / 2);
-        p.slots = (int)std::min<int64_t>(p.target + rows, rows * ((most + p.min_tiles - 1) / p.min_tiles));
+        p.slots = (int)std::min<int64_t>(p.fill, rows * ((most + p.min_tiles - 1) / p.min_tiles));
     }
     return p;
 }
@@ -50,8 +56,8 @@ NodesAttnLayout nodes_attn_layout(const tabed_cache_paged& c, int rows, int N, i
     const NodesPlan p = plan_of(c, rows, N, q_heads);
     NodesAttnLayout L{kRangesBytes, kRangesBytes, kRangesBytes};
     if (p.split) {
-        const size_t places = (size_t)p.slots * c.kv_heads * p.tiles * p.queries;
-        L.off_o = L.off_ml + up(places * 8);
+        const size_t places = (size_t)p.slots * c.kv_heads * p.tiles * p.per_tile;
+        L.off_o = L.off_ml + up(places * 16);
         L.total = L.off_o + up(places * c.head_dim * 4);
     }
     return L;
@@ -64,10 +70,10 @@ hipError_t launch_attention_nodes(const tabed_cache_paged& c, int layer, char* w
     ProfScope prof(TABED_K_BODY, s);
     const NodesPlan p = plan_of(c, rows, N, q_heads);
     const NodesAttnLayout L = nodes_attn_layout(c, rows, N, q_heads);
-    const NodesAttnArgs a{paged_view(c, layer), rows, N, q_heads, q_heads / c.kv_heads, p.tiles, p.slots, p.split, p.target, p.min_tiles, q, out, lse, q_row, q_tok,
-                          out_row, out_tok, ctx_len, parents, n_nodes, scale * 1.44269504088896340736f, reinterpret_cast<int2*>(ws),
-                          reinterpret_cast<float2*>(ws + L.off_ml), reinterpret_cast<float*>(ws + L.off_o)};
-    return with_hd(c.head_dim, [&](auto hd) { return launch_nodes_hd<decltype(hd)::value>(c.type == 2, N * a.group, &prof, a, s); });
+    const NodesAttnArgs a{paged_view(c, layer), rows, N, q_heads, q_heads / c.kv_heads, p.tiles, p.per_tile, p.slots, p.split, p.fill, p.min_tiles, q, out, lse,
+                          q_row, q_tok, out_row, out_tok, ctx_len, parents, n_nodes, scale * 1.44269504088896340736f, reinterpret_cast<int2*>(ws),
+                          reinterpret_cast<float4*>(ws + L.off_ml), reinterpret_cast<float*>(ws + L.off_o)};
+    return with_hd(c.head_dim, [&](auto hd) { return launch_nodes_hd<decltype(hd)::value>(c.type == 2, &prof, a, s); });
 }
 
 }  // namespace tabed

@@ -182,8 +182,8 @@ hipError_t launch_append_nodes(const tabed_cache_paged& c, int layer, int rows, 
 hipError_t launch_keep_nodes(const tabed_cache_paged& c, int rows, int N, const int32_t* ctx_base, const int32_t* path, const int32_t* n_path,
                              int32_t* ctx_len, hipStream_t s);
 struct NodesAttnLayout {
-    size_t off_ml;       // float2 [slots, kv_heads, tiles][queries of a workgroup] maxima and sums of ranges; before it the ranges of every row
-    size_t off_o;        // float [slots, kv_heads, tiles][queries of a workgroup][head_dim] their sums of values
+    size_t off_ml;       // float4 [slots, kv_heads, tiles][queries of a tile] maxima and sums of ranges; before it the ranges of every row
+    size_t off_o;        // float [slots, kv_heads, tiles][queries of a tile][head_dim] their sums of values
     size_t total;
 };
 NodesAttnLayout nodes_attn_layout(const tabed_cache_paged& c, int rows, int N, int q_heads);
