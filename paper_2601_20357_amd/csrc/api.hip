@@ -605,7 +605,8 @@ static int validate_attention_nodes(const tabed_cache_paged* cache, int32_t rows
     if (rc == TABED_OK) rc = validate_nodes(rows, N);
     if (rc != TABED_OK) return rc;
     if (q_heads < 1 || q_heads > 16384) return TABED_ERANGE;
-    return q_heads % cache->kv_heads != 0 ? TABED_EINVAL : TABED_OK;
+    if (q_heads % cache->kv_heads != 0) return TABED_EINVAL;
+    return nodes_attn_workgroups(*cache, rows, N, q_heads) > kMaxWorkgroups ? TABED_ERANGE : TABED_OK;
 }
 
 size_t tabed_attention_nodes_workspace_bytes(const tabed_cache_paged* cache, int32_t rows, int32_t N, int32_t q_heads) {

@@ -62,6 +62,10 @@ NodesAttnLayout nodes_attn_layout(const tabed_cache_paged& c, int rows, int N, i
     }
     return L;
 }
+int64_t nodes_attn_workgroups(const tabed_cache_paged& c, int rows, int N, int q_heads) {
+    const NodesPlan p = plan_of(c, rows, N, q_heads);
+    return ((int64_t)p.slots * c.kv_heads + 7) / 8 * 8 * p.tiles;
+}
 hipError_t launch_nodes_attn_init(char*, hipStream_t) { return hipSuccess; }         // (nothing is expected in it)
 
 hipError_t launch_attention_nodes(const tabed_cache_paged& c, int layer, char* ws, int rows, int N, int q_heads, const uint16_t* q, int64_t q_row,

@@ -68,7 +68,7 @@ ATTN_OK = dict(cache=cache(), layer=0, ws=P, rows=3, N=8, qh=4, q=P, qrow=2048, 
 
 @pytest.mark.parametrize("changed,code", [(dict(cache=cache(**c)), e) for c, e in BAD_CACHES] + [
     (dict(cache=None), ENULL), (dict(layer=-1), ERANGE), (dict(layer=2), ERANGE), (dict(ws=None), ENULL), (dict(rows=0), ERANGE), (dict(rows=65536), ERANGE),
-    (dict(N=0), ERANGE), (dict(N=257), ERANGE), (dict(qh=0), ERANGE), (dict(qh=3), EINVAL), (dict(qh=16386), ERANGE), (dict(q=None), ENULL), (dict(ctx=None), ENULL),
+    (dict(N=0), ERANGE), (dict(N=257), ERANGE), (dict(cache=cache(kv_heads=1024), rows=65535, qh=1024, qrow=65536, qtok=65536, orow=65536, otok=65536), ERANGE), (dict(qh=0), ERANGE), (dict(qh=3), EINVAL), (dict(qh=16386), ERANGE), (dict(q=None), ENULL), (dict(ctx=None), ENULL),
     (dict(out=None), ENULL), (dict(qrow=255), EINVAL), (dict(qtok=0), EINVAL), (dict(orow=255), EINVAL), (dict(otok=255), EINVAL), (dict(scale=0.0), EINVAL),
     (dict(scale=float("nan")), EINVAL), (dict(scale=float("inf")), EINVAL), (dict(ws=C.c_void_p(0x1008)), EALIGN), (dict(q=ODD), EALIGN), (dict(out=ODD), EALIGN),
     (dict(ctx=ODD), EALIGN), (dict(parents=ODD), EALIGN), (dict(nodes=ODD), EALIGN), (dict(lse=ODD), EALIGN)])
