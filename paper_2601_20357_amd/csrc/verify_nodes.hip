@@ -1,7 +1,7 @@
 // Verification of a tree of drafted tokens: multi-round rejection sampling from the root down, one launch.
 //
 // The walk is sequential: which node comes next follows from the rows of the one before it, and only the rows of the nodes on the way are
-// read.  So that each of these steps has the chip's bandwidth all the same, a sequence's vocabulary is cut into pieces of kVerPiece, a workgroup
+// read.  So that each of these steps has the chip's bandwidth all the same, a sequence's vocabulary is cut into pieces of 1024 or 2048, a workgroup
 // each, which walk together: at a step every workgroup reduces its piece, stores what it found, reads what the others found, and comes to
 // the same decision as they do from the same numbers in the same order.  A piece stays in registers: the target's row is read once at a node, the
 // drafts' once for the distances and once more, out of a cache, where a child is rejected; f is kept from level to level.  The masses of the
@@ -19,8 +19,8 @@
 // the same; a row whose wait ended unanswered is left without a token, flagged.
 //
 // What bounds it: the steps, one after the other.  One is 4 to 5 us: 1 for the row's maximum and exponentials, 1.5 until all pieces' are known, 1 for their
-// sum, the rest for the distances, the test and the next node's rows; a launch with one node and nothing to test takes 12.  16 sequences of 22 nodes, V = 32000, 4
-// drafts: 40 us (the longest path of 16 visits five nodes).  64 sequences, V = 128256, 8 drafts: 190 us for some 360 MB.
+// sum, the rest for the distances, the test and the next node's rows; a launch with one node and nothing to test takes 8 to 12.  16 sequences of 22 nodes, V = 32000, 4
+// drafts: 40 us (the longest path of 16 visits five nodes); 1 of 6, a path of four: 23 us.  64 sequences, V = 128256, 8 drafts: 190 us for some 360 MB.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -31,8 +31,7 @@
 
 namespace tabed {
 
-constexpr int kVerThreads = 256, kVerWaves = kVerThreads / 64, kVerE = 8, kVerPiece = kVerThreads * kVerE;
-constexpr int kVerMaxPieces = 262144 / kVerPiece;
+constexpr int kVerThreads = 256, kVerWaves = kVerThreads / 64, kVerMaxPieces = 128;      // pieces are of 4 or 8 elements a thread
 constexpr int kVerDraftsAtOnce = 4;
 constexpr size_t kVerControl = 256;                                      // uint64: the launch's number and the next workgroup's; uint32 in the next line: mark
 constexpr uint32_t kVerMark = 0x7ab3d0deu;
@@ -137,22 +136,25 @@ __device__ __forceinline__ int next_child(const VerifyShared& s, int node, int a
     return -1;
 }
 
-struct Piece {                                                           // a workgroup's part of a row: a thread has two groups of four elements
-    int v0[2], at[2];
+// A workgroup's part of a row, in groups of four elements a thread.
+template <int NG>
+struct Piece {
+    int v0[NG], at[NG];
 };
-template <bool SHORT>                                                    // rows of fewer than four elements
-__device__ __forceinline__ void load_piece(const float* row, int V, const Piece& p, float4 (&x)[2]) {
+template <bool SHORT, int NG>                                            // SHORT: rows of fewer than four elements
+__device__ __forceinline__ void load_piece(const float* row, int V, const Piece<NG>& p, float4 (&x)[NG]) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < NG; ++i) {
         if constexpr (SHORT) x[i] = load_short_row(row, p.at[i], V);
         else x[i] = load_group(row, p.at[i]);
     }
 #pragma unroll
-    for (int i = 0; i < 2; ++i) mask_group(x[i], p.at[i], p.v0[i]);      // (what belongs to other threads, or lies past the row: -inf)
+    for (int i = 0; i < NG; ++i) mask_group(x[i], p.at[i], p.v0[i]);     // (what belongs to other threads, or lies past the row: -inf)
 }
 
-template <bool SHORT>
+template <bool SHORT, int NG>
 __global__ __launch_bounds__(kVerThreads, 3) void k_verify_nodes(VerifyArgs a) {
+    constexpr int kVerE = 4 * NG, kVerPiece = kVerThreads * kVerE;
     __shared__ VerifyShared s;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = a.V, n = a.n;
     if (tid == 0) {
@@ -172,14 +174,14 @@ __global__ __launch_bounds__(kVerThreads, 3) void k_verify_nodes(VerifyArgs a) {
     const bool prepared = ticket >= 0;
     if (!prepared) ticket = blockIdx.x;
     const int b = ticket / a.G, c = ticket % a.G;
-    Piece piece;
+    Piece<NG> piece;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < NG; ++i) {
         piece.v0[i] = c * kVerPiece + i * kVerThreads * 4 + tid * 4;
         piece.at[i] = group_at(min(piece.v0[i], V - 1), V);
     }
-    float4 x[2], ahead[2];                                               // the node's row, and that of its first child
-    load_piece<SHORT>(a.target + (size_t)b * a.N * V, V, piece, ahead);
+    float4 x[NG], ahead[NG];                                             // the node's row, and that of its first child
+    load_piece<SHORT, NG>(a.target + (size_t)b * a.N * V, V, piece, ahead);
     const int count = nodes_of(a.n_nodes, b, a.N);
     const float T = a.temperature[b], u_res = a.u_res != nullptr ? a.u_res[b] : tabed_uniform(a.seed, a.round, (uint32_t)b, (uint32_t)(a.N - 1), 0);
     if (tid < n) s.weight[tid] = a.weights[(size_t)b * n + tid];
@@ -217,12 +219,12 @@ __global__ __launch_bounds__(kVerThreads, 3) void k_verify_nodes(VerifyArgs a) {
     int cur = 0, depth = 0, step = 0, valid = 0, best = 0, level = 0;
     bool fine = prepared;
     double f[kVerE], q[kVerE], total = 0.0, scale = 0.0;                 // f times scale is p, at level 0
-    float4 d[kVerDraftsAtOnce][2];                                       // the rows of the node's first drafts
+    float4 d[kVerDraftsAtOnce][NG];                                      // the rows of the node's first drafts
     double dl[kVerDraftsAtOnce];                                         // and their log-sum-exp
     auto load_drafts = [&](const float* drafts, const double* dlse, int j0) {
 #pragma unroll
         for (int j = 0; j < kVerDraftsAtOnce; ++j) {
-            load_piece<SHORT>(drafts + (size_t)min(j0 + j, n - 1) * V, V, piece, d[j]);
+            load_piece<SHORT, NG>(drafts + (size_t)min(j0 + j, n - 1) * V, V, piece, d[j]);
             dl[j] = dlse[min(j0 + j, n - 1)];
         }
     };
@@ -237,8 +239,8 @@ __global__ __launch_bounds__(kVerThreads, 3) void k_verify_nodes(VerifyArgs a) {
         const float* const row = a.target + ((size_t)b * a.N + cur) * V;
         const float* const drafts = a.drafts + ((size_t)cur * a.B + b) * n * V;
         const double* const dlse = a.dlse + ((size_t)cur * a.B + b) * n;
-        x[0] = ahead[0];
-        x[1] = ahead[1];
+#pragma unroll
+        for (int i = 0; i < NG; ++i) x[i] = ahead[i];
         if (want_dev) load_drafts(drafts, dlse, 0);
         int y = child >= 0 ? s.token[child] : -1;
         const float ly = row[(unsigned)y < (unsigned)V ? y : 0];
@@ -246,7 +248,7 @@ __global__ __launch_bounds__(kVerThreads, 3) void k_verify_nodes(VerifyArgs a) {
         // ---- the piece's maximum, and the sum of exp
         ArgMax top{-INFINITY, 0x7fffffff};
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < NG; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float v = f4get(x[i], e);
@@ -259,7 +261,7 @@ __global__ __launch_bounds__(kVerThreads, 3) void k_verify_nodes(VerifyArgs a) {
                            argmax_merge(ArgMax{s.redf[2], s.redi[2]}, ArgMax{s.redf[3], s.redi[3]}));
         double sum = 0.0;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < NG; ++i)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float v = f4get(x[i], e);
@@ -268,7 +270,7 @@ __global__ __launch_bounds__(kVerThreads, 3) void k_verify_nodes(VerifyArgs a) {
             }
         sum = group_sum(sum, s);
         if (tid == 0) publish(step, __builtin_bit_cast(uint32_t, top.v), (uint32_t)top.i, sum);
-        if (first >= 0) load_piece<SHORT>(a.target + ((size_t)b * a.N + first) * V, V, piece, ahead);      // (on its way while the others are waited for)
+        if (first >= 0) load_piece<SHORT, NG>(a.target + ((size_t)b * a.N + first) * V, V, piece, ahead);      // (on its way while the others are waited for)
 
         if (want_dev) {
             // KL: the piece's sum of exp * ((l - max) / T - log q_j); TVD: of |p - q_j|.  Added up when the walk is over.
@@ -279,7 +281,7 @@ __global__ __launch_bounds__(kVerThreads, 3) void k_verify_nodes(VerifyArgs a) {
                     for (int j = 0; j < kVerDraftsAtOnce; ++j) {
                         double kl = 0.0;
 #pragma unroll
-                        for (int i = 0; i < 2; ++i)
+                        for (int i = 0; i < NG; ++i)
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
                                 const double w = f[i * 4 + e];
@@ -324,12 +326,12 @@ __global__ __launch_bounds__(kVerThreads, 3) void k_verify_nodes(VerifyArgs a) {
             valid = depth + 1;
             if (a.tvd) {
                 for (int j = 0; j < n; ++j) {
-                    float4 dj[2];
-                    load_piece<SHORT>(drafts + (size_t)j * V, V, piece, dj);
+                    float4 dj[NG];
+                    load_piece<SHORT, NG>(drafts + (size_t)j * V, V, piece, dj);
                     const double lse = dlse[j];
                     double tv = 0.0;
 #pragma unroll
-                    for (int i = 0; i < 2; ++i)
+                    for (int i = 0; i < NG; ++i)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) tv += fabs(f[i * 4 + e] * scale - exp64((double)f4get(dj[i], e) * inv_t - lse));
                     tv = group_sum(tv, s);
@@ -378,7 +380,7 @@ __global__ __launch_bounds__(kVerThreads, 3) void k_verify_nodes(VerifyArgs a) {
                         if (j0 + j >= n) break;
                         const double w = (double)s.weight[j0 + j];
 #pragma unroll
-                        for (int i = 0; i < 2; ++i)
+                        for (int i = 0; i < NG; ++i)
 #pragma unroll
                             for (int e = 0; e < 4; ++e) q[i * 4 + e] += w * exp64((double)f4get(d[j][i], e) * inv_t - dl[j]);
                     }
@@ -387,7 +389,7 @@ __global__ __launch_bounds__(kVerThreads, 3) void k_verify_nodes(VerifyArgs a) {
             const double inv = total > 0.0 ? 1.0 / total : 0.0;
             double zsum = 0.0, fn = 0.0;
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < NG; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     double& fe = f[i * 4 + e];
@@ -419,7 +421,7 @@ __global__ __launch_bounds__(kVerThreads, 3) void k_verify_nodes(VerifyArgs a) {
             lds_barrier();                                             // mass is whole, s.rec has been read
         }
         if (!fine || hit < 0) break;
-        if (hit != first) load_piece<SHORT>(a.target + ((size_t)b * a.N + hit) * V, V, piece, ahead);
+        if (hit != first) load_piece<SHORT, NG>(a.target + ((size_t)b * a.N + hit) * V, V, piece, ahead);
         cur = hit;
         ++depth;
     }
@@ -430,12 +432,12 @@ __global__ __launch_bounds__(kVerThreads, 3) void k_verify_nodes(VerifyArgs a) {
         if (gone) {
             float m = -INFINITY;
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < NG; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) m = fmaxf(m, f4get(x[i], e));
             m = block_max(m, s.redf);
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < NG; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float v = f4get(x[i], e);
@@ -468,7 +470,7 @@ __global__ __launch_bounds__(kVerThreads, 3) void k_verify_nodes(VerifyArgs a) {
         if (c == owner) {
             int first = 0x7fffffff, last = -1;
             double lo[kVerE];
-            for (int i = 0; i < 2; ++i) {                                // (the groups one after the other: the order of the row)
+            for (int i = 0; i < NG; ++i) {                                // (the groups one after the other: the order of the row)
                 double part, at = 0.0;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) at += f[i * 4 + e];
@@ -488,7 +490,7 @@ __global__ __launch_bounds__(kVerThreads, 3) void k_verify_nodes(VerifyArgs a) {
             const int pick = block_pick_key(first, last, s.redi, s.redk);
             uint8_t flag = (crossed ? 0 : TABED_FLAG_DEGENERATE) | (gone ? TABED_FLAG_DEGENERATE : 0);
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < NG; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     if (f[i * 4 + e] > 0.0 && piece.at[i] + e == pick) {
@@ -559,13 +561,23 @@ __global__ __launch_bounds__(kVerThreads, 3) void k_verify_nodes(VerifyArgs a) {
     }
 }
 
+// Elements of a workgroup's piece: 4 or 8 a thread.  Small pieces end each step sooner as long as a lane polls one workgroup's record and the chip
+// has room (rows of 32000: 1 sequence 23.2 us against 25.9, 8 sequences 36.7 against 38.1), and then cost more than they give (16 sequences 42.8
+// against 40.6; 1 sequence of 128256 19.4 against 18.5; 4 of them 46.6 against 38.9).
+constexpr int kVerSmallGroups = 256;                                     // workgroups of a launch
+static int piece_of(const tabed_cfg& c) {
+    constexpr int small = kVerThreads * 4;
+    const int pieces = (c.V + small - 1) / small;
+    return pieces <= 64 && (int64_t)c.B * pieces <= kVerSmallGroups ? small : kVerThreads * 8;
+}
 NodesVerifyLayout nodes_verify_layout(const tabed_cfg& c, int N) {
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
     NodesVerifyLayout L;
-    L.G = (c.V + kVerPiece - 1) / kVerPiece;
-    L.off_rec = kVerControl;
-    L.off_dev = L.off_rec + up((size_t)c.B * N * L.G * 4 * 8);
-    L.total = L.off_dev + up((size_t)c.B * c.gamma * L.G * c.n * 2 * 8);
+    L.G = (c.V + piece_of(c) - 1) / piece_of(c);
+    const size_t groups = std::max<size_t>((size_t)c.B * ((c.V + kVerThreads * 8 - 1) / (kVerThreads * 8)), kVerSmallGroups);
+    L.off_rec = kVerControl;                                             // (never less for more sequences or longer rows, whatever their pieces)
+    L.off_dev = L.off_rec + up(groups * N * 4 * 8);
+    L.total = L.off_dev + up(groups * c.gamma * c.n * 2 * 8);
     return L;
 }
 
@@ -588,7 +600,10 @@ hipError_t launch_verify_nodes(const tabed_cfg& c, char* ws, uint64_t round, int
     const VerifyArgs a{c.V, c.n, c.B, N, L.G, c.gamma, c.distance == 1, c.seed, round, target_logits, draft_logits, draft_lse, tokens, node_q, parents,
                        n_nodes, weights, temperature, u_acc, u_res, path, n_path, out_tokens, flags, dev, n_valid, reinterpret_cast<uint64_t*>(ws),
                        reinterpret_cast<uint64_t*>(ws + L.off_rec), reinterpret_cast<uint64_t*>(ws + L.off_dev)};
-    launch(&prof, c.V < 4 ? k_verify_nodes<true> : k_verify_nodes<false>, dim3((unsigned)(c.B * L.G)), dim3(kVerThreads), 0, s, a);
+    const dim3 grid((unsigned)(c.B * L.G)), block(kVerThreads);
+    if (c.V < 4) launch(&prof, k_verify_nodes<true, 1>, grid, block, 0, s, a);
+    else if (piece_of(c) == kVerThreads * 4) launch(&prof, k_verify_nodes<false, 1>, grid, block, 0, s, a);
+    else launch(&prof, k_verify_nodes<false, 2>, grid, block, 0, s, a);
     return hipGetLastError();
 }
 

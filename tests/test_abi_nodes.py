@@ -157,3 +157,14 @@ def test_cache_views(monkeypatch):
     for shape, heads in (((4, 2, 100, 96), 3), ((4, 2, 128, 96), 5), ((4, 128, 96), 3)):
         with pytest.raises(binding.TabedError):
             binding.CachePaged.of_body(torch.zeros(shape), torch.zeros(shape), heads)
+
+
+def test_verify_workspace_of_a_larger_call_serves_smaller_ones():
+    def need(B, V, N=22, n=4, gamma=5):
+        return binding.tabed_verify_nodes_workspace_bytes(binding.make_cfg(V=V, d=64, n=n, B=B, gamma=gamma, h=8, w_dtype=1), N)
+    for V in (300, 32000, 65536, 65537, 262144):
+        sizes = [need(B, V) for B in range(1, 300)]
+        assert sizes == sorted(sizes)
+    for B in (1, 4, 5, 8, 16):
+        sizes = [need(B, V) for V in range(1, 262145, 511)]
+        assert sizes == sorted(sizes)

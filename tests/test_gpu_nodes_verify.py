@@ -92,6 +92,12 @@ def test_vocabularies(binding, V):
     check(binding, make(5, 9, 2, V, seed=V))
 
 
+@pytest.mark.parametrize("B,V", [(1, 65536), (1, 65537), (4, 65533), (5, 65536), (85, 2999), (86, 2999), (3, 32001)])
+@pytest.mark.parametrize("tvd", [False, True])
+def test_sizes_of_pieces(binding, B, V, tvd):
+    check(binding, make(B, 5, 3 if B < 50 else 1, V, seed=B), tvd=tvd)
+
+
 @pytest.mark.parametrize("n", [1, 2, 3, 4, 5, 8, 15, 16])
 def test_drafts(binding, n):
     check(binding, make(4, 7, n, 3000, seed=n))
