@@ -529,7 +529,8 @@ int tabed_cache_append_nodes(const tabed_cache_paged* cache, int32_t layer, int3
  * are rounded to bf16 before the product with the values.  What a node does not see has no influence, whatever it holds.  A node that
  * sees nothing (its blocks are not there) gets zeros and an lse of -inf.  Entries of nodes from n_nodes[r] on are left as they were.
  * q_heads is a multiple of kv_heads, at most 16384.
- * `ws`: tabed_attention_nodes_workspace_bytes bytes, prepared once by ..._init; it then serves calls of any sizes and caches that need no more bytes.
+ * `ws`: tabed_attention_nodes_workspace_bytes bytes, prepared once by ..._init; it then serves calls of any sizes and caches that need no more bytes, calls with
+ * fewer rows or nodes among them.
  * Calls that share a workspace must not overlap.
  */
 size_t tabed_attention_nodes_workspace_bytes(const tabed_cache_paged* cache, int32_t rows, int32_t N, int32_t q_heads);   /* 0: invalid */
@@ -563,8 +564,8 @@ int tabed_attention_nodes(const tabed_cache_paged* cache, int32_t layer, void* w
  *   dev           [B,gamma,n] fp32 out   D(p, q^(j)) at the path's nodes that have children, the first gamma of them; other entries are left as they were
  *   n_valid       [B] int32 out     how many: what tabed_update_weights takes.  dev and n_valid may both be NULL.  cfg->distance 0 or 1 and policies other
  *                 than the grid (2) then; else TABED_EUNSUPPORTED
- * `ws`: tabed_verify_nodes_workspace_bytes bytes, prepared once by ..._init; it then serves calls of any sizes that need no more bytes.  It belongs to the
- * library from the preparation on; calls that share it must not overlap.
+ * `ws`: tabed_verify_nodes_workspace_bytes bytes, prepared once by ..._init; it then serves calls of any sizes that need no more bytes, all that are smaller in
+ * everything among them.  It belongs to the library from the preparation on; calls that share it must not overlap.
  */
 size_t tabed_verify_nodes_workspace_bytes(const tabed_cfg* cfg, int32_t N);   /* 0: invalid */
 int tabed_verify_nodes_workspace_init(const tabed_cfg* cfg, int32_t N, void* ws, void* stream);

@@ -611,7 +611,7 @@ static int validate_attention_nodes(const tabed_cache_paged* cache, int32_t rows
 
 size_t tabed_attention_nodes_workspace_bytes(const tabed_cache_paged* cache, int32_t rows, int32_t N, int32_t q_heads) {
     if (validate_attention_nodes(cache, rows, N, q_heads, false) != TABED_OK) return 0;
-    return nodes_attn_layout(*cache, rows, N, q_heads).total;
+    return nodes_attn_bytes(*cache, rows, N, q_heads);
 }
 
 int tabed_attention_nodes_workspace_init(const tabed_cache_paged* cache, int32_t rows, int32_t N, int32_t q_heads, void* ws, void* stream) {

@@ -5,6 +5,7 @@ namespace tabed {
 
 constexpr size_t kRangesBytes = 8192;                                    // of the rows of a call that is split
 constexpr int kMaxSplitRows = kRangesBytes / 8;
+constexpr int kMinRange = 1024, kLongRow = 8;                            // tokens; of those
 
 template <typename F>
 static auto with_hd(int hd, F&& f) {
@@ -17,34 +18,39 @@ static auto with_hd(int hd, F&& f) {
     }
 }
 
+struct NodesVariant {
+    int queries, unit, tokens, room;                                     // of a workgroup, of a wave, of a tile; workgroups that run at a time
+};
+static NodesVariant variant_of(const tabed_cache_paged& c, int queries) {
+    auto take = [](auto v) {
+        using T = decltype(v);
+        return NodesVariant{T::kQueries, T::kUnit, T::kTokens, 256 * std::max(1, std::min(163840 / (int)(T::kLds + sizeof(NodesShared)), 512 / T::kThreads))};
+    };
+    return with_hd(c.head_dim, [&](auto hd) {
+        return c.type == 2 ? with_nodes_variant<decltype(hd)::value, true>(queries, take) : with_nodes_variant<decltype(hd)::value, false>(queries, take);
+    });
+}
+// Tiles of the longest row there can be.
+static int64_t most_tiles(const tabed_cache_paged& c, int tokens) { return ((int64_t)c.max_blocks * TABED_CACHE_BLOCK + tokens - 1) / tokens; }
+
 struct NodesPlan {
     int tiles, per_tile, slots, split, fill, min_tiles;
 };
 static NodesPlan plan_of(const tabed_cache_paged& c, int rows, int N, int q_heads) {
     const int queries = N * (q_heads / c.kv_heads);
+    const NodesVariant v = variant_of(c, queries);
     NodesPlan p{};
-    int room = 0, tokens = 0, unit = 1;                                  // workgroups that run at a time, tokens of a tile, queries of a wave
-    with_hd(c.head_dim, [&](auto hd) {
-        auto take = [&](auto v) {
-            using T = decltype(v);
-            p.per_tile = T::kQueries;
-            tokens = T::kTokens;
-            unit = T::kUnit;
-            room = 256 * std::max(1, std::min(163840 / (int)(T::kLds + sizeof(NodesShared)), 512 / T::kThreads));
-            return 0;
-        };
-        return c.type == 2 ? with_nodes_variant<decltype(hd)::value, true>(queries, take) : with_nodes_variant<decltype(hd)::value, false>(queries, take);
-    });
+    p.per_tile = v.queries;
     p.tiles = (queries + p.per_tile - 1) / p.per_tile;
-    if (p.tiles > 1) p.per_tile = ((queries + p.tiles - 1) / p.tiles + unit - 1) / unit * unit;      // (as even as whole units of a wave leave them)
+    if (p.tiles > 1) p.per_tile = ((queries + p.tiles - 1) / p.tiles + v.unit - 1) / v.unit * v.unit;      // (as even as whole units of a wave leave them)
     const int64_t units = (int64_t)c.kv_heads * p.tiles;                 // workgroups of a slot
-    const int64_t most = ((int64_t)c.max_blocks * TABED_CACHE_BLOCK + tokens - 1) / tokens;      // tiles of the longest row there can be
-    p.min_tiles = std::max(1, 1024 / tokens);
+    const int64_t most = most_tiles(c, v.tokens);
+    p.min_tiles = std::max(1, kMinRange / v.tokens);
     p.slots = rows;
-    p.fill = (int)std::max<int64_t>(room / units, 2 * rows);
-    // Ranges of 1024 tokens or more (shorter ones cost more in the second launch than they save).  Where rows alone fill the chip they are cut only if one can be so long
-    // that the others would wait for it.
-    if (rows <= kMaxSplitRows && most > (room / units > rows ? 1 : 8) * p.min_tiles) {
+    p.fill = (int)std::max<int64_t>(v.room / units, 2 * rows);
+    // (Shorter ranges cost more in the second launch than they save.)  Where rows alone fill the chip they are cut only if one can be so long that the others
+    // would wait for it.
+    if (rows <= kMaxSplitRows && most > (v.room / units > rows ? 1 : kLongRow) * p.min_tiles) {
         p.split = 1;
         p.slots = (int)std::min<int64_t>(p.fill, rows * ((most + p.min_tiles - 1) / p.min_tiles));
     }
@@ -61,6 +67,23 @@ NodesAttnLayout nodes_attn_layout(const tabed_cache_paged& c, int rows, int N, i
         L.total = L.off_o + up(places * c.head_dim * 4);
     }
     return L;
+}
+// Bytes that calls of up to so many rows and nodes need: the most that any variant of them has of places for ranges' results, not less for more of either.
+size_t nodes_attn_bytes(const tabed_cache_paged& c, int rows, int N, int q_heads) {
+    const int64_t queries = (int64_t)N * (q_heads / c.kv_heads), split_rows = std::min(rows, kMaxSplitRows);
+    int64_t places = 0;
+    for (int64_t some : {(int64_t)16, (int64_t)32, queries}) {
+        some = std::min(some, queries);
+        const NodesVariant v = variant_of(c, (int)some);
+        const int64_t most = most_tiles(c, v.tokens), least = std::max(1, kMinRange / v.tokens);
+        if (most <= least) continue;
+        const int64_t room = (int64_t)v.room * v.queries, row = (some + v.queries - 1) / v.queries * v.queries * c.kv_heads;      // places of as many as run, of a range
+        int64_t twice = 2 * split_rows * row;
+        if (most <= kLongRow * least) twice = std::min(twice, 2 * room);      // (more rows than that are not cut)
+        places = std::max(places, std::min(std::max(room, twice), split_rows * ((most + least - 1) / least) * row));
+    }
+    auto up = [](size_t x) { return (x + 255) / 256 * 256; };
+    return kRangesBytes + up((size_t)places * 16) + up((size_t)places * c.head_dim * 4);
 }
 int64_t nodes_attn_workgroups(const tabed_cache_paged& c, int rows, int N, int q_heads) {
     const NodesPlan p = plan_of(c, rows, N, q_heads);

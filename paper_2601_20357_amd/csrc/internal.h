@@ -187,6 +187,7 @@ struct NodesAttnLayout {
     size_t total;
 };
 NodesAttnLayout nodes_attn_layout(const tabed_cache_paged& c, int rows, int N, int q_heads);
+size_t nodes_attn_bytes(const tabed_cache_paged& c, int rows, int N, int q_heads);
 int64_t nodes_attn_workgroups(const tabed_cache_paged& c, int rows, int N, int q_heads);
 hipError_t launch_nodes_attn_init(char* ws, hipStream_t s);
 hipError_t launch_attention_nodes(const tabed_cache_paged& c, int layer, char* ws, int rows, int N, int q_heads, const uint16_t* q, int64_t q_row,

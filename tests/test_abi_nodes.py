@@ -168,3 +168,18 @@ def test_verify_workspace_of_a_larger_call_serves_smaller_ones():
     for B in (1, 4, 5, 8, 16):
         sizes = [need(B, V) for V in range(1, 262145, 511)]
         assert sizes == sorted(sizes)
+
+
+def test_attention_workspace_of_a_larger_call_serves_smaller_ones(lib):
+    for hd in (32, 64, 96, 128, 256):
+        for kv, group in ((8, 4), (12, 1), (1, 8)):
+            for mb in (10, 100, 130, 2000):
+                def need(rows, N):
+                    c = cache(kv_heads=kv, head_dim=hd, max_blocks=mb, tok_stride=hd, head_stride=64 * hd, block_stride=64 * hd * kv, layer_stride=640 * hd * kv)
+                    return lib.tabed_attention_nodes_workspace_bytes(c, rows, N, kv * group)
+                rows, nodes = (1, 2, 8, 31, 32, 63, 64, 257, 1024, 1025), (1, 2, 4, 5, 8, 9, 16, 17, 32, 33, 64, 65, 128, 129, 255, 256)
+                sizes = [[need(r, n) for n in nodes] for r in rows]
+                assert sizes[0][0] > 0
+                for line in sizes + [list(x) for x in zip(*sizes)]:
+                    line = [x for x in line if x]                        # (0: more than a launch holds)
+                    assert line == sorted(line), (hd, kv, mb)

@@ -353,6 +353,14 @@ def test_attention_one_workspace_for_all_sizes(B):
         check_attention(B, rows, N, qh, kvh, hd, ctx, ws=ws, seed=N, spoil=False)
 
 
+def test_attention_workspace_of_the_largest_call_serves_smaller_ones(B):
+    need = B.tabed_attention_nodes_workspace_bytes(make_cache(B, 70, 3200, 2, 64), 70, 64, 8)
+    ws = torch.full((need + (32 << 20),), 0x5a, dtype=torch.uint8, device=DEV)
+    for rows, N in ((70, 64), (70, 1), (20, 64), (3, 33), (3, 8), (1, 3), (1, 1)):
+        check_attention(B, rows, N, 8, 2, 64, [3000 - 31 * i % 2999 for i in range(rows)], seed=rows + N, ws=ws, spoil=False)
+        assert bool((ws[need:] == 0x5a).all()), (rows, N)
+
+
 def test_attention_past_2_32_bytes(B):
     """Blocks at the far end of a pool of more than 2^32 bytes, in elements too."""
     blocks, kvh, hd = 33_000, 8, 128
