@@ -3,7 +3,7 @@
 //   s_t = scale q k_t,  o = sum_t exp(s_t - m) v_t / sum_t exp(s_t - m)     over the context, the nodes above and the node itself
 //
 // One pass over the keys and values with the running maximum m and sum.  The queries of a row that read one key / value head, N * group of them, go
-// together: an entry of the cache comes from memory once for up to 256 queries.
+// together: an entry of the cache comes from memory once for up to 128 queries.
 //
 // Products are of 16 x 16 x 32, turned so that nothing has to be transposed in registers: S^T = K Q^T has a query in a lane's column and four
 // tokens in its rows, which is, two 16-token halves side by side, how P^T is taken as the column operand of O^T = V^T P^T; the 32 tokens of that product are
@@ -425,11 +425,23 @@ __device__ __forceinline__ int tiles_of(const NodesAttnArgs& a, int row, int tok
     return n > 0 ? (int)((end + tokens - 1) / tokens) : 0;
 }
 
+// A row's length, for its share of the ranges.  UNIT: queries of a wave of four that share e4m3 tiles, 0 elsewhere.  Waves that have no queries of their own take turns
+// with others, so a tile of one or two units of queries takes about half the time of one with three or four (16 rows of 300 to 5000 tokens and 4 to 132 queries, head_dim
+// 128: 77 us against 89 with equal lengths; 8 rows of 4000 to 16000: 89 against 114).  With bf16, whose tiles take a step each and twice the bytes, longer ranges of such rows
+// cost more than they give (78 against 72 us, 102 against 93).
+template <int UNIT>
+__device__ __forceinline__ int length_of(const NodesAttnArgs& a, int row, int tokens) {
+    const int t = tiles_of(a, row, tokens);
+    if constexpr (UNIT == 0) return t;
+    const int q = min(nodes_of(a.n_nodes, row, a.N) * a.group, a.per_tile);
+    return min(a.N * a.group, a.per_tile) <= 2 * UNIT || q > 2 * UNIT ? t : (int)(((int64_t)t * (q > UNIT ? 5 : 4) + 7) / 8);
+}
+
 // Ranges of keys.  Where there are fewer (row, head, tile of queries) than workgroups that run at a time, or rows are long and of unequal lengths, rows are cut
 // into ranges of no more than `per` tiles, the same for all rows and as small as leaves no more than `fill` ranges: all workgroups work that out from the
 // rows' lengths, and each takes the range its slot falls on.  A row of one range is finished by its workgroup; others' results are joined by a
 // second launch.  False: there is no such range.
-template <int THREADS>
+template <int THREADS, int UNIT>
 __device__ __forceinline__ bool find_range(const NodesAttnArgs& a, NodesShared& s, int slot, int tokens, bool tell, NodesRange& g) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     constexpr int W = THREADS / 64;
@@ -437,7 +449,7 @@ __device__ __forceinline__ bool find_range(const NodesAttnArgs& a, NodesShared& 
     if (a.split) {
         double whole = 0.0;
         for (int i = tid; i < a.rows; i += THREADS) {
-            const int t = tiles_of(a, i, tokens);
+            const int t = length_of<UNIT>(a, i, tokens);
             if (i < 64) s.lengths[i] = t;
             whole += t;
         }
@@ -465,7 +477,7 @@ __device__ __forceinline__ bool find_range(const NodesAttnArgs& a, NodesShared& 
         }
         int before = 0;                                                  // ranges of the rows before those of this round
         for (int r0 = 0; r0 < a.rows; r0 += THREADS) {
-            const int i = r0 + tid, n = i < a.rows ? max(1, (tiles_of(a, i, tokens) + per - 1) / per) : 0;
+            const int i = r0 + tid, n = i < a.rows ? max(1, (length_of<UNIT>(a, i, tokens) + per - 1) / per) : 0;
             const int incl = (int)wave_inclusive_scan((double)n);
             __syncthreads();
             if (lane == 63) s.sum[wave] = incl;
@@ -639,7 +651,7 @@ __global__ __launch_bounds__(T::kThreads, 2) void k_attention_nodes(NodesAttnArg
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int kvh = blockIdx.x % a.c.kv_heads, slot = blockIdx.x / a.c.kv_heads;                   // (one tile of queries)
     NodesRange g;
-    if (!find_range<T::kThreads>(a, sh, slot, kNodesTile, kvh == 0, g)) return;
+    if (!find_range<T::kThreads, 0>(a, sh, slot, kNodesTile, kvh == 0, g)) return;
     const int queries = g.nodes * a.group;
     if (queries == 0) return;
 
@@ -772,12 +784,13 @@ __global__ __launch_bounds__(T::kThreads, 2) void k_attention_nodes_wide(NodesAt
     uint64_t(*const s_mask)[kNodeWords] = reinterpret_cast<uint64_t(*)[kNodeWords]>(lds + T::kLds - kMaskBytes);
     __shared__ NodesShared sh;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    // Workgroup w goes to XCD w % 8: the tiles of queries that read the same keys run back to back on one.
-    const int xcd = blockIdx.x & 7, at = blockIdx.x >> 3, tile_q = at % a.tiles, unit = at / a.tiles * 8 + xcd;
+    // Workgroup w goes to XCD w % 8: the tiles of queries that read the same keys run back to back on one.  The last tile, which may have less to do, is another one for each
+    // 32 workgroups, so that no CU has all of them (two tiles of 96 and 36 queries: 90 us against 104).
+    const int xcd = blockIdx.x & 7, at = blockIdx.x >> 3, tile_q = (at % a.tiles + at / a.tiles * a.tiles / 32) % a.tiles, unit = at / a.tiles * 8 + xcd;
     const int kvh = unit % a.c.kv_heads, slot = unit / a.c.kv_heads;
     if (slot >= a.slots) return;                                         // uniform: the grid is padded to whole rounds of XCDs
     NodesRange g;
-    if (!find_range<T::kThreads>(a, sh, slot, T::kTokens, kvh == 0 && tile_q == 0, g)) return;
+    if (!find_range<T::kThreads, F8 ? T::kUnit : 0>(a, sh, slot, T::kTokens, kvh == 0 && tile_q == 0, g)) return;
     const int queries = min(g.nodes * a.group, (tile_q + 1) * a.per_tile), here = queries - tile_q * a.per_tile;
     if (here <= 0) return;
     // As many waves as there are units of queries, 1, 2 or 4, take different ones; the 64-token steps are dealt to the WK waves that have the same.
