@@ -525,8 +525,8 @@ int tabed_cache_append_nodes(const tabed_cache_paged* cache, int32_t layer, int3
  *   q, out  [rows,N,q_heads,head_dim] bf16, strides of a row and of a node each
  *   lse     [rows,N,q_heads] fp32 out, optional: natural logarithm of the sum of exp(scale * score)
  *   scale   > 0, commonly 1 / sqrt(head_dim)
- * Products of bf16 (and e4m3) values are exact, their sums, the softmax and its sum are in fp32; probabilities (with e4m3 values: times the values' scales)
- * are rounded to bf16 before the product with the values.  What a node does not see has no influence, whatever it holds.  A node that
+ * Products of bf16 (and e4m3) values are exact, their sums, the softmax and its sum are in fp32; probabilities are rounded before the product with the
+ * values, to bf16, or with e4m3 values, and then times the values' scales and a power of two, to fp16.  What a node does not see has no influence, whatever it holds.  A node that
  * sees nothing (its blocks are not there) gets zeros and an lse of -inf.  Entries of nodes from n_nodes[r] on are left as they were.
  * q_heads is a multiple of kv_heads, at most 16384.
  * `ws`: tabed_attention_nodes_workspace_bytes bytes, prepared once by ..._init; it then serves calls of any sizes and caches that need no more bytes, calls with

@@ -14,7 +14,10 @@
 // nothing in the loop waits for another wave, and their results meet in LDS at the end.  More (k_attention_nodes_wide): four waves share a tile, one
 // barrier a tile; 1, 2 or 4 of them, as the row's own number of nodes has it, take different queries, and those with the same ones take turns at steps of 64 tokens.
 //
-// The cache's bytes bound it with few queries, the matrix cores and the softmax between the products with many.
+// The cache's bytes bound it with few queries: 1 row of 120011 tokens, 32 / 8 heads of 128, one node 93 us (5.3 TB/s), 16 nodes 110; 64 rows of 256 to 768, 12 heads of
+// 64, 16 nodes 25 (4.2 TB/s).  With many the matrix cores and the softmax between the products do: 8 rows of 10000 tokens, 256 nodes, 32 / 8 heads of 128 430 us
+// (790 TFLOP/s; matrix cores 46 % of the cycles, vector instructions nearly all others, which two waves a SIMD overlap little), in e4m3 517 (every wave widens the
+// tile's values for its own queries: 340 more vector instructions a step of 64 tokens).
 #pragma once
 #include <algorithm>
 #include <mutex>
@@ -629,6 +632,8 @@ __device__ __forceinline__ float4 join_parts(const float* s_o, const float4* s_m
 }
 
 // ---------------------------------------------------------------- up to 32 queries: every wave has tiles of its own
+// QW groups of 16 queries a wave: one for up to 16, two for up to 32, so that no wave multiplies zeros for half of its time; four waves, two where their stages would be more
+// LDS than there is.  Two tiles on their way cover a trip to memory: 5.3 TB/s with one query a head.
 template <int HD_, bool F8_, int QW_, int WK_>
 struct NodesNarrow {
     static constexpr int HD = HD_, QW = QW_, WK = WK_, kThreads = WK * 64, kQueries = QW * 16, kUnit = kQueries, kTokens = kNodesTile;
@@ -762,6 +767,9 @@ __global__ __launch_bounds__(T::kThreads, 2) void k_attention_nodes(NodesAttnArg
 }
 
 // ---------------------------------------------------------------- more: four waves share tiles
+// 32 queries a wave (256 dims: 16, for the registers), so that a fragment of keys or values read from LDS serves two products: with 48 a wave, and one wave a SIMD, 771 us where
+// this takes 477 (8 rows of 4000 to 16000 tokens, 256 nodes, 32 / 8 heads of 128).  Steps of 64 tokens: one test of the maximum, and one pass of the softmax, for
+// twice the products (515 us with 32).  Tiles of 16 KB of keys, two of them: two workgroups a CU.
 template <int HD_, bool F8_>
 struct NodesWide {
     static constexpr int HD = HD_, QW = HD == 256 ? 1 : 2, RT = 4, kWaves = 4, kThreads = kWaves * 64, kUnit = QW * 16, kQueries = kWaves * kUnit;

@@ -49,7 +49,8 @@ static NodesPlan plan_of(const tabed_cache_paged& c, int rows, int N, int q_head
     p.slots = rows;
     p.fill = (int)std::max<int64_t>(v.room / units, 2 * rows);
     // (Shorter ranges cost more in the second launch than they save.)  Where rows alone fill the chip they are cut only if one can be so long that the others
-    // would wait for it.
+    // would wait for it.  No more ranges than run at a time, also where a row's last tile of queries has little to do: the others' workgroups would wait for a second
+    // round (two tiles of 96 and 36 queries, 16 rows of 300 to 5000 tokens: 93 us with as many as the queries would fill, 77 so).
     if (rows <= kMaxSplitRows && most > (v.room / units > rows ? 1 : kLongRow) * p.min_tiles) {
         p.split = 1;
         p.slots = (int)std::min<int64_t>(p.fill, rows * ((most + p.min_tiles - 1) / p.min_tiles));

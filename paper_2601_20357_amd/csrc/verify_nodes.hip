@@ -20,7 +20,8 @@
 //
 // What bounds it: the steps, one after the other.  One is 4 to 5 us: 1 for the row's maximum and exponentials, 1.5 until all pieces' are known, 1 for their
 // sum, the rest for the distances, the test and the next node's rows; a launch with one node and nothing to test takes 8 to 12.  16 sequences of 22 nodes, V = 32000, 4
-// drafts: 40 us (the longest path of 16 visits five nodes); 1 of 6, a path of four: 23 us.  64 sequences, V = 128256, 8 drafts: 190 us for some 360 MB.
+// drafts: 40 us (the longest path of 16 visits five nodes); 1 of 6, a path of four: 23 us.  64 sequences, V = 128256, 8 drafts, half of them greedy: 196 us for 480 MB
+// and some 10^8 exponentials in 64 bits; 12 sequences run at a time.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
