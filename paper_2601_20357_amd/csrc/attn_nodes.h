@@ -33,7 +33,7 @@ namespace tabed {
 struct NodesAttnArgs {
     PagedView c;
     int rows, N, q_heads, group, tiles, per_tile;                        // tiles of queries of a row and key / value head, queries of a tile
-    int slots, split, fill, min_tiles;                                   // ranges of keys, see find_range
+    int slots, split, fill, min_tiles, whole_tiles;                      // ranges of keys, see find_range
     const uint16_t* q;
     uint16_t* out;
     float* lse;
@@ -442,13 +442,14 @@ __device__ __forceinline__ int length_of(const NodesAttnArgs& a, int row, int to
 
 // Ranges of keys.  Where there are fewer (row, head, tile of queries) than workgroups that run at a time, or rows are long and of unequal lengths, rows are cut
 // into ranges of no more than `per` tiles, the same for all rows and as small as leaves no more than `fill` ranges: all workgroups work that out from the
-// rows' lengths, and each takes the range its slot falls on.  A row of one range is finished by its workgroup; others' results are joined by a
+// rows' lengths, and each takes the range its slot falls on.  A short row is not cut.  A row of one range is finished by its workgroup; others' results are joined by a
 // second launch.  False: there is no such range.
 template <int THREADS, int UNIT>
 __device__ __forceinline__ bool find_range(const NodesAttnArgs& a, NodesShared& s, int slot, int tokens, bool tell, NodesRange& g) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     constexpr int W = THREADS / 64;
     int row = slot, range = 0, ranges = 1;
+    auto ranges_of = [&](int length, int each) { return length <= a.whole_tiles ? 1 : (length + each - 1) / each; };
     if (a.split) {
         double whole = 0.0;
         for (int i = tid; i < a.rows; i += THREADS) {
@@ -469,7 +470,7 @@ __device__ __forceinline__ bool find_range(const NodesAttnArgs& a, NodesShared& 
         if (a.rows <= 64 && a.fill > a.rows) {                           // a candidate a thread, between the two
             const int mine = least + (int)((int64_t)(per - least) * tid / THREADS);
             int count = 0;
-            for (int i = 0; i < a.rows; ++i) count += max(1, (s.lengths[i] + mine - 1) / mine);
+            for (int i = 0; i < a.rows; ++i) count += ranges_of(s.lengths[i], mine);
             const uint64_t good = __ballot(count <= a.fill);
             const int best = good ? __builtin_amdgcn_readlane(mine, __ffsll((long long)good) - 1) : 0x7fffffff;
             if (lane == 0) s.sum[wave] = best;
@@ -480,7 +481,7 @@ __device__ __forceinline__ bool find_range(const NodesAttnArgs& a, NodesShared& 
         }
         int before = 0;                                                  // ranges of the rows before those of this round
         for (int r0 = 0; r0 < a.rows; r0 += THREADS) {
-            const int i = r0 + tid, n = i < a.rows ? max(1, (length_of<UNIT>(a, i, tokens) + per - 1) / per) : 0;
+            const int i = r0 + tid, n = i < a.rows ? ranges_of(length_of<UNIT>(a, i, tokens), per) : 0;
             const int incl = (int)wave_inclusive_scan((double)n);
             __syncthreads();
             if (lane == 63) s.sum[wave] = incl;
@@ -632,8 +633,9 @@ __device__ __forceinline__ float4 join_parts(const float* s_o, const float4* s_m
 }
 
 // ---------------------------------------------------------------- up to 32 queries: every wave has tiles of its own
-// QW groups of 16 queries a wave: one for up to 16, two for up to 32, so that no wave multiplies zeros for half of its time; four waves, two where their stages would be more
-// LDS than there is.  Two tiles on their way cover a trip to memory: 5.3 TB/s with one query a head.
+// QW groups of 16 queries a wave: one for up to 16 (6 queries, one row of 600 tokens, heads of 64: 7.8 us, with two groups 9.0; 64 rows of 256 to 768, 16 queries: 25.1 and
+// 27.6), two for up to 32 (16 rows of 300 to 5000, 8 heads of 128, e4m3: 35 us, with waves that share tiles 47; 64 rows of 2000, 12 heads of 64: 77 and 91).  Four waves
+// (with two 42, 81 and 97 us for 35, 77 and 92, one row of 120011 tokens), two where four would need more LDS than there is.
 template <int HD_, bool F8_, int QW_, int WK_>
 struct NodesNarrow {
     static constexpr int HD = HD_, QW = QW_, WK = WK_, kThreads = WK * 64, kQueries = QW * 16, kUnit = kQueries, kTokens = kNodesTile;

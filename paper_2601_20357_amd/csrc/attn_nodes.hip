@@ -5,7 +5,7 @@ namespace tabed {
 
 constexpr size_t kRangesBytes = 8192;                                    // of the rows of a call that is split
 constexpr int kMaxSplitRows = kRangesBytes / 8;
-constexpr int kMinRange = 1024, kLongRow = 8;                            // tokens; of those
+constexpr int kMinRange = 512, kWholeRow = 1024, kLongRow = 8192;        // tokens
 
 template <typename F>
 static auto with_hd(int hd, F&& f) {
@@ -34,7 +34,7 @@ static NodesVariant variant_of(const tabed_cache_paged& c, int queries) {
 static int64_t most_tiles(const tabed_cache_paged& c, int tokens) { return ((int64_t)c.max_blocks * TABED_CACHE_BLOCK + tokens - 1) / tokens; }
 
 struct NodesPlan {
-    int tiles, per_tile, slots, split, fill, min_tiles;
+    int tiles, per_tile, slots, split, fill, min_tiles, whole_tiles;
 };
 static NodesPlan plan_of(const tabed_cache_paged& c, int rows, int N, int q_heads) {
     const int queries = N * (q_heads / c.kv_heads);
@@ -46,12 +46,14 @@ static NodesPlan plan_of(const tabed_cache_paged& c, int rows, int N, int q_head
     const int64_t units = (int64_t)c.kv_heads * p.tiles;                 // workgroups of a slot
     const int64_t most = most_tiles(c, v.tokens);
     p.min_tiles = std::max(1, kMinRange / v.tokens);
+    p.whole_tiles = std::max(1, kWholeRow / v.tokens);
     p.slots = rows;
     p.fill = (int)std::max<int64_t>(v.room / units, 2 * rows);
-    // (Shorter ranges cost more in the second launch than they save.)  Where rows alone fill the chip they are cut only if one can be so long that the others
-    // would wait for it.  No more ranges than run at a time, also where a row's last tile of queries has little to do: the others' workgroups would wait for a second
-    // round (two tiles of 96 and 36 queries, 16 rows of 300 to 5000 tokens: 93 us with as many as the queries would fill, 77 so).
-    if (rows <= kMaxSplitRows && most > (v.room / units > rows ? 1 : kLongRow) * p.min_tiles) {
+    // Ranges of 512 tokens or more (4 rows of 4000 tokens, 16 nodes, 32 / 8 heads of 128: 34 us; of 1024 or more 44, of 256 or more 36), of rows of more than 1024 (one row of
+    // 600, 6 nodes, 12 heads of 64: whole 7.6 us, in two 12).  Where rows alone fill the chip they are cut only if one can be so long that the others would wait for it: of
+    // more than 8192 (64 rows of 2000, 12 nodes, 12 heads of 64: whole 72 us, cut 92).  No more ranges than run at a time, also where a row's last tile of queries has little
+    // to do: the others' workgroups would wait for a second round (tiles of 96 and 36 queries, 16 rows of 300 to 5000: 93 us with as many as the queries would fill, 77 so).
+    if (rows <= kMaxSplitRows && most > std::max(1, (v.room / units > rows ? kWholeRow : kLongRow) / v.tokens)) {
         p.split = 1;
         p.slots = (int)std::min<int64_t>(p.fill, rows * ((most + p.min_tiles - 1) / p.min_tiles));
     }
@@ -77,10 +79,10 @@ size_t nodes_attn_bytes(const tabed_cache_paged& c, int rows, int N, int q_heads
         some = std::min(some, queries);
         const NodesVariant v = variant_of(c, (int)some);
         const int64_t most = most_tiles(c, v.tokens), least = std::max(1, kMinRange / v.tokens);
-        if (most <= least) continue;
+        if (most <= std::max(1, kWholeRow / v.tokens)) continue;
         const int64_t room = (int64_t)v.room * v.queries, row = (some + v.queries - 1) / v.queries * v.queries * c.kv_heads;      // places of as many as run, of a range
         int64_t twice = 2 * split_rows * row;
-        if (most <= kLongRow * least) twice = std::min(twice, 2 * room);      // (more rows than that are not cut)
+        if (most <= std::max(1, kLongRow / v.tokens)) twice = std::min(twice, 2 * room);      // (more rows than that are not cut)
         places = std::max(places, std::min(std::max(room, twice), split_rows * ((most + least - 1) / least) * row));
     }
     auto up = [](size_t x) { return (x + 255) / 256 * 256; };
@@ -98,7 +100,7 @@ hipError_t launch_attention_nodes(const tabed_cache_paged& c, int layer, char* w
     ProfScope prof(TABED_K_BODY, s);
     const NodesPlan p = plan_of(c, rows, N, q_heads);
     const NodesAttnLayout L = nodes_attn_layout(c, rows, N, q_heads);
-    const NodesAttnArgs a{paged_view(c, layer), rows, N, q_heads, q_heads / c.kv_heads, p.tiles, p.per_tile, p.slots, p.split, p.fill, p.min_tiles, q, out, lse,
+    const NodesAttnArgs a{paged_view(c, layer), rows, N, q_heads, q_heads / c.kv_heads, p.tiles, p.per_tile, p.slots, p.split, p.fill, p.min_tiles, p.whole_tiles, q, out, lse,
                           q_row, q_tok, out_row, out_tok, ctx_len, parents, n_nodes, scale * 1.44269504088896340736f, reinterpret_cast<int2*>(ws),
                           reinterpret_cast<float4*>(ws + L.off_ml), reinterpret_cast<float*>(ws + L.off_o)};
     return with_hd(c.head_dim, [&](auto hd) { return launch_nodes_hd<decltype(hd)::value>(c.type == 2, &prof, a, s); });
