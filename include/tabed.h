@@ -579,7 +579,7 @@ int tabed_verify_nodes(const tabed_cfg* cfg, void* ws, uint64_t round, int32_t N
  * ctx_base[r] + i, and ctx_len[r] = ctx_base[r] + the number of nodes kept.
  *   path    [rows,N] int32 in   ascending nodes (path[r][0] = 0 as a rule); the path ends where an entry is not above the one before it, or not below N
  *   n_path  [rows] int32 in     entries of the path, clamped to 0 .. N
- *   ctx_len [rows] int32 out    must not be ctx_base
+ *   ctx_len [rows] int32 out    overlaps none of the others
  * Entries whose source or destination is past the table or in no block are not moved (the positions count all the same).
  */
 int tabed_cache_keep_nodes(const tabed_cache_paged* cache, int32_t rows, int32_t N, const int32_t* ctx_base, const int32_t* path, const int32_t* n_path,

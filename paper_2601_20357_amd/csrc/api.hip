@@ -688,8 +688,12 @@ int tabed_cache_keep_nodes(const tabed_cache_paged* cache, int32_t rows, int32_t
     if (rc == TABED_OK) rc = validate_nodes(rows, N);
     if (rc != TABED_OK) return rc;
     if (!ctx_base || !path || !n_path || !ctx_len) return TABED_ENULL;
-    if (ctx_len == ctx_base) return TABED_EINVAL;
     if (element_misaligned(ctx_base, 0) || element_misaligned(path, 0) || element_misaligned(n_path, 0) || element_misaligned(ctx_len, 0)) return TABED_EALIGN;
+    auto overlaps = [&](const int32_t* in, int64_t n) {                  // (ctx_len is written while others still read)
+        const uintptr_t a = reinterpret_cast<uintptr_t>(ctx_len), b = reinterpret_cast<uintptr_t>(in);
+        return a < b + n * sizeof(int32_t) && b < a + rows * sizeof(int32_t);
+    };
+    if (overlaps(ctx_base, rows) || overlaps(path, (int64_t)rows * N) || overlaps(n_path, rows)) return TABED_EINVAL;
     const hipError_t e = launch_keep_nodes(*cache, rows, N, ctx_base, path, n_path, ctx_len, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? TABED_OK : fail_hip(e);
 }

@@ -183,3 +183,11 @@ def test_attention_workspace_of_a_larger_call_serves_smaller_ones(lib):
                 for line in sizes + [list(x) for x in zip(*sizes)]:
                     line = [x for x in line if x]                        # (0: more than a launch holds)
                     assert line == sorted(line), (hd, kv, mb)
+
+
+@pytest.mark.parametrize("name,at", [("base", 0x1000), ("base", 0x2008), ("base", 0x1ff8), ("path", 0x2008), ("path", 0x1fa4), ("count", 0x2000), ("count", 0x1ff8)])
+def test_keep_refuses_lengths_that_overlap_what_is_read(lib, name, at):
+    changed = {name: C.c_void_p(at)}
+    if at == 0x1000:
+        changed["ctx"] = C.c_void_p(0x1000)
+    assert call(lib.tabed_cache_keep_nodes, KEEP, KEEP_OK, **changed) == EINVAL
