@@ -522,7 +522,7 @@ int tabed_cache_append_nodes(const tabed_cache_paged* cache, int32_t layer, int3
 /*
  * tabed_attention_nodes: attention of a tree's nodes over the cache, in which they are already (tabed_cache_append_nodes with the same ctx_len, parents
  * and n_nodes).  Query head i reads key / value head i / (q_heads / kv_heads).
- *   q, out  [rows,N,q_heads,head_dim] bf16, strides of a row and of a node each
+ *   q, out  [rows,N,q_heads,head_dim] bf16, strides of a row and of a node each; out may be q itself (the same strides) and overlaps it in no other way
  *   lse     [rows,N,q_heads] fp32 out, optional: natural logarithm of the sum of exp(scale * score)
  *   scale   > 0, commonly 1 / sqrt(head_dim)
  * Products of bf16 (and e4m3) values are exact, their sums, the softmax and its sum are in fp32; probabilities are rounded before the product with the

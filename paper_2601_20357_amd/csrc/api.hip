@@ -633,6 +633,7 @@ int tabed_attention_nodes(const tabed_cache_paged* cache, int32_t layer, void* w
     const int64_t heads = (int64_t)q_heads * cache->head_dim;
     if (!(scale > 0.f) || !(scale < INFINITY)) return TABED_EINVAL;
     if (q_row_stride < heads || q_tok_stride < heads || out_row_stride < heads || out_tok_stride < heads) return TABED_EINVAL;
+    if (q == out && (q_row_stride != out_row_stride || q_tok_stride != out_tok_stride)) return TABED_EINVAL;
     if (misaligned(ws) || element_misaligned(q, 1) || element_misaligned(out, 1) || element_misaligned(ctx_len, 0) || element_misaligned(parents, 0) ||
         element_misaligned(n_nodes, 0) || element_misaligned(lse, 0))
         return TABED_EALIGN;

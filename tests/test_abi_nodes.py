@@ -191,3 +191,8 @@ def test_keep_refuses_lengths_that_overlap_what_is_read(lib, name, at):
     if at == 0x1000:
         changed["ctx"] = C.c_void_p(0x1000)
     assert call(lib.tabed_cache_keep_nodes, KEEP, KEEP_OK, **changed) == EINVAL
+
+
+def test_attention_refuses_results_in_place_of_queries_with_other_strides(lib):
+    for changed in (dict(orow=4096), dict(otok=512)):
+        assert call(lib.tabed_attention_nodes, ATTN, ATTN_OK, **changed) == EINVAL

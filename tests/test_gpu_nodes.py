@@ -353,6 +353,18 @@ def test_attention_one_workspace_for_all_sizes(B):
         check_attention(B, rows, N, qh, kvh, hd, ctx, ws=ws, seed=N, spoil=False)
 
 
+@pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("rows,N,ctx", [(2, 5, 300), (1, 24, 5000), (3, 70, 2500), (2, 256, 40)])
+def test_attention_in_place_of_its_queries(B, rows, N, ctx, f8):
+    cache = make_cache(B, rows, ctx + N, 2, 64, f8)
+    q = torch.randn(rows, N, 8, 64, generator=gen(N)).to(torch.bfloat16).to(DEV)
+    out, lens = torch.zeros_like(q), torch.full((rows,), ctx, dtype=torch.int32, device=DEV)
+    ws, parents = B.new_attention_nodes_workspace(cache, rows, N, 8), trees(rows, N, "random").to(DEV)
+    B.tabed_attention_nodes(cache, ws, q, lens, out, parents=parents)
+    B.tabed_attention_nodes(cache, ws, q, lens, q, parents=parents)
+    assert torch.equal(q, out)
+
+
 def test_attention_workspace_of_the_largest_call_serves_smaller_ones(B):
     need = B.tabed_attention_nodes_workspace_bytes(make_cache(B, 70, 3200, 2, 64), 70, 64, 8)
     ws = torch.full((need + (32 << 20),), 0x5a, dtype=torch.uint8, device=DEV)
