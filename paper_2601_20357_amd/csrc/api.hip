@@ -7,6 +7,7 @@
 #include <vector>
 
 #include "internal.h"
+#include "nodes_launch.h"
 
 namespace tabed {
 

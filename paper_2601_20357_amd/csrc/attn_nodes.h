@@ -23,9 +23,10 @@
 #include <mutex>
 #include <type_traits>
 
-#include "internal.h"
+#include "launch_utils.h"
 #include "lmhead_store.h"
 #include "nodes.h"
+#include "nodes_launch.h"
 #include "q8_utils.h"
 
 namespace tabed {

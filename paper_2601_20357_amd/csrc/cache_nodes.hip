@@ -3,8 +3,8 @@
 
 #include <cmath>
 
-#include "internal.h"
 #include "nodes.h"
+#include "nodes_launch.h"
 #include "q8_utils.h"
 
 namespace tabed {

@@ -8,6 +8,7 @@
 #include <type_traits>
 
 #include "body_utils.h"
+#include "launch_utils.h"
 #include "lmhead_store.h"
 #include "q8_utils.h"
 

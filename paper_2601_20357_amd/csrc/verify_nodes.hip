@@ -27,8 +27,8 @@
 #include <algorithm>
 #include <cmath>
 
-#include "internal.h"
 #include "nodes.h"
+#include "nodes_launch.h"
 
 namespace tabed {
 
