@@ -634,7 +634,7 @@ __device__ __forceinline__ float4 join_parts(const float* s_o, const float4* s_m
 }
 
 // ---------------------------------------------------------------- up to 32 queries: every wave has tiles of its own
-// QW groups of 16 queries a wave: one for up to 16 (6 queries, one row of 600 tokens, heads of 64: 7.8 us, with two groups 9.0; 64 rows of 256 to 768, 16 queries: 25.1 and
+// QW groups of 16 queries a wave: one for up to 16 (6 queries, one row of 600 tokens, heads of 64: 7.8 us, with two groups 9.0, by four waves; 64 rows of 256 to 768, 16 queries: 25.1 and
 // 27.6), two for up to 32 (16 rows of 300 to 5000, 8 heads of 128, e4m3: 35 us, with waves that share tiles 47; 64 rows of 2000, 12 heads of 64: 77 and 91).  Four waves
 // (with two 42, 81 and 97 us for 35, 77 and 92, one row of 120011 tokens), two where four would need more LDS than there is.
 template <int HD_, bool F8_, int QW_, int WK_>
@@ -1022,10 +1022,17 @@ __global__ __launch_bounds__(256) void k_attention_nodes_join(NodesAttnArgs a) {
 }
 
 // ---------------------------------------------------------------- host side
-// The variant for a row and head's number of queries, handed to `go`.
+// The variant for a row and head's number of queries, handed to `go`; few: rows and heads leave half of the CUs without a workgroup, and eight waves share what one has (LDS
+// holds their stages where a row of keys has 128 bytes at most): 4 rows of 900 tokens, 6 nodes, 12 heads of 64 8.8 us, with four waves 10.1; 8 rows of 1000, 4 nodes, 32 / 8
+// heads of 128, e4m3 11.7 and 14.2; with more of them they only hold each other up (16 rows of 900 12.5 and 12.3, 16 of 300 to 5000 in e4m3 29.9 and 28.6).
+inline bool few_units(int64_t rows, int kv_heads) { return rows * kv_heads < 128; }
 template <int HD, bool F8, typename F>
-inline auto with_nodes_variant(int queries, F&& go) {
-    constexpr int WK = HD * (F8 ? 1 : 2) >= 512 ? 2 : 4;                 // (LDS)
+inline auto with_nodes_variant(int queries, bool few, F&& go) {
+    constexpr int kRow = HD * (F8 ? 1 : 2), WK = kRow >= 512 ? 2 : 4;    // (LDS)
+    if constexpr (kRow <= 128) {
+        if (few && queries <= 16) return go(NodesNarrow<HD, F8, 1, 8>{});
+        if (few && queries <= 32) return go(NodesNarrow<HD, F8, 2, 8>{});
+    }
     if (queries <= 16) return go(NodesNarrow<HD, F8, 1, WK>{});
     if constexpr (HD < 256)
         if (queries <= 32) return go(NodesNarrow<HD, F8, 2, WK>{});
@@ -1062,7 +1069,8 @@ hipError_t launch_nodes_variant(const ProfScope* prof, const NodesAttnArgs& a, h
     template <>                                                                                                               \
     hipError_t launch_nodes_hd<HD_>(bool f8, const ProfScope* prof, const NodesAttnArgs& a, hipStream_t s) {                  \
         auto go = [&](auto v) { return launch_nodes_variant<decltype(v)>(prof, a, s); };                                      \
-        return f8 ? with_nodes_variant<HD_, true>(a.N * a.group, go) : with_nodes_variant<HD_, false>(a.N * a.group, go);     \
+        const bool few = few_units(a.rows, a.c.kv_heads);                                                                     \
+        return f8 ? with_nodes_variant<HD_, true>(a.N * a.group, few, go) : with_nodes_variant<HD_, false>(a.N * a.group, few, go); \
     }
 template <int HD>
 hipError_t launch_nodes_hd(bool f8, const ProfScope* prof, const NodesAttnArgs& a, hipStream_t s);

@@ -21,13 +21,13 @@ static auto with_hd(int hd, F&& f) {
 struct NodesVariant {
     int queries, unit, tokens, room;                                     // of a workgroup, of a wave, of a tile; workgroups that run at a time
 };
-static NodesVariant variant_of(const tabed_cache_paged& c, int queries) {
+static NodesVariant variant_of(const tabed_cache_paged& c, int queries, bool few) {
     auto take = [](auto v) {
         using T = decltype(v);
         return NodesVariant{T::kQueries, T::kUnit, T::kTokens, 256 * std::max(1, std::min(163840 / (int)(T::kLds + sizeof(NodesShared)), 512 / T::kThreads))};
     };
     return with_hd(c.head_dim, [&](auto hd) {
-        return c.type == 2 ? with_nodes_variant<decltype(hd)::value, true>(queries, take) : with_nodes_variant<decltype(hd)::value, false>(queries, take);
+        return c.type == 2 ? with_nodes_variant<decltype(hd)::value, true>(queries, few, take) : with_nodes_variant<decltype(hd)::value, false>(queries, few, take);
     });
 }
 // Tiles of the longest row there can be.
@@ -38,7 +38,7 @@ struct NodesPlan {
 };
 static NodesPlan plan_of(const tabed_cache_paged& c, int rows, int N, int q_heads) {
     const int queries = N * (q_heads / c.kv_heads);
-    const NodesVariant v = variant_of(c, queries);
+    const NodesVariant v = variant_of(c, queries, few_units(rows, c.kv_heads));
     NodesPlan p{};
     p.per_tile = v.queries;
     p.tiles = (queries + p.per_tile - 1) / p.per_tile;
@@ -77,7 +77,7 @@ size_t nodes_attn_bytes(const tabed_cache_paged& c, int rows, int N, int q_heads
     int64_t places = 0;
     for (int64_t some : {(int64_t)16, (int64_t)32, queries}) {
         some = std::min(some, queries);
-        const NodesVariant v = variant_of(c, (int)some);
+        const NodesVariant v = variant_of(c, (int)some, false);          // (few units: no more places)
         const int64_t most = most_tiles(c, v.tokens), least = std::max(1, kMinRange / v.tokens);
         if (most <= std::max(1, kWholeRow / v.tokens)) continue;
         const int64_t room = (int64_t)v.room * v.queries, row = (some + v.queries - 1) / v.queries * v.queries * c.kv_heads;      // places of as many as run, of a range

@@ -291,6 +291,12 @@ def test_attention_long(B, N, qh, kvh, hd, ctx):
 
 
 @pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("rows,N,qh,kvh,hd", [(1, 6, 12, 12, 64), (10, 9, 12, 12, 64), (11, 9, 12, 12, 64), (3, 20, 4, 4, 32), (2, 31, 4, 4, 64), (15, 4, 32, 8, 128), (16, 4, 32, 8, 128)])
+def test_attention_few_and_many_rows(B, rows, N, qh, kvh, hd, f8):
+    check_attention(B, rows, N, qh, kvh, hd, [(1500, 0, 31, 257, 1, 700, 1024, 255, 512)[i % 9] for i in range(rows)], f8, seed=rows)
+
+
+@pytest.mark.parametrize("f8", [False, True])
 def test_attention_holes(B, f8):
     check_attention(B, 4, 9, 4, 2, 64, [300, 200, 64, 0], f8, holes=[(0, 0), (0, 3), (1, 3), (2, 0), (2, 1), (3, 0)], seed=1)
     check_attention(B, 1, 5, 2, 2, 128, [3000], f8, holes=[(0, e) for e in range(0, 47, 2)], seed=2)
