@@ -148,6 +148,11 @@ __device__ __forceinline__ uint64_t window(const uint64_t* mask, int64_t j0) {
     return m;
 }
 
+// What a step of 32 or 64 tokens is: kWhole, all queries see all of them; kMasked, who sees them is in a mask; kFar (e4m3), kWhole with products that fp16 does not hold.
+enum NodesStep { kWhole, kFar, kMasked };
+template <NodesStep MODE>
+using NodesMode = std::integral_constant<NodesStep, MODE>;
+
 // ---------------------------------------------------------------- a wave's queries, 16 * QW of them, and what they have seen
 template <int HD, bool F8, int QW>
 struct NodesWave {
@@ -156,8 +161,7 @@ struct NodesWave {
     int node[QW];
     f32x4b acc[QW][DT];
     f32x4b rounded[QW];                                                  // bf16: sums of the probabilities as they are rounded
-    float m[QW], l[QW];
-    float lift;                                                          // e4m3: the power of two that values' scales are taken times; 0 before the first
+    float m[QW], l[QW];                                                  // what probabilities are relative to (log2), and their sums
     bool odd;                                                            // some value was not finite, and left out
 
     __device__ __forceinline__ void begin(const NodesAttnArgs& a, int r, int kvh, int q0, int queries) {
@@ -183,14 +187,16 @@ struct NodesWave {
 #pragma unroll
             for (int d = 0; d < DT; ++d) acc[b][d] = f32x4b{0.f, 0.f, 0.f, 0.f};
         }
-        lift = 0.f;
         odd = false;
     }
 
-    // 32 or 64 tokens (RT: halves of 16): their rows of keys and values, and scales.  seen: a bit a token for each query.
-    template <bool MASKED, int RT, typename Seen>
-    __device__ __forceinline__ void step(const unsigned char* sk, const unsigned char* sv, const float* kscale, const float* vscale, float scale2,
+    // RT halves of 16 tokens: their rows of keys and values, and scales.  seen: a bit a token for each query, of kMasked steps.
+    // False, with nothing taken, where a step is not kWhole but kFar.
+    template <NodesStep MODE, int RT, typename Seen>
+    __device__ __forceinline__ bool step(const unsigned char* sk, const unsigned char* sv, const float* kscale, const float* vscale, float scale2,
                                          const Seen (&seen)[QW]) {
+        constexpr bool MASKED = MODE == kMasked, F16 = F8 && MODE != kFar;
+        static_assert(F8 || MODE != kFar);
         static_assert(!MASKED || sizeof(Seen) * 8 >= RT * 16);
         const int col = threadIdx.x & 15, grp = threadIdx.x >> 4 & 3;
         f32x4b s[QW][RT];
@@ -217,10 +223,23 @@ struct NodesWave {
             }
         }
         __builtin_amdgcn_s_setprio(0);
-        f32x4b vs[RT], ks2[RT];
+        f32x4b vs[RT], ks2[RT], size[RT];
         auto sees = [&](int b, int i, int e) { return (seen[b] >> (i * 16 + grp * 4 + e) & 1) != 0; };
+        // e4m3: what is multiplied with the values is probability times scale, and scales can be anything.  So what probabilities are relative to is a power of two that follows
+        // the largest of these products, for every query by what it sees itself: 2^8 when it is chosen and up to 2^15 before it is chosen anew.  fp16 then holds products to 2^-11 of
+        // themselves down to 2^-14 and to 2^-8 down to 2^-17.  A step with smaller ones, or with a scale outside 2^-38 to 2^38, is kFar: products in bf16, to 2^-8 whatever they are.
+        // From there on a wave's steps are, up to the kMasked ones: in these, what others see must not count, and each product goes by itself, in fp16 or in bf16.
+        // (One power of two a wave, by the largest scale that any of its queries saw, let a sibling's entry, or one that hardly counts, take all precision from the others.)
+        // For that choice scales count as 2^-40 to 2^50, so that the largest probability is in 2^-43 to 2^65, and the sum of them is none of tiny ones.
+        constexpr float kRaise = MODE == kFar ? 25.f : 15.f, kLow = -16.9f;      // (fp16 ends at 2^15.99)
+        bool apart = false;                                              // kMasked: there may be products for bf16; kWhole: the step is kFar
+        float big = 0.f, little = 0.f;                                   // kWhole: log2 of the largest and the smallest scale of this lane's tokens
+        // log2 of a scale, at most 0.09 too low: the exponent, and the mantissa as if it were linear, from the bits as 2^23 + bits / 2^9.
+        auto log2_of = [](float v) {
+            return fmaf(__builtin_bit_cast(float, __builtin_amdgcn_alignbit(0x96u, __builtin_bit_cast(uint32_t, v), 9u)), 0x1p-14f, -639.f);
+        };
         if constexpr (F8) {
-            float most = 0.f;
+            float most = 0.f, least = MODE == kWhole ? INFINITY : 0.f;
 #pragma unroll
             for (int i = 0; i < RT; ++i) {
                 ks2[i] = *reinterpret_cast<const f32x4b*>(kscale + i * 16 + grp * 4);
@@ -228,47 +247,23 @@ struct NodesWave {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     ks2[i][e] *= scale2;
-                    bool any = true;
-                    if constexpr (MASKED) {
-                        any = false;
-#pragma unroll
-                        for (int b = 0; b < QW; ++b) any |= sees(b, i, e);
+                    const float v = vs[i][e];                            // (a bit cast of a vector's element reads element 0)
+                    if constexpr (MODE == kWhole) {
+                        most = fmaxf(most, fabsf(v));
+                        least = fminf(least, fabsf(v));
+                    } else {
+                        const float lg = log2_of(v);
+                        if constexpr (MASKED) most = fmaxf(most, lg), least = fminf(least, v == 0.f ? 0.f : lg);
+                        size[i][e] = __builtin_amdgcn_fmed3f(lg, -40.f, 50.f);
                     }
-                    most = fmaxf(most, any ? vs[i][e] : 0.f);
                 }
             }
-            // Probabilities times the values' scales are rounded to fp16, which holds them to 2^-12 of themselves where they are above 2^-14: scales are taken times a
-            // power of two that brings the largest so far near 1 (within 2^6 before it is chosen anew).  A scale that nobody sees, or that is not finite, does not count.
-            if (__any(!(most < INFINITY))) {
-                most = 0.f;
-#pragma unroll
-                for (int i = 0; i < RT; ++i)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        bool any = !MASKED;
-                        if constexpr (MASKED)
-#pragma unroll
-                            for (int b = 0; b < QW; ++b) any |= sees(b, i, e);
-                        most = fmaxf(most, any && vs[i][e] < INFINITY ? vs[i][e] : 0.f);
-                    }
+            if constexpr (MASKED) apart = most > 50.f || least < -40.f;
+            if constexpr (MODE == kWhole) {
+                big = __builtin_amdgcn_logf(most);
+                little = __builtin_amdgcn_logf(least);
+                apart = big > 38.f || little < -38.f;
             }
-            if constexpr (MASKED) most = wave_max(most);
-            else most = max_lanes16_32(most);
-            if (__any(most * lift > 64.f || (lift == 0.f && most > 0.f))) {
-                const int e = min(max((int)(__builtin_bit_cast(uint32_t, most) >> 23), 4), 250);
-                const float next = __builtin_bit_cast(float, (uint32_t)(254 - e) << 23), change = lift == 0.f ? 0.f : next / lift;
-                lift = next;
-#pragma unroll
-                for (int b = 0; b < QW; ++b)
-#pragma unroll
-                    for (int d = 0; d < DT; ++d)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[b][d][i] *= change;
-            }
-#pragma unroll
-            for (int i = 0; i < RT; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) vs[i][e] *= lift;
         }
         // ---- the softmax, in units of log2.  Scores are taken relative to the maximum so far before the new one is known: it is raised only where it would be by
         // more than 2^6 (probabilities are relative to the one they were taken with, and no less exact), and then they are made again.
@@ -290,6 +285,54 @@ struct NodesWave {
             };
             const float base = m[b] == -INFINITY ? 0.f : m[b];
             relative_to(base);
+            if constexpr (F8) {
+                auto log2_product = [&](int i, int e) {
+                    const float v = vs[i][e];
+                    return p[b][i][e] + (MODE == kWhole ? log2_of(v) : size[i][e]);
+                };
+                float top = -INFINITY, low = MODE == kWhole ? INFINITY : 0.f;
+#pragma unroll
+                for (int i = 0; i < RT; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float y = MODE == kWhole ? p[b][i][e] : log2_product(i, e);
+                        top = fmaxf(top, y);
+                        if constexpr (MODE == kWhole) low = fminf(low, y);
+                        if constexpr (MASKED) low = fminf(low, sees(b, i, e) ? y : 0.f);
+                    }
+                // (kWhole: bounds first, of the largest and the smallest score and scale)
+                if (__any(MODE == kWhole ? top + big > kRaise || low + little < kLow || m[b] == -INFINITY : top > kRaise || (m[b] == -INFINITY && top > -INFINITY))) {
+                    if constexpr (MODE == kWhole) {
+                        top = -INFINITY;
+                        low = INFINITY;
+#pragma unroll
+                        for (int i = 0; i < RT; ++i)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                top = fmaxf(top, log2_product(i, e));
+                                low = fminf(low, log2_product(i, e));
+                            }
+                    }
+                    top = max_lanes16_32(top);
+                    const bool mine = top > kRaise || (m[b] == -INFINITY && top > -INFINITY);
+                    const float next = ceilf(base + top) - 8.f, change = mine ? next - base : 0.f;
+                    const int fade = m[b] == -INFINITY ? 0 : (int)fmaxf(-change, -1000.f);
+                    m[b] = mine ? next : m[b];
+                    l[b] = ldexpf(l[b], fade);
+#pragma unroll
+                    for (int d = 0; d < DT; ++d)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[b][d][e] = ldexpf(acc[b][d][e], fade);
+                    low -= change;
+#pragma unroll
+                    for (int i = 0; i < RT; ++i)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) p[b][i][e] -= change;
+                    if constexpr (MODE == kWhole) apart |= low < kLow;
+                }
+                if constexpr (MASKED) apart |= low < kLow;
+                continue;
+            }
             float top = -INFINITY;
 #pragma unroll
             for (int i = 0; i < RT; ++i)
@@ -308,6 +351,63 @@ struct NodesWave {
                     for (int e = 0; e < 4; ++e) acc[b][d][e] *= fade;
                 relative_to(next == -INFINITY ? 0.f : next);
             }
+        }
+        if constexpr (F8 && MODE == kWhole)
+            if (__any(apart)) return false;
+        // ---- O^T += V^T P^T
+        bool left_out = false;
+        const int k8 = col >> 1, vrow = F8 ? (k8 < 4 ? grp * 4 + k8 : 12 + grp * 4 + k8) : grp * 4 + (col >> 2);      // of 32, or of 16
+        auto values8 = [&](int h, int d) {                               // e4m3: eight tokens' values of a dim
+            auto from = (__attribute__((address_space(3))) i32x2*)(sv + vrow * kRow + (d ^ turn_v<HD, F8>(vrow)) * 16 + (col & 1) * 8 + h * 32 * kRow);
+            i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32(from);
+            if constexpr (MASKED) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const uint32_t x = (uint32_t)w[i], nan = ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;     // bytes 0x7f and 0xff
+                    left_out |= nan != 0;
+                    w[i] = (int)(x & ~((nan >> 7) * 255u));
+                }
+            }
+            return w;
+        };
+        if constexpr (F8 && MASKED) {
+            if (__any(apart)) {                                          // products that fp16 does not hold, in bf16 into the same sums
+#pragma unroll
+                for (int h = 0; h < RT / 2; ++h) {
+                    bf16x8 rest[QW];
+#pragma unroll
+                    for (int b = 0; b < QW; ++b) {
+                        float x[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            const int i = 2 * h + k / 4, e = k % 4;
+                            const float one = __builtin_amdgcn_exp2f(p[b][i][e]);
+                            float w = one * vs[i][e];
+                            w = sees(b, i, e) ? w : 0.f;
+                            const bool held = (int)(fabsf(w) >= 0x1p-17f) & (int)(fabsf(w) <= 65504.f);
+                            x[k] = held ? 0.f : w;
+                            l[b] += held ? 0.f : one;
+                            p[b][i][e] = held ? p[b][i][e] : -INFINITY;
+                        }
+                        const uint2 lo = pack_bf16x4(x[0], x[1], x[2], x[3]), hi = pack_bf16x4(x[4], x[5], x[6], x[7]);
+                        rest[b] = __builtin_bit_cast(bf16x8, u32x4b{lo.x, lo.y, hi.x, hi.y});
+                    }
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) {
+                        const i32x2 w = values8(h, d);
+                        const bf16x8 vf = widen_bf16((uint32_t)w[0], (uint32_t)w[1]);
+#pragma unroll
+                        for (int b = 0; b < QW; ++b) acc[b][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, rest[b], acc[b][d], 0, 0, 0);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < RT; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) vs[i][e] = fabsf(vs[i][e]) < INFINITY ? vs[i][e] : 0.f;
+            }
+        }
+#pragma unroll
+        for (int b = 0; b < QW; ++b)
 #pragma unroll
             for (int i = 0; i < RT; ++i)
 #pragma unroll
@@ -320,19 +420,15 @@ struct NodesWave {
                     }
                     p[b][i][e] = x;
                 }
-        }
-        // ---- O^T += V^T P^T
-        bool left_out = false;
         __builtin_amdgcn_s_setprio(1);
-        using Frag = std::conditional_t<F8, f16x8, bf16x8>;
-        const int k8 = col >> 1, vrow = F8 ? (k8 < 4 ? grp * 4 + k8 : 12 + grp * 4 + k8) : grp * 4 + (col >> 2);      // of 32, or of 16
+        using Frag = std::conditional_t<F16, f16x8, bf16x8>;
 #pragma unroll
         for (int h = 0; h < RT / 2; ++h) {
             if (h > 0) __builtin_amdgcn_sched_barrier(0);
             Frag pf[QW];
 #pragma unroll
             for (int b = 0; b < QW; ++b) {
-                if constexpr (F8) {
+                if constexpr (F16) {
                     union {
                         f16x8 v;
                         f16x2v h[4];
@@ -347,25 +443,19 @@ struct NodesWave {
                     const uint2 lo = pack_bf16x4(p[b][2 * h][0], p[b][2 * h][1], p[b][2 * h][2], p[b][2 * h][3]), hi = pack_bf16x4(p[b][2 * h + 1][0], p[b][2 * h + 1][1], p[b][2 * h + 1][2], p[b][2 * h + 1][3]);
                     pf[b] = __builtin_bit_cast(bf16x8, u32x4b{lo.x, lo.y, hi.x, hi.y});
                     // Results are divided by the sum of what was multiplied: with few tokens the rounding of the largest would show in all dims.
-                    const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4b{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
-                    rounded[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[b], rounded[b], 0, 0, 0);
+                    if constexpr (!F8) {
+                        const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4b{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
+                        rounded[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pf[b], rounded[b], 0, 0, 0);
+                    }
                 }
             }
 #pragma unroll
             for (int d = 0; d < DT; ++d) {
                 Frag vf;
                 if constexpr (F8) {
-                    auto from = (__attribute__((address_space(3))) i32x2*)(sv + vrow * kRow + (d ^ turn_v<HD, F8>(vrow)) * 16 + (col & 1) * 8 + h * 32 * kRow);
-                    i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32(from);
-                    if constexpr (MASKED) {
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const uint32_t x = (uint32_t)w[i], nan = ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;     // bytes 0x7f and 0xff
-                            left_out |= nan != 0;
-                            w[i] = (int)(x & ~((nan >> 7) * 255u));
-                        }
-                    }
-                    vf = widen_f16((uint32_t)w[0], (uint32_t)w[1]);
+                    const i32x2 w = values8(h, d);
+                    if constexpr (F16) vf = widen_f16((uint32_t)w[0], (uint32_t)w[1]);
+                    else vf = widen_bf16((uint32_t)w[0], (uint32_t)w[1]);
                 } else {
                     u32x4b x;
 #pragma unroll
@@ -388,30 +478,28 @@ struct NodesWave {
                 }
 #pragma unroll
                 for (int b = 0; b < QW; ++b) {
-                    if constexpr (F8) acc[b][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[b], acc[b][d], 0, 0, 0);
+                    if constexpr (F16) acc[b][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[b], acc[b][d], 0, 0, 0);
                     else acc[b][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[b], acc[b][d], 0, 0, 0);
                 }
             }
         }
         __builtin_amdgcn_s_setprio(0);
         if constexpr (MASKED) odd |= left_out;
+        return true;
     }
 
-    // Maximum, sum of probabilities, and the sum that results are divided by, of this wave's query b (in a lane of any group of 16).
+    // What probabilities are relative to, their sum, and the sum that results are divided by, of this wave's query b (in a lane of any group of 16).
     __device__ __forceinline__ float4 sums(int b) const {
         const float whole = add_lanes16_32(l[b]);
         return make_float4(m[b], whole, F8 ? whole : rounded[b][0], 0.f);
     }
-    __device__ __forceinline__ float drop() const { return !F8 ? 1.f : lift == 0.f ? 0.f : 1.f / lift; }      // what takes the lift back
 };
 
-// What a partial result (its maximum and sums) counts for in one with maximum m.  One that has seen something counts, so that an infinite value in it stays;
-// one that has seen a NaN and nothing else has no maximum.
+// What a partial result, relative to its m, counts for in one relative to m.  What is not finite stays whatever it counts for; a part that has seen a NaN and nothing else has no m.
 __device__ __forceinline__ float share(float4 ml, float m) {
-    if (ml.x == -INFINITY) return ml.y == ml.y ? 0.f : 1.f;
-    const float f = __builtin_amdgcn_exp2f(ml.x - m);
-    return f < 1e-37f ? 1e-37f : f;
+    return ml.x == -INFINITY ? (ml.y == ml.y ? 0.f : 1.f) : __builtin_amdgcn_exp2f(ml.x - m);
 }
+__device__ __forceinline__ float counted(float x, float f) { return fabsf(x) < INFINITY ? x * f : x; }
 
 // ---------------------------------------------------------------- what a workgroup takes
 struct NodesRange {
@@ -625,10 +713,10 @@ __device__ __forceinline__ float4 join_parts(const float* s_o, const float4* s_m
         const float4 part = s_ml[w * apart + i];
         const f32x4b x = *reinterpret_cast<const f32x4b*>(s_o + (size_t)(w * apart + i) * LINE + dim);
         const float f = share(part, ml.x);
-        ml.y += f == 0.f ? 0.f : part.y * f;
-        ml.z += f == 0.f ? 0.f : part.z * f;
+        ml.y += part.y * f;
+        ml.z += part.z * f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] += f == 0.f ? 0.f : x[e] * f;
+        for (int e = 0; e < 4; ++e) o[e] += counted(x[e], f);
     }
     return ml;
 }
@@ -700,6 +788,7 @@ __global__ __launch_bounds__(T::kThreads, 2) void k_attention_nodes(NodesAttnArg
     // Tiles that all queries see to their end come first; from the first other one on (nodes, the end of the row, a block that is not there) every tile
     // goes by what is seen.  (One loop with both kinds in it has two sets of sums, and takes twice the registers for them.)
     int stage = 0, t = t0;
+    bool far = false;                                                    // uniform
     auto arrive_tile = [&] {
         const bool more = t + WK < g.t_end;
         // (what was read of the stage that is filled now has arrived)
@@ -710,7 +799,7 @@ __global__ __launch_bounds__(T::kThreads, 2) void k_attention_nodes(NodesAttnArg
         if (more) asm volatile("s_waitcnt vmcnt(%0)" :: "n"(T::kAll) : "memory");
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     };
-    auto take = [&](auto masked) {
+    auto take = [&](auto mode) {
         const unsigned char* const sk = area + stage * T::kStage;
         const unsigned char* const sv = sk + T::kTile;
         const float* const sc = reinterpret_cast<const float*>(sv + T::kTile);
@@ -718,20 +807,28 @@ __global__ __launch_bounds__(T::kThreads, 2) void k_attention_nodes(NodesAttnArg
 #pragma unroll
         for (int b = 0; b < QW; ++b) {
             seen[b] = ~0u;
-            if constexpr (masked.value) seen[b] = there >> stage & 1 ? (uint32_t)window(s_mask[w.node[b]], (int64_t)t * kNodesTile - g.ctx) : 0u;
+            if constexpr (mode.value == kMasked) seen[b] = there >> stage & 1 ? (uint32_t)window(s_mask[w.node[b]], (int64_t)t * kNodesTile - g.ctx) : 0u;
         }
-        w.template step<masked.value, 2>(sk, sv, sc, sc + 32, a.scale2, seen);
+        if constexpr (F8 && mode.value == kWhole) {
+            // (In the same loop: a loop of its own for what is kFar costs this kernel 170 registers that spill.)
+            if (far || !w.template step<kWhole, 2>(sk, sv, sc, sc + 32, a.scale2, seen)) {
+                far = true;
+                w.template step<kFar, 2>(sk, sv, sc, sc + 32, a.scale2, seen);
+            }
+        } else {
+            w.template step<mode.value, 2>(sk, sv, sc, sc + 32, a.scale2, seen);
+        }
         stage ^= 1;
         t += WK;
     };
     while (t < g.t_end && (int64_t)(t + 1) * kNodesTile <= g.ctx && (there >> stage & 1)) {
         arrive_tile();
-        take(std::false_type{});
+        take(NodesMode<kWhole>{});
     }
     const int first_masked = t;
     while (t < g.t_end) {
         arrive_tile();
-        take(std::true_type{});
+        take(NodesMode<kMasked>{});
     }
 
     // ---- the waves' results as one
@@ -740,18 +837,11 @@ __global__ __launch_bounds__(T::kThreads, 2) void k_attention_nodes(NodesAttnArg
     float* const s_o = reinterpret_cast<float*>(lds);
     float4* const s_ml = reinterpret_cast<float4*>(lds + (size_t)WK * T::kQueries * T::kLine * 4);
     const int col = lane & 15, grp = lane >> 4;
-    const float drop = w.drop();
 #pragma unroll
     for (int b = 0; b < QW; ++b) {
         const int i = wave * T::kQueries + b * 16 + col;
 #pragma unroll
-        for (int d = 0; d < HD / 16; ++d) {
-            f32x4b x = w.acc[b][d];
-            if constexpr (F8)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] *= drop;
-            *reinterpret_cast<f32x4b*>(s_o + (size_t)i * T::kLine + d * 16 + grp * 4) = x;
-        }
+        for (int d = 0; d < HD / 16; ++d) *reinterpret_cast<f32x4b*>(s_o + (size_t)i * T::kLine + d * 16 + grp * 4) = w.acc[b][d];
         const float4 ml = w.sums(b);
         if (grp == 0) s_ml[i] = ml;
     }
@@ -881,14 +971,15 @@ __global__ __launch_bounds__(T::kThreads, 2) void k_attention_nodes_wide(NodesAt
         ++t;
     };
     constexpr int kStep = T::RT * 16;                                    // tokens of a wave's step
-    auto take = [&](auto masked) {
-        if (idle) return;
+    constexpr int kSteps = T::kTokens / kStep;
+    auto take = [&](auto mode, int from) {                               // the tile's steps from `from` on; how far that came
+        if (idle) return kSteps;
         const unsigned char* const base = lds + stage * T::kStage;
 #pragma unroll 1
-        for (int step = 0; step < T::kTokens / kStep; ++step) {
-            if (((t * (T::kTokens / kStep) + step) & (WK - 1)) != wk) continue;
+        for (int step = from; step < kSteps; ++step) {
+            if (((t * kSteps + step) & (WK - 1)) != wk) continue;
             const int64_t j0 = (int64_t)t * T::kTokens + step * kStep - g.ctx;
-            if constexpr (masked.value)
+            if constexpr (mode.value == kMasked)
                 if (j0 >= g.nodes) break;                                // (past the row's end)
             const unsigned char* const sk = base + step * kStep * T::kRow;
             const float* const sc = reinterpret_cast<const float*>(base + 2 * T::kTile) + step * kStep;
@@ -896,20 +987,35 @@ __global__ __launch_bounds__(T::kThreads, 2) void k_attention_nodes_wide(NodesAt
 #pragma unroll
             for (int b = 0; b < QW; ++b) {
                 seen[b] = ~0ull;
-                if constexpr (masked.value) seen[b] = pages >> (step * kStep / TABED_CACHE_BLOCK) & 1 ? window(s_mask[w.node[b]], j0) : 0ull;
+                if constexpr (mode.value == kMasked) seen[b] = pages >> (step * kStep / TABED_CACHE_BLOCK) & 1 ? window(s_mask[w.node[b]], j0) : 0ull;
             }
-            w.template step<masked.value, T::RT>(sk, sk + T::kTile, sc, sc + T::kTokens, a.scale2, seen);
+            if (!w.template step<mode.value, T::RT>(sk, sk + T::kTile, sc, sc + T::kTokens, a.scale2, seen)) return step;
         }
+        return kSteps;
     };
-    while (t < g.t_end && (int64_t)(t + 1) * T::kTokens <= g.ctx && pages == (1u << T::kPages) - 1) {
+    auto whole = [&] { return t < g.t_end && (int64_t)(t + 1) * T::kTokens <= g.ctx && pages == (1u << T::kPages) - 1; };
+    int came = kSteps;
+    while (whole()) {
         arrive_tile();
-        take(std::false_type{});
+        came = take(NodesMode<kWhole>{}, 0);
+        if (came < kSteps) break;
         next_tile();
+    }
+    if constexpr (F8) {
+        if (came < kSteps) {                                             // (in a tile that is there; all waves meet as often as there are tiles, whichever loop they are in)
+            take(NodesMode<kFar>{}, came);
+            next_tile();
+            while (whole()) {
+                arrive_tile();
+                take(NodesMode<kFar>{}, 0);
+                next_tile();
+            }
+        }
     }
     const int first_masked = t;
     while (t < g.t_end) {
         arrive_tile();
-        take(std::true_type{});
+        take(NodesMode<kMasked>{}, 0);
         next_tile();
     }
 
@@ -920,18 +1026,11 @@ __global__ __launch_bounds__(T::kThreads, 2) void k_attention_nodes_wide(NodesAt
     float* const s_o = reinterpret_cast<float*>(lds);
     float4* const s_ml = reinterpret_cast<float4*>(lds + (size_t)T::kQueries * T::kLine * 4);
     const int col = lane & 15, grp = lane >> 4, apart = WQ * T::kUnit;
-    const float drop = w.drop();
 #pragma unroll
     for (int b = 0; b < QW; ++b) {
         const int i = wk * apart + wq * T::kUnit + b * 16 + col;
 #pragma unroll
-        for (int d = 0; d < HD / 16; ++d) {
-            f32x4b x = w.acc[b][d];
-            if constexpr (F8)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) x[e] *= drop;
-            *reinterpret_cast<f32x4b*>(s_o + (size_t)i * T::kLine + d * 16 + grp * 4) = x;
-        }
+        for (int d = 0; d < HD / 16; ++d) *reinterpret_cast<f32x4b*>(s_o + (size_t)i * T::kLine + d * 16 + grp * 4) = w.acc[b][d];
         const float4 ml = w.sums(b);
         if (grp == 0) s_ml[i] = ml;
     }
@@ -970,8 +1069,8 @@ __global__ __launch_bounds__(256) void k_attention_nodes_join(NodesAttnArgs a) {
         if (s0 + lane < ranges) {
             const float4 ml = a.ml[place(s0 + lane)];
             f = share(ml, m);
-            lw = f == 0.f ? 0.f : ml.y * f;
-            lrw = f == 0.f ? 0.f : ml.z * f;
+            lw = ml.y * f;
+            lrw = ml.z * f;
         }
         l += wave_sum(lw);
         lr += wave_sum(lrw);
@@ -989,8 +1088,8 @@ __global__ __launch_bounds__(256) void k_attention_nodes_join(NodesAttnArgs a) {
                 const float fs = s + i8 * PARTS < some ? lane_f32(f, s + i8 * PARTS) : 0.f;
 #pragma unroll
                 for (int p = 0; p < PL; ++p) {
-                    o[p][0] += fs == 0.f ? 0.f : x[i8][p].x * fs;
-                    o[p][1] += fs == 0.f ? 0.f : x[i8][p].y * fs;
+                    o[p][0] += counted(x[i8][p].x, fs);
+                    o[p][1] += counted(x[i8][p].y, fs);
                 }
             }
         }
