@@ -340,7 +340,9 @@ struct NodesWave {
                 for (int e = 0; e < 4; ++e) top = fmaxf(top, p[b][i][e]);
             top = max_lanes16_32(top);
             if (__any(top > 6.f || (m[b] == -INFINITY && top > -INFINITY))) {
-                const float next = top > -INFINITY ? fmaxf(m[b], base + top) : m[b], fade = next == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[b] - next);
+                // (A query whose own maximum does not ask for it stays as it is, to the bit: others' scores are those of entries that it may not see.)
+                const bool mine = top > 6.f || m[b] == -INFINITY;
+                const float next = mine ? fmaxf(m[b], base + top) : m[b], fade = next == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[b] - next);
                 m[b] = next;
                 l[b] *= fade;
 #pragma unroll

@@ -114,7 +114,7 @@ def test_a_large_sibling_is_nothing_to_those_beside_it(B, N, qh, kvh, hd, scale)
     check(B, cache, q.cpu(), ctx, parents)
 
 
-@pytest.mark.parametrize("bf16", [False])
+@pytest.mark.parametrize("bf16", [False, True])
 @pytest.mark.parametrize("hd", [64, 128, 256])
 @pytest.mark.parametrize("N,qh,kvh", SHAPES)
 def test_a_loud_sibling_is_nothing_to_those_beside_it(B, N, qh, kvh, hd, bf16):
