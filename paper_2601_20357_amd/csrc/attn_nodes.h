@@ -266,7 +266,7 @@ struct NodesWave {
             }
         }
         // ---- the softmax, in units of log2.  Scores are taken relative to the maximum so far before the new one is known: it is raised only where it would be by
-        // more than 2^6 (probabilities are relative to the one they were taken with, and no less exact), and then they are made again.
+        // more than 2^8 (probabilities are relative to the one they were taken with, and no less exact), and then they are made again.
         float p[QW][RT][4];
 #pragma unroll
         for (int b = 0; b < QW; ++b) {
@@ -339,9 +339,9 @@ struct NodesWave {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) top = fmaxf(top, p[b][i][e]);
             top = max_lanes16_32(top);
-            if (__any(top > 6.f || (m[b] == -INFINITY && top > -INFINITY))) {
+            if (__any(top > 8.f || (m[b] == -INFINITY && top > -INFINITY))) {
                 // (A query whose own maximum does not ask for it stays as it is, to the bit: others' scores are those of entries that it may not see.)
-                const bool mine = top > 6.f || m[b] == -INFINITY;
+                const bool mine = top > 8.f || m[b] == -INFINITY;
                 const float next = mine ? fmaxf(m[b], base + top) : m[b], fade = next == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[b] - next);
                 m[b] = next;
                 l[b] *= fade;
