@@ -686,6 +686,35 @@ __device__ __forceinline__ void add_odd(const NodesAttnArgs& a, const NodesRange
     }
 }
 
+// What was left out may be what nobody sees: slots behind the row's end or nodes that are not there, in a pool that was never cleared, or the block read in place of one that is not there.
+// The workgroup goes once over the row's tokens in those tiles, all at a time (add_odd goes one by one: with 6000 tokens behind a hole 40 nodes took 576 us for 26), and only
+// if one of them has such a value is there something to add.
+template <int HD, bool F8, int THREADS, typename Masked>
+__device__ __forceinline__ bool odd_is_seen(const NodesAttnArgs& a, const NodesRange& g, int t_begin, int t_end, int kvh, int* found, Masked masked) {
+    constexpr int kPieces = HD * (F8 ? 1 : 2) / 16;
+    __syncthreads();
+    if (threadIdx.x == 0) *found = 0;
+    __syncthreads();
+    const int64_t first = (int64_t)t_begin * kNodesTile, end = min((int64_t)t_end * kNodesTile, (int64_t)g.ctx + g.nodes);
+    for (int64_t i = first * kPieces + threadIdx.x; i < end * kPieces; i += THREADS) {
+        const int64_t pos = i / kPieces;
+        if (!masked((int)(pos / kNodesTile))) continue;
+        const int block = a.c.block_of(g.row, pos);
+        if (block < 0) continue;
+        const int64_t from = a.c.entry(a.c.layer, block, kvh, (int)(pos % TABED_CACHE_BLOCK)) * (F8 ? 1 : 2) + i % kPieces * 16;
+        const u32x4b x = *reinterpret_cast<const u32x4b*>(a.c.v + from);
+        bool odd = false;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if constexpr (F8) odd |= (((x[e] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
+            else odd |= (x[e] & 0x7f80u) == 0x7f80u || (x[e] & 0x7f800000u) == 0x7f800000u;
+        }
+        if (odd) *found = 1;
+    }
+    __syncthreads();
+    return *found != 0;
+}
+
 // Four dims of query qi of (row, head): the result, or a range's part of it.
 template <int HD>
 __device__ __forceinline__ void store_result(const NodesAttnArgs& a, const NodesRange& g, int kvh, int tile_q, int qi, int dim, float4 ml, const float (&o)[4]) {
@@ -850,13 +879,14 @@ __global__ __launch_bounds__(T::kThreads, 2) void k_attention_nodes(NodesAttnArg
     if (lane == 0) sh.first_masked[wave] = first_masked;
     if (w.odd) sh.pick[3] = 1;
     __syncthreads();
-    const bool odd = sh.pick[3] != 0;
+    auto masked = [&](int tile) { return tile >= sh.first_masked[(tile - g.t_begin) % WK]; };
+    const bool odd = sh.pick[3] != 0 && odd_is_seen<HD, F8, T::kThreads>(a, g, g.t_begin, g.t_end, kvh, &sh.pick[3], masked);
     for (int p = tid; p < queries * (HD / 4); p += T::kThreads) {
         const int i = p / (HD / 4), dim = p % (HD / 4) * 4;
         float o[4];
         const float4 ml = join_parts<T::kLine>(s_o, s_ml, WK, T::kQueries, i, dim, o);
         if (odd)
-            add_odd<HD, F8>(a, g, g.t_begin, g.t_end, kvh, s_mask[i / a.group], dim, [&](int tile) { return tile >= sh.first_masked[(tile - g.t_begin) % WK]; }, o);
+            add_odd<HD, F8>(a, g, g.t_begin, g.t_end, kvh, s_mask[i / a.group], dim, masked, o);
         store_result<HD>(a, g, kvh, 0, i, dim, ml, o);
     }
 }
@@ -1037,12 +1067,14 @@ __global__ __launch_bounds__(T::kThreads, 2) void k_attention_nodes_wide(NodesAt
         if (grp == 0) s_ml[i] = ml;
     }
     __syncthreads();
-    const bool odd = sh.pick[3] != 0;
+    auto masked = [](int) { return true; };                              // from the first one on
+    const int odd_from = first_masked * (T::kTokens / kNodesTile), odd_to = g.t_end * (T::kTokens / kNodesTile);
+    const bool odd = sh.pick[3] != 0 && odd_is_seen<HD, F8, T::kThreads>(a, g, odd_from, odd_to, kvh, &sh.pick[3], masked);
     for (int p = tid; p < here * (HD / 4); p += T::kThreads) {
         const int i = p / (HD / 4), dim = p % (HD / 4) * 4, qi = tile_q * a.per_tile + i;
         float o[4];
         const float4 ml = join_parts<T::kLine>(s_o, s_ml, WK, apart, i, dim, o);
-        if (odd) add_odd<HD, F8>(a, g, first_masked * (T::kTokens / kNodesTile), g.t_end * (T::kTokens / kNodesTile), kvh, s_mask[qi / a.group], dim, [](int) { return true; }, o);
+        if (odd) add_odd<HD, F8>(a, g, odd_from, odd_to, kvh, s_mask[qi / a.group], dim, masked, o);
         store_result<HD>(a, g, kvh, tile_q, qi, dim, ml, o);
     }
 }
