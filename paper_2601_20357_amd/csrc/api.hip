@@ -665,10 +665,11 @@ int tabed_verify_nodes_workspace_init(const tabed_cfg* cfg, int32_t N, void* ws,
     return e == hipSuccess ? TABED_OK : fail_hip(e);
 }
 
-int tabed_verify_nodes(const tabed_cfg* cfg, void* ws, uint64_t round, int32_t N, const float* target_logits, const float* draft_logits,
+// tabed_verify_nodes, for the tests with waits that end after `spins` polls, and with workgroup `late` of every sequence coming 3 ms after the others (0, -1: as in earnest).
+int tabed_testing_verify_nodes(const tabed_cfg* cfg, void* ws, uint64_t round, int32_t N, const float* target_logits, const float* draft_logits,
                        const double* draft_lse, const int32_t* tokens, const float* node_q, const int32_t* parents, const int32_t* n_nodes,
                        const float* weights, const float* temperature, const float* u_acc, const float* u_res, int32_t* path, int32_t* n_path,
-                       int32_t* out_tokens, uint8_t* flags, float* dev, int32_t* n_valid, void* stream) {
+                       int32_t* out_tokens, uint8_t* flags, float* dev, int32_t* n_valid, void* stream, int32_t spins, int32_t late) {
     const int rc = validate_verify_nodes(cfg, N);
     if (rc != TABED_OK) return rc;
     if (!ws || !target_logits || !draft_logits || !draft_lse || !tokens || !node_q || !weights || !temperature || !path || !n_path || !out_tokens || !flags)
@@ -680,8 +681,16 @@ int tabed_verify_nodes(const tabed_cfg* cfg, void* ws, uint64_t round, int32_t N
         if (element_misaligned(p, 0)) return TABED_EALIGN;
     const hipError_t e = launch_verify_nodes(*cfg, static_cast<char*>(ws), round, N, target_logits, draft_logits, draft_lse, tokens, node_q, parents, n_nodes,
                                              weights, temperature, u_acc, u_res, path, n_path, out_tokens, flags, dev, n_valid,
-                                             static_cast<hipStream_t>(stream));
+                                             static_cast<hipStream_t>(stream), spins, late);
     return e == hipSuccess ? TABED_OK : fail_hip(e);
+}
+
+int tabed_verify_nodes(const tabed_cfg* cfg, void* ws, uint64_t round, int32_t N, const float* target_logits, const float* draft_logits,
+                       const double* draft_lse, const int32_t* tokens, const float* node_q, const int32_t* parents, const int32_t* n_nodes,
+                       const float* weights, const float* temperature, const float* u_acc, const float* u_res, int32_t* path, int32_t* n_path,
+                       int32_t* out_tokens, uint8_t* flags, float* dev, int32_t* n_valid, void* stream) {
+    return tabed_testing_verify_nodes(cfg, ws, round, N, target_logits, draft_logits, draft_lse, tokens, node_q, parents, n_nodes, weights, temperature, u_acc, u_res, path,
+                                      n_path, out_tokens, flags, dev, n_valid, stream, 0, -1);
 }
 
 int tabed_cache_keep_nodes(const tabed_cache_paged* cache, int32_t rows, int32_t N, const int32_t* ctx_base, const int32_t* path, const int32_t* n_path,

@@ -25,6 +25,7 @@ struct NodesVerifyLayout {
     int G;               // workgroups of a sequence
     size_t off_rec;      // uint64 [B][N][G][4] what a workgroup found at a step of the walk
     size_t off_dev;      // uint64 [B][gamma][G][n][2] its sums of the distances
+    size_t off_state;    // uint64 [B] what has come of a row
     size_t total;
 };
 NodesVerifyLayout nodes_verify_layout(const tabed_cfg& c, int N);
@@ -32,6 +33,6 @@ hipError_t launch_nodes_verify_init(const tabed_cfg& c, int N, char* ws, hipStre
 hipError_t launch_verify_nodes(const tabed_cfg& c, char* ws, uint64_t round, int N, const float* target_logits, const float* draft_logits,
                                const double* draft_lse, const int32_t* tokens, const float* node_q, const int32_t* parents, const int32_t* n_nodes,
                                const float* weights, const float* temperature, const float* u_acc, const float* u_res, int32_t* path, int32_t* n_path,
-                               int32_t* out_tokens, uint8_t* flags, float* dev, int32_t* n_valid, hipStream_t s);
+                               int32_t* out_tokens, uint8_t* flags, float* dev, int32_t* n_valid, hipStream_t s, int spins = 0, int late = -1);      // (the last two: for tests)
 
 }  // namespace tabed

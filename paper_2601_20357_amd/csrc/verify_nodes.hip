@@ -16,7 +16,8 @@
 // Why nothing waits for ever: workgroups are numbered as they start, sequence by sequence, so that a sequence's workgroups wait for ones that run already
 // or start as soon as any other sequence, or another kernel, ends; launches on the four queues of a process each hold back less than one sequence's
 // workgroups, at most 127 of the 768 that run at a time.  A workspace that was never prepared is known by a mark.  A wait has a bound of some seconds all
-// the same; a row whose wait ended unanswered is left without a token, flagged.
+// the same, and what comes of a row is then settled by one word: whoever has all of the walk's records and whoever gives up set it, the first of them for all.  A row that was
+// given up is left without a token, flagged, by its first workgroup; where it was not, who would have given up finds the records that it waited for.
 //
 // What bounds it: the steps, one after the other.  One is 4 to 5 us: 1 for the row's maximum and exponentials, 1.5 until all pieces' are known, 1 for their
 // sum, the rest for the distances, the test and the next node's rows; a launch with one node and nothing to test takes 8 to 12.  16 sequences of 22 nodes, V = 32000, 4
@@ -40,6 +41,7 @@ constexpr int kVerSpins = 1 << 24;
 
 struct VerifyArgs {
     int V, n, B, N, G, gamma, tvd;
+    int spins, late;                                                     // polls of a wait; for tests: a workgroup of every sequence that comes 3 ms late, -1: none
     uint64_t seed, round;
     const float* target;
     const float* drafts;
@@ -61,7 +63,9 @@ struct VerifyArgs {
     uint64_t* ctl;
     uint64_t* rec;
     uint64_t* devrec;
+    uint64_t* state;                                                     // [B] the launch's number, and what has come of the row
 };
+enum : uint32_t { kVerDone = 1, kVerGone = 2 };
 
 __device__ __forceinline__ void say(uint64_t* p, uint32_t v, uint32_t launch) {
     __hip_atomic_store(p, (uint64_t)launch << 32 | v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -70,15 +74,43 @@ __device__ __forceinline__ uint32_t lo32(double v) { return (uint32_t)__builtin_
 __device__ __forceinline__ uint32_t hi32(double v) { return (uint32_t)(__builtin_bit_cast(uint64_t, v) >> 32); }
 __device__ __forceinline__ double from32(uint32_t lo, uint32_t hi) { return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo); }
 __device__ __forceinline__ float as_float(uint32_t v) { return __builtin_bit_cast(float, v); }
+// What comes of the row: `mine`, unless somebody settled it before.  The word holds the launch before this one, as a rule, or anything else that is not of this launch: a first try
+// goes by that, and what it found is looked at when it is back.
+__device__ __forceinline__ bool try_settle(uint64_t* state, uint64_t& seen, uint32_t mine, uint32_t launch) {
+    return __hip_atomic_compare_exchange_strong(state, &seen, (uint64_t)launch << 32 | mine, __ATOMIC_RELAXED, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+struct Settling {
+    uint64_t seen;
+    bool won;
+    __device__ __forceinline__ void begin(uint64_t* state, uint32_t mine, uint32_t launch) {
+        seen = launch == 1 ? 0ull : (uint64_t)(launch - 1) << 32 | kVerDone;
+        won = try_settle(state, seen, mine, launch);
+    }
+    __device__ __forceinline__ uint32_t end(uint64_t* state, uint32_t mine, uint32_t launch) {
+        if (!won && (uint32_t)(seen >> 32) != launch) won = try_settle(state, seen, mine, launch);
+        return won ? mine : (uint32_t)seen;
+    }
+};
+
 // The word at p once it is this launch's; ok turns false where it does not come.
-__device__ __forceinline__ uint32_t hear(const uint64_t* p, uint32_t launch, bool& ok) {
-    for (int i = 0; i < kVerSpins; ++i) {
+__device__ __forceinline__ uint32_t hear(const uint64_t* p, uint32_t launch, int spins, bool& ok) {
+    for (int i = 0; i < spins; ++i) {
         const uint64_t w = __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         if ((uint32_t)(w >> 32) == launch) return (uint32_t)w;
         if (i > 64) __builtin_amdgcn_s_sleep(1);
     }
     ok = false;
     return 0;
+}
+// A thread whose words did not come: the row is given up, unless somebody has all records of the walk; then they are there.  (A call, so that what never happens takes no
+// registers from what does: within the loops above it cost 5 % of a large batch's time.)
+__device__ __attribute__((noinline)) bool hear_or_give_up(const uint64_t* from, int words, uint32_t* to, uint32_t launch, uint64_t* state) {
+    Settling settling;
+    settling.begin(state, kVerGone, launch);
+    if (settling.end(state, kVerGone, launch) != kVerDone) return false;
+    bool ok = true;
+    for (int w = threadIdx.x; w < words; w += kVerThreads) to[w] = hear(from + w, launch, kVerSpins, ok);
+    return ok;
 }
 
 // e^x in 64 bits: x = n ln 2 + r, |r| <= ln 2 / 2, the series of e^r up to r^11 / 11! (what is left out is below 7e-15 of the result, ln 2's rounding
@@ -109,9 +141,9 @@ struct VerifyShared {
     double red[kVerWaves][kVerDraftsAtOnce];
     float redf[kVerWaves];
     int redi[kVerWaves], redk[kVerWaves];
-    int ticket, bad;
+    int ticket, bad, done;
     uint32_t launch;
-    float weight[TABED_MAX_N];
+    float weight[TABED_MAX_N], dist[TABED_MAX_N];
     uint8_t flag[TABED_MAX_NODES];
     int path[TABED_MAX_NODES];
     int16_t at_step[TABED_MAX_NODES];                                    // of the path's nodes
@@ -175,6 +207,10 @@ __global__ __launch_bounds__(kVerThreads, 3) void k_verify_nodes(VerifyArgs a) {
     const bool prepared = ticket >= 0;
     if (!prepared) ticket = blockIdx.x;
     const int b = ticket / a.G, c = ticket % a.G;
+    if (c == a.late) {                                                   // (tests)
+        const uint64_t began = __builtin_amdgcn_s_memrealtime();
+        while (__builtin_amdgcn_s_memrealtime() - began < 300000) __builtin_amdgcn_s_sleep(8);
+    }
     Piece<NG> piece;
 #pragma unroll
     for (int i = 0; i < NG; ++i) {
@@ -197,14 +233,16 @@ __global__ __launch_bounds__(kVerThreads, 3) void k_verify_nodes(VerifyArgs a) {
     lds_barrier();
     const bool greedy = !(T > 0.f);
     const double inv_t = greedy ? 1.0 : 1.0 / (double)T;
+    uint64_t* const state = a.state + b;
     uint64_t* const rec_b = a.rec + (size_t)b * a.N * a.G * 4;
     uint64_t* const dev_b = a.devrec + (size_t)b * a.gamma * a.G * n * 2;
 
-    // A step's records, read by all into s.rec; false, for all, where one does not come.
+    // A step's records, read by all into s.rec; false, for all, where one does not come and the row is given up.
     auto collect = [&](int step) {
         bool ok = true;
         const uint64_t* from = rec_b + (size_t)step * a.G * 4;
-        for (int w = tid; w < a.G * 4; w += kVerThreads) s.rec[w / 4][w % 4] = hear(from + w, launch, ok);
+        for (int w = tid; w < a.G * 4; w += kVerThreads) s.rec[w / 4][w % 4] = hear(from + w, launch, a.spins, ok);
+        if (__builtin_expect(!ok, 0)) ok = hear_or_give_up(from, a.G * 4, &s.rec[0][0], launch, state);
         if (!ok) s.bad = 1;                                              // (never taken back: who reads it behind the barrier reads it before the next)
         lds_barrier();
         return s.bad == 0;
@@ -428,6 +466,10 @@ __global__ __launch_bounds__(kVerThreads, 3) void k_verify_nodes(VerifyArgs a) {
     }
 
     // ---- the last draw: the piece that it falls into by the masses, in it the token
+    bool settles = c == 0 || c < valid;                                  // those that write anything
+    Settling settling{};                                                 // (thread 0; on its way while the token is looked for)
+    int token = -1;                                                      // the thread that found it, and what is flagged
+    uint8_t token_flag = 0;
     if (count > 0 && fine && !greedy) {
         const bool gone = level > 0 && !(total > 0.0);                   // nothing is left of f: p again
         if (gone) {
@@ -468,6 +510,8 @@ __global__ __launch_bounds__(kVerThreads, 3) void k_verify_nodes(VerifyArgs a) {
             crossed = over != 0;
             run = lane_f64(incl, 63);
         }
+        settles = settles || c == owner;
+        if (settles && tid == 0) settling.begin(state, kVerDone, launch);
         if (c == owner) {
             int first = 0x7fffffff, last = -1;
             double lo[kVerE];
@@ -497,14 +541,70 @@ __global__ __launch_bounds__(kVerThreads, 3) void k_verify_nodes(VerifyArgs a) {
                     if (f[i * 4 + e] > 0.0 && piece.at[i] + e == pick) {
                         const double l = lo[i * 4 + e], h = l + f[i * 4 + e];
                         if (fmin(fabs(h - goal), fabs(goal - l)) < (double)kMargin * whole) flag |= TABED_FLAG_SAMPLE_MARGIN;
-                        a.out_tokens[(size_t)b * a.N + depth] = pick;
-                        a.flags[(size_t)b * a.N] = flag;
+                        token = pick;
+                        token_flag = flag;
                     }
             if (pick < 0 && tid == 0) {                                  // no element has any mass (NaN)
-                a.out_tokens[(size_t)b * a.N + depth] = 0;
-                a.flags[(size_t)b * a.N] = TABED_FLAG_DEGENERATE;
+                token = 0;
+                token_flag = TABED_FLAG_DEGENERATE;
             }
         }
+    } else if (count > 0 && fine && settles && tid == 0) {
+        settling.begin(state, kVerDone, launch);
+    }
+
+    // ---- the verdict, once it is back
+    bool open = settles && count > 0 && fine;
+    auto verdict = [&] {
+        if (tid == 0) s.done = settling.end(state, kVerDone, launch) == kVerDone;
+        lds_barrier();
+        fine = s.done != 0;
+        open = false;
+    };
+    if (open && (a.tvd || c >= valid)) verdict();
+
+    // ---- the distances: the positions are dealt to the workgroups, a wave adds up a draft's.  (KL: what is added up is said by all that have come to the position, also by those that
+    // give up there, so that the first position need not wait for the verdict.)
+    for (int i = c; i < valid && fine; i += a.G) {
+        const uint64_t* const from = rec_b + (size_t)s.at_step[i] * a.G * 4;
+        for (int j = wave; j < n; j += kVerWaves) {
+            bool ok = true;
+            float m[2] = {-INFINITY, -INFINITY};
+            double sum[2] = {0.0, 0.0}, part[2] = {0.0, 0.0};
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int g = h * 64 + lane;
+                if (g >= a.G) continue;
+                const uint64_t* const dev = dev_b + (((size_t)i * a.G + g) * n + j) * 2;
+                m[h] = as_float(hear(from + g * 4, launch, kVerSpins, ok));
+                sum[h] = from32(hear(from + g * 4 + 2, launch, kVerSpins, ok), hear(from + g * 4 + 3, launch, kVerSpins, ok));
+                part[h] = from32(hear(dev, launch, kVerSpins, ok), hear(dev + 1, launch, kVerSpins, ok));
+            }
+            const float top = wave_max(fmaxf(m[0], m[1]));
+            double z = 0.0, t = 0.0;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const double up = ((double)m[h] - (double)top) * inv_t;
+                if (a.tvd) t += part[h];
+                else if (m[h] != -INFINITY) {
+                    const double w = exp64(up);
+                    z += w * sum[h];
+                    t += w * (part[h] + up * sum[h]);
+                }
+            }
+            z = wave_sum(z);
+            t = wave_sum(t);
+            const bool all = __all(ok);
+            if (lane == 0) s.dist[j] = all ? (float)(a.tvd ? 0.5 * t : t / z - log(z)) : __builtin_nanf("");
+        }
+        if (open) verdict();
+        lds_barrier();
+        if (tid < n && fine) a.dev[((size_t)b * a.gamma + i) * n + tid] = s.dist[tid];
+        lds_barrier();
+    }
+    if (token >= 0 && fine) {
+        a.out_tokens[(size_t)b * a.N + depth] = token;
+        a.flags[(size_t)b * a.N] = token_flag;
     }
 
     // ---- the first workgroup tells the way
@@ -522,42 +622,6 @@ __global__ __launch_bounds__(kVerThreads, 3) void k_verify_nodes(VerifyArgs a) {
         if (tid == 0) {
             a.n_path[b] = said;
             if (a.n_valid != nullptr) a.n_valid[b] = said > 0 ? valid : 0;
-        }
-    }
-
-    // ---- the distances: the positions are dealt to the workgroups, a wave adds up a draft's
-    if (!fine) return;
-    lds_barrier();
-    for (int i = c; i < valid; i += a.G) {
-        const uint64_t* const from = rec_b + (size_t)s.at_step[i] * a.G * 4;
-        bool ok = true;
-        for (int j = wave; j < n; j += kVerWaves) {
-            float m[2] = {-INFINITY, -INFINITY};
-            double sum[2] = {0.0, 0.0}, part[2] = {0.0, 0.0};
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int g = h * 64 + lane;
-                if (g >= a.G) continue;
-                const uint64_t* const dev = dev_b + (((size_t)i * a.G + g) * n + j) * 2;
-                m[h] = as_float(hear(from + g * 4, launch, ok));
-                sum[h] = from32(hear(from + g * 4 + 2, launch, ok), hear(from + g * 4 + 3, launch, ok));
-                part[h] = from32(hear(dev, launch, ok), hear(dev + 1, launch, ok));
-            }
-            const float top = wave_max(fmaxf(m[0], m[1]));
-            double z = 0.0, t = 0.0;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const double up = ((double)m[h] - (double)top) * inv_t;
-                if (a.tvd) t += part[h];
-                else if (m[h] != -INFINITY) {
-                    const double w = exp64(up);
-                    z += w * sum[h];
-                    t += w * (part[h] + up * sum[h]);
-                }
-            }
-            z = wave_sum(z);
-            t = wave_sum(t);
-            if (lane == 0) a.dev[((size_t)b * a.gamma + i) * n + j] = (float)(a.tvd ? 0.5 * t : t / z - log(z));
         }
     }
 }
@@ -578,7 +642,8 @@ NodesVerifyLayout nodes_verify_layout(const tabed_cfg& c, int N) {
     const size_t groups = std::max<size_t>((size_t)c.B * ((c.V + kVerThreads * 8 - 1) / (kVerThreads * 8)), kVerSmallGroups);
     L.off_rec = kVerControl;                                             // (never less for more sequences or longer rows, whatever their pieces)
     L.off_dev = L.off_rec + up(groups * N * 4 * 8);
-    L.total = L.off_dev + up(groups * c.gamma * c.n * 2 * 8);
+    L.off_state = L.off_dev + up(groups * c.gamma * c.n * 2 * 8);
+    L.total = L.off_state + up((size_t)c.B * 8);
     return L;
 }
 
@@ -595,12 +660,12 @@ hipError_t launch_nodes_verify_init(const tabed_cfg& c, int N, char* ws, hipStre
 hipError_t launch_verify_nodes(const tabed_cfg& c, char* ws, uint64_t round, int N, const float* target_logits, const float* draft_logits,
                                const double* draft_lse, const int32_t* tokens, const float* node_q, const int32_t* parents, const int32_t* n_nodes,
                                const float* weights, const float* temperature, const float* u_acc, const float* u_res, int32_t* path, int32_t* n_path,
-                               int32_t* out_tokens, uint8_t* flags, float* dev, int32_t* n_valid, hipStream_t s) {
+                               int32_t* out_tokens, uint8_t* flags, float* dev, int32_t* n_valid, hipStream_t s, int spins, int late) {
     ProfScope prof(TABED_K_TREE, s);
     const NodesVerifyLayout L = nodes_verify_layout(c, N);
-    const VerifyArgs a{c.V, c.n, c.B, N, L.G, c.gamma, c.distance == 1, c.seed, round, target_logits, draft_logits, draft_lse, tokens, node_q, parents,
+    const VerifyArgs a{c.V, c.n, c.B, N, L.G, c.gamma, c.distance == 1, spins > 0 ? spins : kVerSpins, late, c.seed, round, target_logits, draft_logits, draft_lse, tokens, node_q, parents,
                        n_nodes, weights, temperature, u_acc, u_res, path, n_path, out_tokens, flags, dev, n_valid, reinterpret_cast<uint64_t*>(ws),
-                       reinterpret_cast<uint64_t*>(ws + L.off_rec), reinterpret_cast<uint64_t*>(ws + L.off_dev)};
+                       reinterpret_cast<uint64_t*>(ws + L.off_rec), reinterpret_cast<uint64_t*>(ws + L.off_dev), reinterpret_cast<uint64_t*>(ws + L.off_state)};
     const dim3 grid((unsigned)(c.B * L.G)), block(kVerThreads);
     if (c.V < 4) launch(&prof, k_verify_nodes<true, 1>, grid, block, 0, s, a);
     else if (piece_of(c) == kVerThreads * 4) launch(&prof, k_verify_nodes<false, 1>, grid, block, 0, s, a);
