@@ -569,6 +569,7 @@ int tabed_attention_nodes(const tabed_cache_paged* cache, int32_t layer, void* w
  * `ws`: tabed_verify_nodes_workspace_bytes bytes, prepared once by ..._init; it then serves calls of any sizes that need no more bytes, all that are smaller in
  * everything among them.  It belongs to the library from the preparation on; calls that share it must not overlap.
  * A row whose workgroups waited for each other in vain, for some seconds, has no path: n_path and n_valid 0, path and out_tokens -1, flags[b][0] TABED_FLAG_DEGENERATE.
+ * So have, at once, all rows of a call with a workspace that was prepared for fewer bytes than it needs, or never.
  */
 size_t tabed_verify_nodes_workspace_bytes(const tabed_cfg* cfg, int32_t N);   /* 0: invalid */
 int tabed_verify_nodes_workspace_init(const tabed_cfg* cfg, int32_t N, void* ws, void* stream);

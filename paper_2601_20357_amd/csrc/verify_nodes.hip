@@ -15,7 +15,7 @@
 //
 // Why nothing waits for ever: workgroups are numbered as they start, sequence by sequence, so that a sequence's workgroups wait for ones that run already
 // or start as soon as any other sequence, or another kernel, ends; launches on the four queues of a process each hold back less than one sequence's
-// workgroups, at most 127 of the 768 that run at a time.  A workspace that was never prepared is known by a mark.  A wait has a bound of some seconds all
+// workgroups, at most 127 of the 768 that run at a time.  A workspace that was never prepared, or for less, is known by a mark.  A wait has a bound of some seconds all
 // the same, and what comes of a row is then settled by one word: whoever has all of the walk's records and whoever gives up set it, the first of them for all.  A row that was
 // given up is left without a token, flagged, by its first workgroup; where it was not, who would have given up finds the records that it waited for.
 //
@@ -35,12 +35,13 @@ namespace tabed {
 
 constexpr int kVerThreads = 256, kVerWaves = kVerThreads / 64, kVerMaxPieces = 128;      // pieces are of 4 or 8 elements a thread
 constexpr int kVerDraftsAtOnce = 4;
-constexpr size_t kVerControl = 256;                                      // uint64: the launch's number and the next workgroup's; uint32 in the next line: mark
+constexpr size_t kVerControl = 256;                                      // uint64: the launch's number and the next workgroup's; in the next line: mark, and what was prepared
 constexpr uint32_t kVerMark = 0x7ab3d0deu;
 constexpr int kVerSpins = 1 << 24;
 
 struct VerifyArgs {
     int V, n, B, N, G, gamma, tvd;
+    uint32_t units;                                                      // of 256 bytes of workspace
     int spins, late;                                                     // polls of a wait; for tests: a workgroup of every sequence that comes 3 ms late, -1: none
     uint64_t seed, round;
     const float* target;
@@ -192,14 +193,15 @@ __global__ __launch_bounds__(kVerThreads, 3) void k_verify_nodes(VerifyArgs a) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = a.V, n = a.n;
     if (tid == 0) {
         // One trip: the launch's number and this workgroup's.  The last one to come makes both ready for the next launch.
-        const uint32_t mark = __hip_atomic_load(reinterpret_cast<const uint32_t*>(a.ctl + 16), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const uint64_t known = __hip_atomic_load(a.ctl + 16, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const uint32_t mark = (uint32_t)known;
         const uint64_t got = __hip_atomic_fetch_add(a.ctl, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         const uint32_t launch = (uint32_t)(got >> 32), at = (uint32_t)got, count = (uint32_t)(a.B * a.G);
         if (mark == kVerMark && at == count - 1)
             __hip_atomic_store(a.ctl, (uint64_t)(launch == 0xffffffffu ? 1u : launch + 1) << 32, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         s.launch = launch;
         s.bad = 0;
-        s.ticket = mark == kVerMark && at < count ? (int)at : -1;
+        s.ticket = mark == kVerMark && (uint32_t)(known >> 32) >= a.units && at < count ? (int)at : -1;
     }
     lds_barrier();
     const uint32_t launch = __builtin_amdgcn_readfirstlane(s.launch);
@@ -649,7 +651,7 @@ NodesVerifyLayout nodes_verify_layout(const tabed_cfg& c, int N) {
 
 __global__ void k_verify_nodes_init(uint32_t* ws, size_t words) {
     for (size_t i = blockIdx.x * (size_t)blockDim.x + threadIdx.x; i < words; i += (size_t)gridDim.x * blockDim.x)
-        ws[i] = i == 1 ? 1u : i == 32 ? kVerMark : 0u;                    // (launch 1, workgroup 0)
+        ws[i] = i == 1 ? 1u : i == 32 ? kVerMark : i == 33 ? (uint32_t)(words / 64) : 0u;      // (launch 1, workgroup 0)
 }
 hipError_t launch_nodes_verify_init(const tabed_cfg& c, int N, char* ws, hipStream_t s) {
     const size_t words = nodes_verify_layout(c, N).total / 4;
@@ -663,7 +665,7 @@ hipError_t launch_verify_nodes(const tabed_cfg& c, char* ws, uint64_t round, int
                                int32_t* out_tokens, uint8_t* flags, float* dev, int32_t* n_valid, hipStream_t s, int spins, int late) {
     ProfScope prof(TABED_K_TREE, s);
     const NodesVerifyLayout L = nodes_verify_layout(c, N);
-    const VerifyArgs a{c.V, c.n, c.B, N, L.G, c.gamma, c.distance == 1, spins > 0 ? spins : kVerSpins, late, c.seed, round, target_logits, draft_logits, draft_lse, tokens, node_q, parents,
+    const VerifyArgs a{c.V, c.n, c.B, N, L.G, c.gamma, c.distance == 1, (uint32_t)(L.total / 256), spins > 0 ? spins : kVerSpins, late, c.seed, round, target_logits, draft_logits, draft_lse, tokens, node_q, parents,
                        n_nodes, weights, temperature, u_acc, u_res, path, n_path, out_tokens, flags, dev, n_valid, reinterpret_cast<uint64_t*>(ws),
                        reinterpret_cast<uint64_t*>(ws + L.off_rec), reinterpret_cast<uint64_t*>(ws + L.off_dev), reinterpret_cast<uint64_t*>(ws + L.off_state)};
     const dim3 grid((unsigned)(c.B * L.G)), block(kVerThreads);

@@ -59,3 +59,27 @@ def test_a_row_has_a_whole_verdict_or_none(N, kind, tvd):
         for k in want:
             assert torch.equal(again[k].cpu(), want[k]), (late, k)
     assert ended > 0                                                     # (waits of 40 polls end before 3 ms)
+
+
+def test_a_workspace_prepared_for_less_ends_flagged():
+    """A buffer that is large enough, prepared for a smaller call: what lies behind that may look like anything, here like words of the next launches."""
+    from paper_2601_20357_amd import binding
+    large, small = tv.make(8, 9, 3, 7000, seed=1), tv.make(2, 3, 1, 500, seed=2)
+    make = lambda c: binding.make_cfg(V=c["target"].shape[2], d=64, n=c["drafts"].shape[2], B=len(c["target"]), gamma=c["target"].shape[1], h=8, w_dtype=1, seed=77)  # noqa: E731
+    cfg, less = make(large), make(small)
+    need = binding.tabed_verify_nodes_workspace_bytes(cfg, 9)
+    assert binding.tabed_verify_nodes_workspace_bytes(less, 3) < need
+    want, want_small = tv.run(binding, large, cfg=cfg)[0], tv.run(binding, small, cfg=less)[0]
+    for launch in (1, 2):
+        ws = torch.full((need // 8,), launch << 32 | 1, dtype=torch.int64, device=DEV).view(torch.uint8)
+        binding.tabed_verify_nodes_workspace_init(less, 3, ws)
+        for _ in range(2):
+            o = tv.run(binding, large, ws=ws, cfg=cfg)[0]
+            assert o["n_path"].tolist() == [0] * 8 and (o["path"] == -1).all() and (o["out"] == -1).all() and (o["flags"][:, 0] == 4).all() and (o["n_valid"] == 0).all()
+            again = tv.run(binding, small, ws=ws, cfg=less)[0]
+            for k in want_small:
+                assert torch.equal(again[k], want_small[k]), k
+        binding.tabed_verify_nodes_workspace_init(cfg, 9, ws)
+        again = tv.run(binding, large, ws=ws, cfg=cfg)[0]
+        for k in want:
+            assert torch.equal(again[k], want[k]), k
