@@ -353,7 +353,7 @@ __global__ __launch_bounds__(kVerThreads, 3) void k_verify_nodes(VerifyArgs a) {
         double z = 0.0;
         for (int g = lane; g < a.G; g += 64) {
             const float mg = as_float(s.rec[g][0]);
-            const double w = mg == -INFINITY ? 0.0 : exp64(((double)mg - (double)all.v) * inv_t) * from32(s.rec[g][2], s.rec[g][3]);
+            const double w = (mg == -INFINITY ? 0.0 : exp64(((double)mg - (double)all.v) * inv_t)) * from32(s.rec[g][2], s.rec[g][3]);      // (a NaN among -inf stays one)
             z += w;
             if (wave == 0) s.p_mass[g] = w;                              // (times 1 / z below)
         }
@@ -588,7 +588,9 @@ __global__ __launch_bounds__(kVerThreads, 3) void k_verify_nodes(VerifyArgs a) {
             for (int h = 0; h < 2; ++h) {
                 const double up = ((double)m[h] - (double)top) * inv_t;
                 if (a.tvd) t += part[h];
-                else if (m[h] != -INFINITY) {
+                else if (m[h] == -INFINITY) {
+                    z += 0.0 * sum[h];
+                } else {
                     const double w = exp64(up);
                     z += w * sum[h];
                     t += w * (part[h] + up * sum[h]);

@@ -1,5 +1,6 @@
 """Verification of trees where a workgroup comes so late that others have stopped waiting for it: a row has a verdict that is whole, or none, flagged."""
 import ctypes
+import math
 
 import pytest
 import torch
@@ -83,3 +84,18 @@ def test_a_workspace_prepared_for_less_ends_flagged():
         again = tv.run(binding, large, ws=ws, cfg=cfg)[0]
         for k in want:
             assert torch.equal(again[k], want[k]), k
+
+
+@pytest.mark.parametrize("at", [0, 1024, 4096])
+def test_nan_among_masked_logits_ends_flagged(at):
+    """A NaN is one also where all others of its workgroup's 1024 logits are -inf."""
+    from paper_2601_20357_amd import binding
+    c = tv.make(3, 4, 2, 5000, seed=8, temp=[1.0])
+    c["target"][1, 0, at:at + 1024] = -math.inf
+    want = tv.run(binding, c)[0]
+    c["target"][1, 0, at + 500] = math.nan
+    o = tv.run(binding, c)[0]
+    assert o["n_path"][1] == 1 and o["path"][1].tolist() == [0, -1, -1, -1] and o["flags"][1, 0] == 4 and 0 <= int(o["out"][1, 0]) < 5000
+    assert int(o["n_valid"][1]) == 0 or bool(o["dev"][1, 0].isnan().all())
+    for k in o:
+        assert torch.equal(o[k][[0, 2]], want[k][[0, 2]]), k
