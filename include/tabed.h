@@ -527,8 +527,8 @@ int tabed_cache_append_nodes(const tabed_cache_paged* cache, int32_t layer, int3
  *   scale   > 0, commonly 1 / sqrt(head_dim)
  * Products of bf16 (and e4m3) values are exact, their sums, the softmax and its sum are in fp32; probabilities are rounded before the product with the
  * values, to bf16 (2^-8 of themselves), or with e4m3 values, and then times the values' scales: to fp16 (2^-11) relative to a query's largest such product, or to bf16 where they are
- * too far apart for that (below 2^-22 to 2^-29 of the largest; the context's others, too, from there on).  Scales above 2^50 or below 2^-40 may lose probabilities below 2^-80 of the
- * largest.  What a node does not see has no influence, whatever it holds.  A node that
+ * too far apart for that (below 2^-22 to 2^-29 of the largest; the context's others, too, from there on).  Products below 2^-130 of
+ * the largest, in which a scale above 2^38 counts as that, and probabilities below 2^-95 of the largest may be lost.  What a node does not see has no influence, whatever it holds.  A node that
  * sees nothing (its blocks are not there) gets zeros and an lse of -inf.  Entries of nodes from n_nodes[r] on are left as they were.
  * q_heads is a multiple of kv_heads, at most 16384.
  * `ws`: tabed_attention_nodes_workspace_bytes bytes, prepared once by ..._init; it then serves calls of any sizes and caches that need no more bytes, calls with

@@ -230,7 +230,7 @@ struct NodesWave {
         // themselves down to 2^-14 and to 2^-8 down to 2^-17.  A step with smaller ones, or with a scale outside 2^-38 to 2^38, is kFar: products in bf16, to 2^-8 whatever they are.
         // From there on a wave's steps are, up to the kMasked ones: in these, what others see must not count, and each product goes by itself, in fp16 or in bf16.
         // (One power of two a wave, by the largest scale that any of its queries saw, let a sibling's entry, or one that hardly counts, take all precision from the others.)
-        // For that choice scales count as 2^-40 to 2^50, so that the largest probability is in 2^-43 to 2^65, and the sum of them is none of tiny ones.
+        // For that choice scales count as 2^-40 to 2^38, so that the largest probability is in 2^-32 to 2^65: the sum of them is none of tiny ones, and products with tiny scales are there.
         constexpr float kRaise = MODE == kFar ? 25.f : 15.f, kLow = -16.9f;      // (fp16 ends at 2^15.99)
         bool apart = false;                                              // kMasked: there may be products for bf16; kWhole: the step is kFar
         float big = 0.f, little = 0.f;                                   // kWhole: log2 of the largest and the smallest scale of this lane's tokens
@@ -254,15 +254,15 @@ struct NodesWave {
                     } else {
                         const float lg = log2_of(v);
                         if constexpr (MASKED) most = fmaxf(most, lg), least = fminf(least, v == 0.f ? 0.f : lg);
-                        size[i][e] = __builtin_amdgcn_fmed3f(lg, -40.f, 50.f);
+                        size[i][e] = __builtin_amdgcn_fmed3f(lg, -40.f, 38.f);
                     }
                 }
             }
-            if constexpr (MASKED) apart = most > 50.f || least < -40.f;
+            if constexpr (MASKED) apart = most > 38.f || least < -40.f;
             if constexpr (MODE == kWhole) {
                 big = __builtin_amdgcn_logf(most);
                 little = __builtin_amdgcn_logf(least);
-                apart = big > 38.f || little < -38.f;
+                if (__any(big > 38.f || little < -38.f)) return false;
             }
         }
         // ---- the softmax, in units of log2.  Scores are taken relative to the maximum so far before the new one is known: it is raised only where it would be by

@@ -61,8 +61,14 @@ def check(B, cache, q, ctx, parents, prob=2.0 ** -8):
     # As in the tests of sizes: scores' sums in fp32, the product with the scale, the exponential of a difference of up to 2^7; then the result's own rounding, the
     # probability's, its error twice, the sums in fp32 (whose terms are up to 2^17 here: 2^-24 for every doubling of a sum's length, 2^-14 covers them).
     rel = (hd + 4) * 2.0 ** -24 * float((q.double().abs().sum(-1).amax() * k.abs().amax() * hd ** -0.5).clamp(max=2.0 ** 12)) + 2.0 ** -14
-    # Results below the smallest normal number of bf16 and fp32, 2^-126, may be rounded to 0 or to any of the few numbers there.
-    tol = 2.0 ** -8 * want.abs() + mass * (prob + 2 * rel + 2.0 ** -14) + 2.0 ** -126
+    # Results below the smallest normal number of bf16 and fp32, 2^-126, may be rounded to 0 or to any of the few numbers there.  So may probabilities, and products of
+    # them and scales: they are taken relative to the largest product, which becomes 2^7 at least, with scales counted as 2^-40 to 2^38.  No probability is above 1, so lost are
+    # probabilities, or products, below 2^-133 of the largest scale so counted: of each token that, once as it is and once times its scale, times a value of at most 448.
+    lost = 0.0
+    if cache.vscale is not None:
+        most = float(cache.vscale.max())
+        lost = (ctx + N) * 448 * 2.0 ** -133 * min(max(most, 2.0 ** -40), 2.0 ** 38) * max(1.0, most)
+    tol = 2.0 ** -8 * want.abs() + mass * (prob + 2 * rel + 2.0 ** -14) + 2.0 ** -126 + lost
     got = out.cpu().double()
     bad = (got - want).abs() > tol
     assert not bad.any(), f"{int(bad.sum())} of {bad.numel()} off, at most {float(((got - want).abs() / tol).nan_to_num(9e9).max()):.2f} times the tolerance"
@@ -88,6 +94,13 @@ SCALES = {"up": lambda t: torch.exp2(8.0 * (t // 32)), "down": lambda t: torch.e
 def test_scales_of_values(B, N, qh, kvh, hd, kind):
     ctx = 350
     check(B, make(B, ctx + N, kvh, hd, hd + N, SCALES[kind]), queries(N, qh, hd, 1), ctx, tree(N))
+
+
+@pytest.mark.parametrize("kind", ["both", "large", "up", "some"])
+@pytest.mark.parametrize("N,qh,kvh,hd,ctx", [(130, 12, 3, 256, 100), (40, 8, 2, 128, 350), (5, 4, 2, 64, 200), (17, 2, 1, 64, 900)])
+def test_scales_and_scores_far_apart(B, N, qh, kvh, hd, ctx, kind):
+    """Scores of 30 and more either side of the mean: products of any size, some of them of tokens whose value is 0 in a dim."""
+    check(B, make(B, ctx + N, kvh, hd, hd + N, SCALES[kind]), (20 * queries(N, qh, hd, 8).float()).to(torch.bfloat16), ctx, tree(N))
 
 
 @pytest.mark.parametrize("hd", [64, 128, 256])
