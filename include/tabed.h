@@ -527,9 +527,9 @@ int tabed_cache_append_nodes(const tabed_cache_paged* cache, int32_t layer, int3
  *   scale   > 0, commonly 1 / sqrt(head_dim)
  * Products of bf16 (and e4m3) values are exact, their sums, the softmax and its sum are in fp32; probabilities are rounded before the product with the
  * values, to bf16 (2^-8 of themselves), or with e4m3 values, and then times the values' scales: to fp16 (2^-11) relative to a query's largest such product, or to bf16 where they are
- * too far apart for that (below 2^-22 to 2^-29 of the largest; the context's others, too, from there on).  Products below 2^-130 of
- * the largest, in which a scale above 2^38 counts as that, and probabilities below 2^-95 of the largest may be lost.  What a node does not see has no influence, whatever it holds.  A node that
- * sees nothing (its blocks are not there) gets zeros and an lse of -inf.  Entries of nodes from n_nodes[r] on are left as they were.
+ * too far apart for that (below 2^-22 to 2^-29 of the largest; the context's others, too, from there on).  Products below 2^-130 of the largest, in
+ * which a scale above 2^38 counts as that, and probabilities below 2^-95 of the largest may be lost.  Sums are of probabilities up to 2^8 times values: magnitudes of values stay below
+ * 2^100.  What a node does not see has no influence, whatever it holds.  A node that sees nothing (its blocks are not there) gets zeros and an lse of -inf.  Entries of nodes from n_nodes[r] on are left as they were.
  * q_heads is a multiple of kv_heads, at most 16384.
  * `ws`: tabed_attention_nodes_workspace_bytes bytes, prepared once by ..._init; it then serves calls of any sizes and caches that need no more bytes, calls with
  * fewer rows or nodes among them.
@@ -568,6 +568,9 @@ int tabed_attention_nodes(const tabed_cache_paged* cache, int32_t layer, void* w
  *                 than the grid (2) then; else TABED_EUNSUPPORTED
  * `ws`: tabed_verify_nodes_workspace_bytes bytes, prepared once by ..._init; it then serves calls of any sizes that need no more bytes, all that are smaller in
  * everything among them.  It belongs to the library from the preparation on; calls that share it must not overlap.
+ * A sequence's workgroups wait for each other: V / 1024 of them, rounded up, with few sequences, else V / 2048, at most 128.  Launches that run at the same time on a device, those of
+ * other processes included, may hold (sequence's workgroups - 1) each of the 768 that run at a time (three a compute unit) waiting, and must leave some: six launches for V = 262144, ten for
+ * V = 152064, 24 for V = 32000 and few sequences.  The four hardware queues of one process are within that.  Kernels of others that wait for workgroups of their own in this way take from the 768.
  * A row whose workgroups waited for each other in vain, for some seconds, has no path: n_path and n_valid 0, path and out_tokens -1, flags[b][0] TABED_FLAG_DEGENERATE.
  * So have, at once, all rows of a call with a workspace that was prepared for fewer bytes than it needs, or never.
  */

@@ -15,9 +15,9 @@
 // barrier a tile; 1, 2 or 4 of them, as the row's own number of nodes has it, take different queries, and those with the same ones take turns at steps of 64 tokens.
 //
 // The cache's bytes bound it with few queries: 1 row of 120011 tokens, 32 / 8 heads of 128, one node 93 us (5.3 TB/s), 16 nodes 110; 64 rows of 256 to 768, 12 heads of
-// 64, 16 nodes 25 (4.2 TB/s).  With many the matrix cores and the softmax between the products do: 8 rows of 10000 tokens, 256 nodes, 32 / 8 heads of 128 430 us
-// (790 TFLOP/s; matrix cores 46 % of the cycles, vector instructions nearly all others, which two waves a SIMD overlap little), in e4m3 517 (every wave widens the
-// tile's values for its own queries: 340 more vector instructions a step of 64 tokens).
+// 64, 16 nodes 25 (4.2 TB/s).  With many the matrix cores and the softmax between the products do: 8 rows of 10000 tokens, 256 nodes, 32 / 8 heads of 128 434 us
+// (780 TFLOP/s; matrix cores 46 % of the cycles, vector instructions nearly all others, which two waves a SIMD overlap little), in e4m3 532 (every wave widens the
+// tile's values for its own queries: 320 more vector instructions a step of 64 tokens).
 #pragma once
 #include <algorithm>
 #include <mutex>
@@ -229,7 +229,9 @@ struct NodesWave {
         // the largest of these products, for every query by what it sees itself: 2^8 when it is chosen and up to 2^15 before it is chosen anew.  fp16 then holds products to 2^-11 of
         // themselves down to 2^-14 and to 2^-8 down to 2^-17.  A step with smaller ones, or with a scale outside 2^-38 to 2^38, is kFar: products in bf16, to 2^-8 whatever they are.
         // From there on a wave's steps are, up to the kMasked ones: in these, what others see must not count, and each product goes by itself, in fp16 or in bf16.
-        // (One power of two a wave, by the largest scale that any of its queries saw, let a sibling's entry, or one that hardly counts, take all precision from the others.)
+        // (One power of two a wave, by the largest scale that any of its queries saw, let a sibling's entry, or one that hardly counts, take all precision from the others.  It was
+        // 2 % faster: 16 ragged trees 78 us for 80; with scores of four times the spread, where steps are kFar, 80 for 85; 8 rows of 10000, 256 nodes 523 for 532.  Heads of 256 dims
+        // with more than 16 queries are short of registers: 4 rows of 3000, 64 nodes, 32 / 8 heads 70 for 80.)
         // For that choice scales count as 2^-40 to 2^38, so that the largest probability is in 2^-32 to 2^65: the sum of them is none of tiny ones, and products with tiny scales are there.
         constexpr float kRaise = MODE == kFar ? 25.f : 15.f, kLow = -16.9f;      // (fp16 ends at 2^15.99)
         bool apart = false;                                              // kMasked: there may be products for bf16; kWhole: the step is kFar
@@ -521,7 +523,7 @@ __device__ __forceinline__ int tiles_of(const NodesAttnArgs& a, int row, int tok
 
 // A row's length, for its share of the ranges.  UNIT: queries of a wave of four that share e4m3 tiles, 0 elsewhere.  Waves that have no queries of their own take turns
 // with others, so a tile of one or two units of queries takes about half the time of one with three or four (16 rows of 300 to 5000 tokens and 4 to 132 queries, head_dim
-// 128: 77 us against 89 with equal lengths; 8 rows of 4000 to 16000: 89 against 114).  With bf16, whose tiles take a step each and twice the bytes, longer ranges of such rows
+// 128: 80 us against 96 with equal lengths; 8 rows of 4000 to 16000: 95 against 123).  With bf16, whose tiles take a step each and twice the bytes, longer ranges of such rows
 // cost more than they give (78 against 72 us, 102 against 93).
 template <int UNIT>
 __device__ __forceinline__ int length_of(const NodesAttnArgs& a, int row, int tokens) {

@@ -12,7 +12,6 @@ hipError_t launch_keep_nodes(const tabed_cache_paged& c, int rows, int N, const 
 struct NodesAttnLayout {
     size_t off_ml;       // float4 [slots, kv_heads, tiles][queries of a tile] maxima and sums of ranges; before it the ranges of every row
     size_t off_o;        // float [slots, kv_heads, tiles][queries of a tile][head_dim] their sums of values
-    size_t total;
 };
 NodesAttnLayout nodes_attn_layout(const tabed_cache_paged& c, int rows, int N, int q_heads);
 size_t nodes_attn_bytes(const tabed_cache_paged& c, int rows, int N, int q_heads);

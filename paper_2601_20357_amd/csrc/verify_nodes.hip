@@ -15,14 +15,15 @@
 //
 // Why nothing waits for ever: workgroups are numbered as they start, sequence by sequence, so that a sequence's workgroups wait for ones that run already
 // or start as soon as any other sequence, or another kernel, ends; launches on the four queues of a process each hold back less than one sequence's
-// workgroups, at most 127 of the 768 that run at a time.  A workspace that was never prepared, or for less, is known by a mark.  A wait has a bound of some seconds all
+// workgroups, at most 127 of the 768 that run at a time.  (More launches at a time, as of several processes, can fill the device with workgroups that wait: seven do for rows of
+// 262144.  Nothing here can know of them; the caller keeps to a limit.)  A workspace that was never prepared, or for less, is known by a mark.  A wait has a bound of some seconds all
 // the same, and what comes of a row is then settled by one word: whoever has all of the walk's records and whoever gives up set it, the first of them for all.  A row that was
 // given up is left without a token, flagged, by its first workgroup; where it was not, who would have given up finds the records that it waited for.
 //
 // What bounds it: the steps, one after the other.  One is 4 to 5 us: 1 for the row's maximum and exponentials, 1.5 until all pieces' are known, 1 for their
-// sum, the rest for the distances, the test and the next node's rows; a launch with one node and nothing to test takes 8 to 12.  16 sequences of 22 nodes, V = 32000, 4
-// drafts: 40 us (the longest path of 16 visits five nodes); 1 of 6, a path of four: 23 us.  64 sequences, V = 128256, 8 drafts, half of them greedy: 196 us for 480 MB
-// and some 10^8 exponentials in 64 bits; 12 sequences run at a time.
+// sum, the rest for the distances, the test and the next node's rows; a launch with one node and nothing to test takes 8 to 12, and settling what comes of the row half a us of any.  16
+// sequences of 22 nodes, V = 32000, 4 drafts: 40 us (the longest path of 16 visits five nodes); 1 of 6, a path of four: 23 us.  64 sequences, V = 128256, 8 drafts, half of them
+// greedy: 208 us for 480 MB and some 10^8 exponentials in 64 bits; 12 sequences run at a time, and while one waits for its pieces its workgroups request the first child's row only.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
