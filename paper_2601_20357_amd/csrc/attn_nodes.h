@@ -16,8 +16,8 @@
 //
 // The cache's bytes bound it with few queries: 1 row of 120011 tokens, 32 / 8 heads of 128, one node 93 us (5.3 TB/s), 16 nodes 110; 64 rows of 256 to 768, 12 heads of
 // 64, 16 nodes 25 (4.2 TB/s).  With many the matrix cores and the softmax between the products do: 8 rows of 10000 tokens, 256 nodes, 32 / 8 heads of 128 434 us
-// (780 TFLOP/s; matrix cores 46 % of the cycles, vector instructions nearly all others, which two waves a SIMD overlap little), in e4m3 532 (every wave widens the
-// tile's values for its own queries: 320 more vector instructions a step of 64 tokens).
+// (780 TFLOP/s; matrix cores 46 % of the cycles, vector instructions nearly all others, which two waves a SIMD overlap little), in e4m3 527 (every wave widens the
+// tile's values for its own queries: 300 more vector instructions a step of 64 tokens).
 #pragma once
 #include <algorithm>
 #include <mutex>
@@ -230,8 +230,8 @@ struct NodesWave {
         // themselves down to 2^-14 and to 2^-8 down to 2^-17.  A step with smaller ones, or with a scale outside 2^-38 to 2^38, is kFar: products in bf16, to 2^-8 whatever they are.
         // From there on a wave's steps are, up to the kMasked ones: in these, what others see must not count, and each product goes by itself, in fp16 or in bf16.
         // (One power of two a wave, by the largest scale that any of its queries saw, let a sibling's entry, or one that hardly counts, take all precision from the others.  It was
-        // 2 % faster: 16 ragged trees 78 us for 80; with scores of four times the spread, where steps are kFar, 80 for 85; 8 rows of 10000, 256 nodes 523 for 532.  Heads of 256 dims
-        // with more than 16 queries are short of registers: 4 rows of 3000, 64 nodes, 32 / 8 heads 70 for 80.)
+        // a little faster: 16 ragged trees of up to 33 nodes 78.5 us for 79.0; with scores of four times the spread, where steps are kFar, 80 for 84; heads of 256 dims, 4 rows of 3000, 64
+        // nodes, 32 / 8 heads 72 for 76.)
         // For that choice scales count as 2^-40 to 2^38, so that the largest probability is in 2^-32 to 2^65: the sum of them is none of tiny ones, and products with tiny scales are there.
         constexpr float kRaise = MODE == kFar ? 25.f : 15.f, kLow = -16.9f;      // (fp16 ends at 2^15.99)
         bool apart = false;                                              // kMasked: there may be products for bf16; kWhole: the step is kFar
@@ -1023,7 +1023,18 @@ __global__ __launch_bounds__(T::kThreads, 2) void k_attention_nodes_wide(NodesAt
                 seen[b] = ~0ull;
                 if constexpr (mode.value == kMasked) seen[b] = pages >> (step * kStep / TABED_CACHE_BLOCK) & 1 ? window(s_mask[w.node[b]], j0) : 0ull;
             }
-            if (!w.template step<mode.value, T::RT>(sk, sk + T::kTile, sc, sc + T::kTokens, a.scale2, seen)) return step;
+            if constexpr (mode.value == kMasked && F8) {                 // (in halves: with 64 tokens, of which some are not seen, registers spill in all steps' way, 16 ragged trees 80 us for 79)
+#pragma unroll 1
+                for (int half = 0; half < 2; ++half) {
+                    uint32_t some[QW];
+#pragma unroll
+                    for (int b = 0; b < QW; ++b) some[b] = (uint32_t)(seen[b] >> half * 32);
+                    const unsigned char* const row = sk + half * kNodesTile * T::kRow;
+                    w.template step<kMasked, 2>(row, row + T::kTile, sc + half * kNodesTile, sc + T::kTokens + half * kNodesTile, a.scale2, some);
+                }
+            } else if (!w.template step<mode.value, T::RT>(sk, sk + T::kTile, sc, sc + T::kTokens, a.scale2, seen)) {
+                return step;
+            }
         }
         return kSteps;
     };

@@ -49,11 +49,12 @@ static NodesPlan plan_of(const tabed_cache_paged& c, int rows, int N, int q_head
     p.whole_tiles = std::max(1, kWholeRow / v.tokens);
     p.slots = rows;
     p.fill = (int)std::max<int64_t>(v.room / units, 2 * rows);
-    // Ranges of 512 tokens or more (4 rows of 4000 tokens, 16 nodes, 32 / 8 heads of 128: 34 us; of 1024 or more 44, of 256 or more 36), of rows of more than 1024 (one row of
-    // 600, 6 nodes, 12 heads of 64, four waves: whole 7.6 us, in two 12).  Where rows alone fill the chip they are cut only if one can be so long that the others would wait for it: of
-    // more than 8192 (64 rows of 2000, 12 nodes, 12 heads of 64: whole 72 us, cut 92).  How long a row can be goes by the table's width, since the lengths are known on the GPU alone: under
-    // a table of more than 8192 tokens those 64 rows are cut (101 us), and short rows, which never are, pay for the second launch (64 rows of 256 to 768, 16 nodes 24 us, then 37).  No more ranges than run at a time, also where a row's last tile of queries has little
-    // to do: the others' workgroups would wait for a second round (tiles of 96 and 36 queries, 16 rows of 300 to 5000: 93 us with as many as the queries would fill, 77 so).
+    // Ranges of 512 tokens or more (4 rows of 4000 tokens, 16 nodes, 32 / 8 heads of 128: 34 us; of 1024 or more 44, of 256 or more 36), of rows of more than 1024 (one row
+    // of 600, 6 nodes, 12 heads of 64, four waves: whole 7.6 us, in two 12).  Where rows alone fill the chip they are cut only if one can be so long that the others would
+    // wait for it: of more than 8192 (64 rows of 2000, 12 nodes, 12 heads of 64: whole 72 us, cut 92).  How long a row can be goes by the table's width, since the lengths
+    // are known on the GPU alone: under a table of more than 8192 tokens those 64 rows are cut (101 us), and short rows, which never are, pay for the second launch (64
+    // rows of 256 to 768, 16 nodes 24 us, then 37).  No more ranges than run at a time, also where a row's last tile of queries has little to do: the others' workgroups
+    // would wait for a second round (tiles of 96 and 36 queries, 16 rows of 300 to 5000: 93 us with as many as the queries would fill, 77 so).
     if (rows <= kMaxSplitRows && most > std::max(1, (v.room / units > rows ? kWholeRow : kLongRow) / v.tokens)) {
         p.split = 1;
         p.slots = (int)std::min<int64_t>(p.fill, rows * ((most + p.min_tiles - 1) / p.min_tiles));
