@@ -127,6 +127,22 @@ def test_a_large_sibling_is_nothing_to_those_beside_it(B, N, qh, kvh, hd, scale)
     check(B, cache, q.cpu(), ctx, parents)
 
 
+@pytest.mark.parametrize("N,qh,kvh", SHAPES)
+def test_a_large_sibling_beside_tokens_without_values(B, N, qh, kvh):
+    """As above, where the others see tokens whose scale is 0 next to it: what they add to the sums of probabilities, they add in the same order."""
+    hd = 64
+    for ctx, bad in ((75, 2), (60, 1), (0, 2)):
+        cache, parents, q = make(B, ctx + N, kvh, hd, 15), tree(N), queries(N, qh, hd, 13).to(DEV)
+        cache.vscale[0, :, :, ::3] = 0.0
+        below = torch.tensor([bad in ref.above(parents, 0, j) for j in range(N)])
+        clean = [x[0].cpu() for x in call(B, cache, q, ctx, parents)]
+        cache.vscale[0, (ctx + bad) // 64, :, (ctx + bad) % 64] = 2.0 ** 60
+        got = [x[0].cpu() for x in call(B, cache, q, ctx, parents)]
+        for a, c in zip(got, clean):
+            assert torch.equal(a[~below], c[~below])
+        check(B, cache, q.cpu(), ctx, parents)
+
+
 @pytest.mark.parametrize("bf16", [False, True])
 @pytest.mark.parametrize("hd", [64, 128, 256])
 @pytest.mark.parametrize("N,qh,kvh", SHAPES)
